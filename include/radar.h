@@ -407,6 +407,139 @@ size_t radar_noalloc_scratch_bytes(void);
 int radar_verify_accept_greedy_noalloc(radar_ctx* ctx, const radar_accept_args* args, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * The 4-bit paged cache: radar_cache_extend, radar_cache_store, radar_cache_load, radar_cache_attention.
+ * (The paper's steps read a prefix cache and say nothing of how it is held; this is one that takes 4.5 bits a value, kept up
+ * to date on the device between the acceptance of one step and the attention of the next.)
+ *
+ * Values.  16 consecutive channels of a token's key or value are a group: a scale s = 2^(E - 20) (1 + m / 8) in eight bits,
+ * E << 3 | m, and a code q in -8 .. 7 for each channel, held as q + 8; the value is q s, exact in bf16.  Every bit pattern is
+ * a finite number, so pages need no clearing.  A group is stored with s = max |x| / 7 rounded to four significant bits (ties
+ * to even) within [2^-20, 3840], and q = x / s rounded to an integer (ties to even) within -8 .. 7: values above 26880
+ * and below -30720 saturate.  A NaN is stored as 0 and records RADAR_ERR_NUMERIC.
+ * Blocks.  16 consecutive tokens of one KV head are a block of 18 d bytes: K codes (16 rows of d / 2), K scales (d), V codes, V
+ * scales.
+ *   K codes   d / 8 words of 32 bits a row; nibble n < 4 of a word is its channel 2 n, nibble 4 + n its channel 2 n + 1;
+ *   K scales  group g of row r at (r % 8) * d / 8 + g / w * 2 w + r / 8 * w + g % w, w = d / 64;
+ *   V codes   row r stands at place p = r % 2 * 4 + r % 8 / 2 + r / 8 * 8, its words as in K; with d = 128 the rows at places 2
+ *             and 3 of every four have their two halves of 32 bytes exchanged;
+ *   V scales  group g of the row at place p at g * 16 + p % 4 * 4 + p / 4.
+ * (The order in which the attention's threads read them: no two lanes of a warp meet in a bank.)
+ * Pages.  page_size tokens, 16, 32, 64 or a multiple of 128: [Hkv][page_size / 16] blocks, radar_cache_page_bytes; a pool is
+ * [n_pages] of them, 16-byte aligned, one pool a layer (layer_stride bytes apart).  Token j of request b is slot
+ * block_table[b * max_pages + j / page_size] * page_size + j % page_size.
+ * d is 64 or 128 in all four calls. */
+size_t radar_cache_page_bytes(int Hkv, int d, int page_size);
+
+/* radar_cache_extend - block tables and slots for the tokens that requests add or give up.
+ * Request b holds cache_len[b] tokens and changes by n = new_len[b] + extra (behind radar_verify_accept new_len is accept_len
+ * and extra 1: the root and the accepted nodes).  n < 0: it gives up its last tokens (a finished request all of them), and
+ * the pages that it no longer needs go onto the stack free_pages[0 .. free_count), request after request, in the order of its
+ * table.  n > 0: the pages that it lacks come from the top of the stack, request after request, behind all that was given up;
+ * a request whose pages are not there any more (counting what all requests before it asked for) gets none, granted[b] = 0,
+ * and keeps its length.  Outputs: block_table (only the entries of pages that were granted), free_pages, free_count_out,
+ * cache_len_out, granted, start[0 .. B] (the running sum of the added tokens, granted or not) and slots[start[b] + j] of
+ * the j-th added token, -1 where it was not granted.  With path_nodes ([B][path_stride]; entry j is the tree row of the j-th added
+ * token) src_row[start[b] + j] = b * rows + path_nodes[b][j], the row that radar_cache_store takes it from.
+ * cache_len_out may be cache_len and free_count_out free_count.  A request whose length would leave [0, max_pages * page_size],
+ * or is not in it, adds nothing and records RADAR_ERR_INVALID_ARG, as do a free_count outside [0, free_capacity], a stack
+ * that would overflow, a slot at or beyond slot_capacity (it is not written) and a path row outside [0, rows) (src_row -1). */
+typedef struct {
+    int B, page_size, max_pages;
+    const int32_t* cache_len;           /* [B] */
+    const int32_t* new_len;             /* [B] */
+    int extra;
+    int32_t* block_table;               /* [B][max_pages] in/out */
+    int32_t* free_pages;                /* [free_capacity] in/out */
+    const int32_t* free_count;          /* [1] */
+    int free_capacity;
+    int32_t* cache_len_out;             /* [B] */
+    int32_t* free_count_out;            /* [1] */
+    uint8_t* granted;                   /* [B] */
+    int32_t* start;                     /* [B + 1] */
+    int64_t* slots;                     /* [slot_capacity], NULL if that is 0 */
+    int64_t slot_capacity;
+    const int32_t* path_nodes;          /* [B][path_stride] or NULL */
+    int path_stride, rows;              /* with path_nodes */
+    int32_t* src_row;                   /* [slot_capacity], with path_nodes */
+} radar_cache_extend_args;
+
+int radar_cache_extend(radar_ctx* ctx, const radar_cache_extend_args* args, void* stream);
+
+/* radar_cache_store - rows of K and V into their slots, all layers in one call.
+ * Token i < n_tokens of layer l: row src_row[i] (i without src_row) of K and V, element h * d + c of a row at
+ * row * row_stride (rows of a fused projection are read in place), into slot slots[i] of the layer's pool.  A slot below 0 is
+ * skipped (a token that was not granted); one outside the pool, or a row outside [0, n_rows), records
+ * RADAR_ERR_INVALID_ARG and is skipped.  No two tokens of a call may have one slot.  K, V, row_stride and row_layer_stride
+ * times the element size: multiples of 16 bytes. */
+typedef struct {
+    int n_layers, Hkv, d, page_size;
+    int dtype;                          /* RADAR_F32 or RADAR_BF16: K and V */
+    int64_t n_tokens, n_rows, n_pages;
+    const void *K, *V;
+    int64_t row_stride, row_layer_stride;     /* elements */
+    const int64_t* slots;               /* [n_tokens] */
+    const int32_t* src_row;             /* [n_tokens] or NULL */
+    void* pages;
+    int64_t page_layer_stride;          /* bytes */
+} radar_cache_store_args;
+
+int radar_cache_store(radar_ctx* ctx, const radar_cache_store_args* args, void* stream);
+
+/* radar_cache_load - cached tokens as rows: of request b the tokens first[b] .. first[b] + start[b + 1] - start[b] - 1 become the
+ * rows start[b] .. of K and V ([n_layers][n_rows][Hkv][d], contiguous rows; RADAR_BF16 holds the values exactly).  start is
+ * non-decreasing, start[0] = 0.  Rows at or beyond n_rows, tokens outside [0, max_pages * page_size) and pages outside
+ * the pool record RADAR_ERR_INVALID_ARG and are skipped. */
+typedef struct {
+    int n_layers, B, Hkv, d, page_size, max_pages;
+    int dtype;                          /* RADAR_F32 or RADAR_BF16: K and V */
+    int64_t n_rows, n_pages;
+    const void* pages;
+    int64_t page_layer_stride;          /* bytes */
+    const int32_t* block_table;         /* [B][max_pages] */
+    const int32_t *first, *start;       /* [B], [B + 1] */
+    void *K, *V;
+    int64_t row_layer_stride;           /* elements */
+} radar_cache_load_args;
+
+int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* args, void* stream);
+
+/* radar_cache_attention - tree-masked attention of one layer over the 4-bit cache, GQA; what radar_tree_attention does over the
+ * rows that radar_cache_load would give.  Q and O [B][rows][Hq][d], Kt and Vt [B][rows][Hkv][d] in bf16, 1 <= rows <= 64 (1: single
+ * tokens); q_row_stride and kv_row_stride: elements between consecutive rows of Q, and of Kt and Vt (rows of a fused projection
+ * are read in place; the rows of a sequence follow those of the one before), O is contiguous.  Row i < n_nodes[b] attends to the
+ * prefix [0, cache_len[b]) and to the tree rows t < n_nodes[b] with bit t of mask[b][i] set (mask NULL: t <= i, a chain).
+ * Rows i >= n_nodes[b] of O and lse are left untouched; a row that attends to nothing gets 0, and lse -inf.
+ * lse (optional) [B][Hq][rows].  scale <= 0 selects 1/sqrt(d).  Products are accumulated in fp32; the probabilities enter P V as
+ * bf16.  max_cache_len (host) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes is out of range
+ * records RADAR_ERR_INVALID_ARG and is skipped; a page outside the pool records it too and is read as page 0.
+ * Q, Kt, Vt, O, pages and the row strides times two: 16 bytes; the workspace 256.
+ * Hq a multiple of Hkv, at most 128 query heads to a KV head.  The workspace's size is enough for any fewer sequences and any
+ * shorter max_cache_len. */
+typedef struct {
+    int B, Hq, Hkv, d, rows;
+    int dtype;                          /* RADAR_BF16 */
+    const void* Q;
+    const void *Kt, *Vt;
+    int64_t q_row_stride, kv_row_stride;
+    const uint64_t* mask;               /* [B][rows] or NULL */
+    const int32_t* n_nodes;             /* [B], or NULL: rows */
+    const void* pages;
+    int64_t n_pages;
+    int page_size, max_pages;
+    const int32_t* block_table;         /* [B][max_pages] */
+    const int32_t* cache_len;           /* [B] */
+    int max_cache_len;                  /* host value */
+    float scale;
+    void* O;
+    float* lse;                         /* or NULL */
+    void* workspace;
+    size_t workspace_bytes;
+} radar_cache_attn_args;
+
+size_t radar_cache_attn_workspace_bytes(const radar_ctx* ctx, int B, int Hq, int Hkv, int d, int rows, int max_cache_len);
+int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args* args, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * radar_policy_train_step - one REINFORCE step of the prediction model on a batch of data points {S, D}.
  * (Sec. 4.2: the MDP of Eq. 3-9 and the loss of Eq. 10; Sec. 4.3: the data point x = {S, D}, the acceptance
  * length drawn from d_T; App. "Implementation Details": the network, learning rate 1e-4, batches of 256.  The

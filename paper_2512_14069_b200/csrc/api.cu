@@ -102,6 +102,12 @@ extern "C" const char* radar_kernel_name(int id) {
         case RADAR_K_TRAIN_ADAM: return "train_adam";
         case RADAR_K_ROW_MERGE: return "row_merge";
         case RADAR_K_EXPAND_CALLS: return "expand_calls";
+        case RADAR_K_CACHE_EXTEND: return "cache_extend";
+        case RADAR_K_CACHE_LENGTHS: return "cache_lengths";
+        case RADAR_K_CACHE_STORE: return "cache_store";
+        case RADAR_K_CACHE_LOAD: return "cache_load";
+        case RADAR_K_CACHE_ATTN: return "cache_attention";
+        case RADAR_K_CACHE_COMBINE: return "cache_attention_combine";
         default: return "?";
     }
 }
@@ -148,7 +154,7 @@ extern "C" const char* radar_status_string(int status) {
         case RADAR_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case RADAR_ERR_CUDA: return "CUDA runtime error";
         case RADAR_ERR_TIMEOUT: return "a bounded device-side wait ran out";
-        case RADAR_ERR_NUMERIC: return "NaN in the logits";
+        case RADAR_ERR_NUMERIC: return "NaN in the logits, or in rows for the cache";
         case RADAR_ERR_TREE: return "inconsistent tree (pruned parent, bad draft row or token)";
         default: return "unknown status";
     }

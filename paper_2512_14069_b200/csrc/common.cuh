@@ -27,6 +27,12 @@ enum radar_kernel_id {
     RADAR_K_TRAIN_ADAM,         // REINFORCE step: batch loss + Adam update
     RADAR_K_ROW_MERGE,          // expansion: the merge of a long pass's rows
     RADAR_K_EXPAND_CALLS,       // radar_expand_calls: the calls of a sequence in one kernel
+    RADAR_K_CACHE_EXTEND,       // 4-bit cache: lengths, pages and block tables
+    RADAR_K_CACHE_LENGTHS,      // ... lengths and free count behind a launch of several blocks
+    RADAR_K_CACHE_STORE,
+    RADAR_K_CACHE_LOAD,
+    RADAR_K_CACHE_ATTN,
+    RADAR_K_CACHE_COMBINE,
     RADAR_K_COUNT
 };
 
@@ -42,7 +48,9 @@ enum radar_smem_slot {
     RADAR_SMEM_ACCLEN = RADAR_SMEM_WALK + 4,        // the same
     RADAR_SMEM_ATTN_FMA = RADAR_SMEM_ACCLEN + 4,        // + 4 * (bf16) + 2 * (d == 128) + (clusters)
     RADAR_SMEM_ATTN_TC = RADAR_SMEM_ATTN_FMA + 8,   // + 8 * fine + 4 * (d == 128) + 2 * two + paged
-    RADAR_SMEM_COUNT = RADAR_SMEM_ATTN_TC + 16
+    RADAR_SMEM_CACHE_ATTN = RADAR_SMEM_ATTN_TC + 16,   // + 4 * (d == 128) + row tiles of eight - 1
+    RADAR_SMEM_CACHE_EXTEND = RADAR_SMEM_CACHE_ATTN + 8,   // + (several blocks)
+    RADAR_SMEM_COUNT = RADAR_SMEM_CACHE_EXTEND + 2
 };
 
 struct radar_ctx {
