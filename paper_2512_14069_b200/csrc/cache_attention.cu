@@ -34,6 +34,7 @@ using tc05::mbar_drain;
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kStageKeys = 32;       // keys of a stage: two blocks
 constexpr float kMove = 8.f;         // log2 units
+constexpr int kTensorRows = 48;      // query rows of a KV head from which on the form of cache_attention_tc.cu takes them
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -54,9 +55,22 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+// m ln 2 + ln l, m in log2 units
+__device__ __forceinline__ float lse_of(float m, float l) {
+    constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
+    return fmaf(m, kHi, fmaf(m, kLo, logf(l)));
+}
+// eight channels of a finished row: O and, from one of its threads, lse
+__device__ __forceinline__ void write_row(const radar_cache_attn_args& a, int b, int node, int hq, int c, int D, const float (&o)[8], float m, float l, bool first) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(o[2 * e] * inv, o[2 * e + 1] * inv);
+        w[e] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * a.rows + node) * a.Hq + hq) * D + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (first && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = l > 0.f ? lse_of(m, l) : -CUDART_INF_F;
 }
 
 // What a warp keeps of its rows.  Thread (g, q) has rows 2q and 2q + 1 of each tile of eight.
@@ -508,7 +522,7 @@ extern "C" size_t radar_cache_attn_workspace_bytes(const radar_ctx* ctx, int B, 
     const Plan p = plan(ctx, B, Hkv, Hq / Hkv, rows, max_cache_len);
     const int64_t most = std::max<int64_t>(1, (max_cache_len + kWarps * kStageKeys - 1) / (kWarps * kStageKeys));
     const int64_t cut = std::max<int64_t>(B, (int64_t)ctx->sm_count * 12 / ((int64_t)Hkv * p.n_tiles));
-    return partial_bytes(std::min(B * most, cut) * rows * Hq, d);
+    return std::max(partial_bytes(std::min(B * most, cut) * rows * Hq, d), cache_attn_tc_workspace_bytes(ctx, d));
 }
 
 extern "C" int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args* a, void* stream_) {
@@ -529,6 +543,7 @@ extern "C" int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args
     CacheAttnParams P;
     P.a = *a;
     P.G = a->Hq / a->Hkv;
+    if (a->rows * P.G >= kTensorRows) return cache_attn_tc_launch(ctx, a, stream);
     const Plan p = plan(ctx, a->B, a->Hkv, P.G, a->rows, a->max_cache_len);
     P.n_tiles = p.n_tiles;
     P.n_splits = p.n_splits;

@@ -1,0 +1,853 @@
+// Attention over the 4-bit paged cache for many query rows (whole draft trees), on the tensor cores.
+//
+// The tile space, the softmax groups, the issuing warp and the epilogue are those of tree_attention_tc.cu: units of (sequence, KV head,
+// pair of row blocks of 128 query rows), their tiles of 128 keys laid end to end and cut into equal ranges, one thread a query
+// row.  What differs is where a tile comes from: the producer fetches blocks as they lie in the cache (bulk copies, 64 keys of a
+// head a stage, K and V together), and four warps decode them into the bf16 tiles that the products read, exactly (cache.cuh).
+// These warps also do the epilogue, which falls to them once a segment.
+//   warps 0-3 / 4-7  softmax groups 0 / 1
+//   warps 8-11       decoders: a block of 16 keys of every stage each; tree rows by TMA; epilogue
+//   warp 12          producer: segments, stages, Q
+//   warp 13          issues the products
+// K and V have two tiles each (three are worth no more, and the stages need the room).
+#include <cmath>
+#include <type_traits>
+
+#include "cache_attention.cuh"
+#include "tree_tiles.cuh"
+
+namespace radar {
+namespace {
+
+using namespace cache4;
+
+constexpr int kTcThreads = 512;
+constexpr int kEpilogueWarp = 8, kDecodeWarps = 4, kProducerWarp = 12, kMmaWarp = 13;
+// Registers a thread: 128 at launch, then shared out by warpgroup (two of softmax; what they take the other two give).
+constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
+static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
+constexpr int kStaticSmem = 3072;
+constexpr int kStageKeys = 64;       // keys of a stage: a block for each decoder
+static_assert(kStageKeys == kDecodeWarps * kBlock && 2 * kStageKeys == kTileKeys, "two stages a tile, a block a warp");
+
+template <int D, bool TWO>
+struct Smem {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kQBlock = 128 * D * 2;
+    static constexpr int kQBytes = (TWO ? 2 : 1) * kQBlock;
+    static constexpr int kTileBytes = kTileKeys * D * 2;
+    static constexpr int kStageBytes = kStageKeys / kBlock * Layout<D>::kBytes;
+    static constexpr int kRingK = 2, kRingV = 2;
+    static constexpr int kRoom = 227 * 1024 - kStaticSmem - kQBytes - (kRingK + kRingV) * kTileBytes;
+    static constexpr int kRingS = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
+    static_assert(kRingS >= 2, "both halves of a tile are in the ring together");
+    static constexpr int kDynamic = kQBytes + (kRingK + kRingV) * kTileBytes + kRingS * kStageBytes;
+};
+
+// 32 channels of a row, two groups: four chunks of 16 bytes of the swizzled row, from chunk `chunk` on.
+__device__ __forceinline__ void store_channels(const uint4 w, uint32_t byte0, uint32_t byte1, unsigned char* row, int chunk, int key7) {
+    const uint32_t s0 = scale_pair(byte0), s1 = scale_pair(byte1), f0 = offset_pair(s0), f1 = offset_pair(s1);
+    auto put = [&](int c, uint32_t x, uint32_t s, uint32_t f) {
+        *reinterpret_cast<uint4*>(row + (((chunk + c) ^ key7) << 4)) = make_uint4(decode<0>(x, s, f), decode<1>(x, s, f), decode<2>(x, s, f), decode<3>(x, s, f));
+    };
+    put(0, w.x, s0, f0);
+    put(1, w.y, s0, f0);
+    put(2, w.z, s1, f1);
+    put(3, w.w, s1, f1);
+}
+
+// One block's keys into rows key0 .. key0 + 15 of a K-major tile with the 128-byte swizzle.  A lane takes 32 channels of a row.
+template <int D>
+__device__ __forceinline__ void decode_keys(const unsigned char* block, unsigned char* tile, int key0) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kPasses = D / 64, kRows = 16 / kPasses;
+    const int q = D == 128 ? (lane & 1) | (lane >> 4) << 1 : lane & 1, r0 = (lane >> 1) & (kRows - 1);
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int r = r0 + pass * kRows;
+        const uint4 w = *reinterpret_cast<const uint4*>(block + r * Layout<D>::kRow + q * 16);
+        uint32_t b0, b1;
+        if (D == 128) {
+            const uint32_t sc = *reinterpret_cast<const uint16_t*>(block + Layout<D>::kKScales + (r & 7) * 16 + q * 4 + (r >> 3) * 2);
+            b0 = __byte_perm(sc, 0, 0x4040);
+            b1 = __byte_perm(sc, 0, 0x4141);
+        } else {
+            const unsigned char* sc = block + Layout<D>::kKScales + (r & 7) * 8 + q * 4 + (r >> 3);
+            b0 = sc[0] * 0x10001u;
+            b1 = sc[2] * 0x10001u;
+        }
+        store_channels(w, b0, b1, tile + (q >> 1) * (kTileKeys * 128) + (key0 + r) * 128, (q & 1) * 4, r & 7);
+    }
+}
+// ... and its values, whose rows stand in the order of their places.
+template <int D>
+__device__ __forceinline__ void decode_values(const unsigned char* block, unsigned char* tile, int key0) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kPasses = D / 64;
+    const int q = D == 128 ? (lane & 1) | (lane >> 4) << 1 : lane & 1;
+    const int p0 = ((lane >> 1) & 1) | ((lane >> 2) & 1) << 2 | ((lane >> 3) & 1) << 1 | (D == 64 ? (lane >> 4) << 3 : 0);
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int p = p0 + pass * 8, r = (p & 3) << 1 | ((p >> 2) & 1) | (p & 8);
+        const uint4 w = *reinterpret_cast<const uint4*>(block + Layout<D>::kVCodes + p * Layout<D>::kRow + ((q * 16) ^ (D == 128 && (p & 2) ? 32 : 0)));
+        const unsigned char* sc = block + Layout<D>::kVScales + q * 32 + (p & 3) * 4 + (p >> 2);
+        store_channels(w, sc[0] * 0x10001u, sc[16] * 0x10001u, tile + (q >> 1) * (kTileKeys * 128) + (key0 + r) * 128, (q & 1) * 4, r & 7);
+    }
+}
+
+// TWO: the launch may contain units with two live row blocks; decides the shared-memory layout
+template <int D, bool TWO>
+__global__ void __launch_bounds__(kTcThreads, 1)
+cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKt,
+                     const __grid_constant__ CUtensorMap tmVt, const TcParams P) {
+    chain_trigger();                     // every warp waits for the predecessor where its role begins; the barrier,
+                                         // tensor-memory and descriptor set-up needs nothing from global memory
+    using SM = Smem<D, TWO>;
+    constexpr int H = SM::kHalves;
+    constexpr int RK = SM::kRingK, RV = SM::kRingV, RS = SM::kRingS;
+    const radar_attn_args& a = P.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int pp = blockIdx.x % P.n_cls;                    // class
+    const int ci = blockIdx.x / P.n_cls;
+    const int G = P.G;
+
+    // Static block first (padded to a multiple of 1024 bytes and aligned to it), the tiles behind it: the
+    // swizzled tiles need a 1024-byte boundary and there is no room left for alignment slack.
+    struct __align__(1024) Static {
+        uint64_t bar_qfull, bar_qempty, bar_kfull[RK], bar_kempty[RK], bar_vfull[RV], bar_vempty[RV];
+        uint64_t bar_stfull[RS], bar_stempty[RS];      // the cache's bytes as they lie there, 64 keys a stage
+        uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2];
+        uint64_t bar_idle;               // every product issued has run
+        uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
+        uint64_t bar_pready[2];          // ... all of them
+        uint64_t bar_mlfull, bar_mlempty;
+        uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
+        Segment seg[kSegRing];
+        float2 ml[2][128];               // per group: (m in log2 units, l) of the rows at the end of a segment
+        uint32_t q_last, st_next, k_tree, v_tree;    // what is in flight at the end: phase parity of the last Q, ...
+        uint32_t tmem_base;
+        int abort;
+    };
+    static_assert(sizeof(Static) <= kStaticSmem, "static shared-memory block");
+    __shared__ union { Static st; unsigned char bytes[kStaticSmem]; } s_static;
+    Static& st = s_static.st;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* sQ = smem_raw;
+    unsigned char* sK = sQ + SM::kQBytes;
+    unsigned char* sV = sK + RK * SM::kTileBytes;
+    unsigned char* sS = sV + RV * SM::kTileBytes;
+
+    // ---- set-up ----
+    if (warp == 0) {
+        if (lane == 0) {
+            st.abort = 0;
+            mbar_init(&st.bar_qfull, 1);
+            mbar_init(&st.bar_qempty, 1);
+            for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], kDecodeWarps); mbar_init(&st.bar_kempty[i], 1); }
+            for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecodeWarps); mbar_init(&st.bar_vempty[i], 1); }
+            for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[i], 1); mbar_init(&st.bar_stempty[i], kDecodeWarps); }
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
+                mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
+            }
+            for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
+            mbar_init(&st.bar_idle, 1);
+            st.q_last = 1;
+            st.st_next = st.k_tree = st.v_tree = 0;
+            mbar_init(&st.bar_mlfull, 8);
+            mbar_init(&st.bar_mlempty, 4);
+            fence_barrier_init();
+        }
+    } else if (warp == kMmaWarp) {
+        tmem_alloc(&st.tmem_base, 512);
+        tmem_relinquish();
+        if (lane == 0) {
+            tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmKt); tma_prefetch_desc(&tmVt);
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    // All of tensor memory is this CTA's, so its addresses are constants (the producer checks): S/P buffers in columns 0 and
+    // 128, O accumulators in 256 and 384.  An address that the compiler does not know to be the same in every lane costs the
+    // issuing warp a handful of instructions for every product.
+    constexpr uint32_t tmem = 0;
+    bool ok = true;                         // no wait of this thread has run out
+    // Each role starts with chain_sync(): the bounds of the waits behind it are for this kernel's own work.  (A warp that went
+    // straight to its first wait would spend them on whatever is left of the predecessor.)
+    // the producer's next segment; false behind the last one
+    auto take_segment = [&](uint32_t seg, Segment& s) {
+        ok = mbar_wait_while(ok, &st.bar_segfull[seg % kSegRing], (seg / kSegRing) & 1);
+        ok = __all_sync(kFull, ok);
+        s = st.seg[seg % kSegRing];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&st.bar_segempty[seg % kSegRing]);
+        return ok && s.n > 0;
+    };
+
+    if (warp < kEpilogueWarp) {
+        regs_inc<kSoftmaxRegs>();
+        chain_sync();
+        // =================================== softmax groups ===================================
+        // One thread per query row, which holds the tile's 128 scores in registers: tensor memory is read once and no two
+        // threads have to agree on a maximum.  (Two threads a row, 64 scores each read twice for want of registers, was the
+        // form before: 32 layers, 8 sequences of 6000 to 8192 tokens, 64 / 8 heads 4118 -> 3930 us; one layer of it within a
+        // step 307 -> 295; 32 layers of one sequence of 2048 tokens, 32 / 8 heads 105 -> 101.)
+        const int grp = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;                 // row of the block == tensor-memory lane
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + grp * 128 + lane_addr;
+        const uint32_t tO = tmem + 256 + grp * 128 + lane_addr;
+        const int rb_node = (int)(((uint32_t)row * P.g_magic) >> 16);        // row / G
+        uint32_t sc = 0;                         // S tiles this group has waited for
+        Segment s;
+        for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+            const bool two = TWO && s.rows > P.rb_rows;
+            const int blk = two ? grp : 0;                       // row block within the unit
+            const int node = (pp * P.n_blk + blk) * P.nodes_per_rb + rb_node;
+            const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
+            // A warp none of whose 32 rows is live does no arithmetic (the products of its rows are never read):
+            // it only keeps the barriers going.
+            const bool warp_live = row - lane < rows_here;
+            // the row's ancestor word is needed by the tree tile only (the unit's last): it is loaded here and first
+            // touched there, so that the segment does not start with a wait for global memory
+            uint32_t mask_lo, mask_hi;
+            if (a.mask != nullptr) {
+                asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(mask_lo), "=r"(mask_hi) : "l"(a.mask + (int64_t)s.b * P.nodes + min(node, P.nodes - 1)));
+            } else {                             // a chain
+                mask_lo = node >= 31 ? 0xffffffffu : (2u << node) - 1u;
+                mask_hi = node < 32 ? 0u : node >= 63 ? 0xffffffffu : (2u << (node - 32)) - 1u;
+            }
+            const int n_my = two ? s.n : (s.n - grp + 1) >> 1;
+            float m_run = -CUDART_INF_F, l_run = 0.f;
+
+#pragma unroll 1
+            for (int j = 0; j < n_my; ++j) {
+                const int t = s.t0 + (two ? j : 2 * j + grp);
+                ok = mbar_wait_while(ok, &st.bar_sfull[grp], sc & 1);
+                ok = __all_sync(kFull, ok);                      // warp-uniform: guards .aligned ops
+                ++sc;
+                tc_fence_after_sync();
+                if (ok && warp_live) {
+                    uint32_t sv[4][32];
+                    const int valid = s.Pb - t * kTileKeys;
+                    if (t == s.nt - 1 || valid < kTileKeys) {
+                        // Keys that the row may not attend to (and, of the tree tile, which has 64, the columns that are stale)
+                        // become -inf in tensor memory, 32 at a time: one tile of a unit or two need it, and an unrolled path
+                        // for them would be fetched into the instruction cache anew each time.
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t al;
+                            if (t == s.nt - 1) {
+                                const int live = s.M - c * 32;
+                                al = row < rows_here && c < 2 && live > 0 ? (c == 0 ? mask_lo : mask_hi) & (live >= 32 ? 0xffffffffu : (1u << live) - 1u) : 0u;
+                            } else {
+                                const int lim = valid - c * 32;
+                                al = lim >= 32 ? 0xffffffffu : (lim <= 0 ? 0u : ((1u << lim) - 1u));
+                            }
+                            tmem_ld32(tS + c * 32, sv[0]);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((al >> e) & 1u)) sv[0][e] = 0xff800000u;     // -inf
+                            tmem_st32(tS + c * 32, sv[0]);
+                        }
+                        tmem_wait_st();
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sv[c]);
+                    tmem_wait_ld();
+                    float mxa[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        mxa[c] = __uint_as_float(sv[c][0]);
+#pragma unroll
+                        for (int e = 1; e < 31; e += 2)                     // three-input maxima: half the instructions
+                            mxa[c] = max3(mxa[c], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
+                        mxa[c] = fmaxf(mxa[c], __uint_as_float(sv[c][31]));
+                    }
+                    const float mx = fmaxf(max3(mxa[0], mxa[1], mxa[2]), mxa[3]);
+                    // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
+                    const float m_tile = mx * P.scale_log2;
+                    float factor = 1.f;
+                    if (j == 0) {
+                        m_run = m_tile;
+                    } else if (m_tile > m_run + kRescaleThreshold) {
+                        factor = ex2(m_run - m_tile);           // m_run may be -inf: factor 0 clears O and l
+                        m_run = m_tile;
+                    }
+                    const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
+                    if (j > 0 && __any_sync(kFull, factor != 1.f)) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st16(tO + c, o);
+                        }
+                    }
+                    // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
+                    // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
+                    // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
+                    // two of them.
+                    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
+                    uint32_t pk[16];
+                    auto scale = [&](const int p) {
+                        uint32_t &x = sv[p >> 4][2 * (p & 15)], &y = sv[p >> 4][2 * (p & 15) + 1];
+                        const float2 s2 = make_float2(__uint_as_float(x), __uint_as_float(y));
+                        const float2 t2 = fma2_in_order(s2, sc2, nm2);
+                        x = __float_as_uint(t2.x);
+                        y = __float_as_uint(t2.y);
+                    };
+                    auto finish = [&](const int p) {
+                        const float p0 = __uint_as_float(sv[p >> 4][2 * (p & 15)]), p1 = __uint_as_float(sv[p >> 4][2 * (p & 15) + 1]);
+                        ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
+                        pk[p & 15] = bf16x2_in_order(p0, p1);
+                        if ((p & 15) == 15) tmem_st16(tS + (p >> 4) * 16, pk);
+                    };
+                    // pairs that the scaling is ahead, that the rest is behind, and that the first stores are given to land in
+                    constexpr int kAhead = 2, kLag = 4, kLanding = 4;
+#pragma unroll
+                    for (int p = 0; p < kAhead; ++p) scale(p);
+#pragma unroll
+                    for (int p = 0; p < 64 + kLag; ++p) {
+                        if (p < 64) sv[p >> 4][2 * (p & 15)] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15)])));
+                        if (p + kAhead < 64) scale(p + kAhead);
+                        if (p < 64) sv[p >> 4][2 * (p & 15) + 1] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15) + 1])));
+                        if (p >= kLag) finish(p - kLag);
+                        if (p == kFirstKeys / 2 - 1 + kLag + kLanding) {
+                            tmem_wait_st();
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&st.bar_pfirst[grp]);
+                        }
+                    }
+                    l_run = l_run * factor + ((ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
+                    tmem_wait_st();
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (!(ok && warp_live)) mbar_arrive(&st.bar_pfirst[grp]);
+                    mbar_arrive(&st.bar_pready[grp]);
+                }
+            }
+
+            // the rows' (m, l) go to the epilogue, which has taken those of the segment before
+            ok = mbar_wait_while(ok, &st.bar_mlempty, (seg & 1) ^ 1);
+            st.ml[grp][row] = make_float2(m_run, l_run);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&st.bar_mlfull);
+        }
+    } else if (warp < kProducerWarp) {
+        regs_dec<kEpilogueRegs>();
+        chain_sync();
+        // =================================== decoders, and epilogue ===================================
+        // A warp takes one block of 16 keys of every stage.  Its lanes are dealt out over rows and channels so that the eight
+        // lanes of a phase of a 16-byte store write to eight different chunks of the 128-byte swizzle.  The epilogue of a segment
+        // comes behind the first tile of the next one, when its last product is about done: the products have a tile to go on with.
+        const int row = (warp - kEpilogueWarp) * 32 + lane;
+        const uint32_t tO = tmem + 256 + ((uint32_t)((warp - kEpilogueWarp) * 32) << 16);
+        const int rb_node = (int)(((uint32_t)row * P.g_magic) >> 16);        // row / G
+        uint32_t oc[2] = {0, 0};             // accumulators waited for
+        auto epilogue = [&](const Segment& s, const uint32_t seg) {
+            const bool two = TWO && s.rows > P.rb_rows;
+            const bool final_rows = s.n == s.nt;                 // the whole unit
+            const int slot = seg == 0 ? 0 : 1;                   // a CTA has at most a cut first and a cut last segment
+            ok = mbar_wait_lazy(ok, &st.bar_mlfull, seg & 1);
+            const float2 ml0 = st.ml[0][row], ml1 = st.ml[1][row];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&st.bar_mlempty);
+#pragma unroll 1
+            for (int blk = 0; blk < 2; ++blk) {
+                // two live row blocks: accumulator blk is row block blk; one: both belong to it, merged in the first trip
+                if (blk == 1 && !two) {
+                    if (lane == 0) mbar_arrive(&st.bar_ofree[1]);
+                    break;
+                }
+                ok = mbar_wait_while(ok, &st.bar_odone[blk], oc[blk] & 1);
+                ++oc[blk];
+                const bool merge = !two && s.n > 1;
+                if (merge) {
+                    ok = mbar_wait_while(ok, &st.bar_odone[1], oc[1] & 1);
+                    ++oc[1];
+                }
+                ok = __all_sync(kFull, ok);
+                tc_fence_after_sync();
+                const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
+                const bool row_live = row < rows_here;
+                if (ok && row - lane < rows_here) {
+                    float m_out = blk == 0 ? ml0.x : ml1.x, l_out = blk == 0 ? ml0.y : ml1.y, w0 = 1.f, w1 = 0.f;
+                    if (merge) {
+                        m_out = fmaxf(ml0.x, ml1.x);
+                        const float ms = m_out == -CUDART_INF_F ? 0.f : m_out;
+                        w0 = ex2(ml0.x - ms);                        // exp2(-inf) = 0
+                        w1 = ex2(ml1.x - ms);
+                        l_out = ml0.y * w0 + ml1.y * w1;
+                    }
+                    const float m_safe = m_out == -CUDART_INF_F ? 0.f : m_out;
+                    const float inv = final_rows ? (l_out > 0.f ? 1.f / l_out : 0.f) : 1.f;
+                    const int node = (pp * P.n_blk + blk) * P.nodes_per_rb + rb_node;
+                    const int hq = s.g * G + row - rb_node * G;
+                    const int64_t out_row = ((int64_t)s.b * P.nodes + node) * a.Hq + hq;
+                    const int64_t rec = ((int64_t)blockIdx.x * 2 + slot) * kPairRows + blk * 128 + row;
+                    __nv_bfloat16* dst_o = reinterpret_cast<__nv_bfloat16*>(a.O) + out_row * D;
+                    float* dst_p = P.part_o + rec * D;                  // 128-byte aligned (workspace carve)
+                    const bool wide = (reinterpret_cast<uintptr_t>(dst_o) & 31) == 0;
+#pragma unroll 1
+                    for (int col = 0; col < D; col += 16) {
+                        uint32_t o[16], o2[16];
+                        tmem_ld16(tO + blk * 128 + col, o);
+                        if (merge) tmem_ld16(tO + 128 + col, o2);
+                        tmem_wait_ld();
+                        float v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(o[e]) * w0;
+                        if (merge) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = fmaf(__uint_as_float(o2[e]), w1, v[e]);
+                        }
+                        if (row_live) {
+                            uint32_t w[8];
+                            if (final_rows) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const __nv_bfloat162 t2 = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
+                                    w[e] = *reinterpret_cast<const uint32_t*>(&t2);
+                                }
+                                if (wide) {
+                                    st_global_32b(dst_o + col, w);
+                                } else {
+                                    *reinterpret_cast<uint4*>(dst_o + col) = make_uint4(w[0], w[1], w[2], w[3]);
+                                    *reinterpret_cast<uint4*>(dst_o + col + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[q * 8 + e]);
+                                    st_global_32b(dst_p + col + q * 8, w);
+                                }
+                            }
+                        }
+                    }
+                    if (row_live) {
+                        const float m_nat = m_safe * 0.6931471805599453f;
+                        if (final_rows) {
+                            if (a.lse != nullptr) a.lse[((int64_t)s.b * a.Hq + hq) * P.nodes + node] = l_out > 0.f ? m_nat + logf(l_out) : -CUDART_INF_F;
+                        } else {
+                            P.part_ml[rec] = make_float2(m_out == -CUDART_INF_F ? m_out : m_nat, l_out);
+                        }
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.bar_ofree[blk]);
+            }
+        };
+        uint32_t k_slot = 0, k_par = 1, v_slot = 0, v_par = 1, st_slot = 0, st_par = 0;
+        const int blk16 = warp - kEpilogueWarp;
+        auto next_stage = [&](uint32_t& slot, uint32_t& par) { if (++slot == RS) { slot = 0; par ^= 1; } };
+        // one tile: both halves of K, then both of V
+        auto decode_tile = [&](const Segment& s, const int t) {
+            const bool tree = t == s.nt - 1;
+            if (tree) {
+                for (int is_v = 0; is_v < 2; ++is_v) {
+                    uint32_t &slot = is_v ? v_slot : k_slot, &par = is_v ? v_par : k_par;
+                    ok = mbar_wait_while(ok, is_v ? &st.bar_vempty[slot] : &st.bar_kempty[slot], par);
+                    ok = __all_sync(kFull, ok);
+                    uint64_t* full = is_v ? &st.bar_vfull[slot] : &st.bar_kfull[slot];
+                    if (lane == 0) {
+                        if (blk16 == 0 && ok) {
+                            mbar_arrive_expect_tx(full, kTreeKeys * D * 2);
+                            for (int h = 0; h < H; ++h)
+                                tma_load_4d((is_v ? sV : sK) + slot * SM::kTileBytes + h * (kTreeKeys * 128), is_v ? &tmVt : &tmKt, full, h * 64, s.g, s.b * P.nodes, 0);
+                            (is_v ? st.v_tree : st.k_tree) = 1u | slot << 8 | (par ^ 1) << 16;
+                        } else if (ok) {
+                            mbar_arrive(full);
+                        }
+                    }
+                    if (++slot == (uint32_t)(is_v ? RV : RK)) { slot = 0; par ^= 1; }
+                }
+                return;
+            }
+            const int halves = min(2, (s.Pb - t * kTileKeys + kStageKeys - 1) / kStageKeys);
+            ok = mbar_wait_while(ok, &st.bar_kempty[k_slot], k_par);
+            uint32_t sl = st_slot, pr = st_par;
+            for (int half = 0; half < halves; ++half) {
+                ok = mbar_wait_while(ok, &st.bar_stfull[sl], pr);
+                decode_keys<D>(sS + sl * SM::kStageBytes + blk16 * Layout<D>::kBytes, sK + k_slot * SM::kTileBytes, half * kStageKeys + blk16 * 16);
+                next_stage(sl, pr);
+            }
+            fence_proxy_async_smem();
+            ok = __all_sync(kFull, ok);
+            if (lane == 0 && ok) mbar_arrive(&st.bar_kfull[k_slot]);
+            if (++k_slot == RK) { k_slot = 0; k_par ^= 1; }
+            ok = mbar_wait_while(ok, &st.bar_vempty[v_slot], v_par);
+            for (int half = 0; half < halves; ++half) {
+                decode_values<D>(sS + st_slot * SM::kStageBytes + blk16 * Layout<D>::kBytes, sV + v_slot * SM::kTileBytes, half * kStageKeys + blk16 * 16);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.bar_stempty[st_slot]);
+                next_stage(st_slot, st_par);
+            }
+            fence_proxy_async_smem();
+            ok = __all_sync(kFull, ok);
+            if (lane == 0 && ok) mbar_arrive(&st.bar_vfull[v_slot]);
+            if (++v_slot == RV) { v_slot = 0; v_par ^= 1; }
+        };
+        Segment s, done;
+        done.n = 0;
+        uint32_t seg = 0;
+        for (; take_segment(seg, s); ++seg) {
+            decode_tile(s, s.t0);
+            if (seg > 0) epilogue(done, seg - 1);
+#pragma unroll 1
+            for (int i = 1; i < s.n; ++i) decode_tile(s, s.t0 + i);
+            done = s;
+        }
+        if (seg > 0) epilogue(done, seg - 1);
+    } else {
+        regs_dec<kIssueRegs>();
+        chain_sync();                            // every global access of the CTA comes behind one
+        if (warp == kProducerWarp) {
+            // =================================== TMA producer ===================================
+            // The whole warp walks the tiles: lane c fetches copy c of a stage (a page holds 64 keys of a head in one piece, or fewer),
+            // the leading lane does the waits, the byte counts and Q.
+            const bool lead = lane == 0;
+            const bool usable = (smem_u32(smem_raw) & 1023u) == 0 && st.tmem_base == 0;     // (else the tiles would not sit on their swizzle boundary)
+            if (!usable && lead) set_status(P.status, RADAR_ERR_CUDA);
+            long long tot_all;
+            Cursor<kFourBit> cur = first_segment<kFourBit>(P, pp, ci, tot_all);
+            if (!usable) cur.t0 = cur.t1 = 0;
+            Cut cut;
+            cut.unit.valid = 0;
+            cut.tot = tot_all;
+            uint32_t st_slot = 0, st_par = 1;
+            const int per = min(P.blocks_per_page, kStageKeys / kBlock);          // blocks of a copy
+            for (uint32_t seg = 0;; ++seg) {
+                const bool on = cur.valid();
+                const int b = cur.b, g = cur.g, n = cur.t1 - cur.t0, t0 = cur.t0, nt = cur.s.nt, Pb = cur.s.Pb;
+                const bool two = TWO && cur.two_rb(P);
+                if (lead) {
+                    ok = mbar_wait_while(ok, &st.bar_segempty[seg % kSegRing], ((seg / kSegRing) & 1) ^ 1);
+                    Segment s;                       // (behind a wait that ran out the others are sent home)
+                    s.n = on && ok ? n : 0; s.t0 = t0; s.nt = nt; s.Pb = Pb; s.M = cur.s.M; s.rows = cur.s.rows; s.b = b; s.g = g; s.layer = 0;
+                    st.seg[seg % kSegRing] = s;
+                    mbar_arrive(&st.bar_segfull[seg % kSegRing]);
+                }
+                if (!on) break;
+                if (t0 == 0 && n < nt) {                             // necessarily the last segment of this CTA
+                    cut.unit.valid = 1; cut.unit.b = b; cut.unit.g = g; cut.unit.slot = seg == 0 ? 0 : 1; cut.unit.layer = 0; cut.unit.rows = cur.s.rows;
+                    cut.nt = nt; cut.w = cur.s.w; cut.u0 = cur.U;
+                }
+                cur.next(P, pp);
+                const int32_t* table = a.block_table + (long long)b * a.max_pages;
+                // The segment's first tile, then Q (its slot is free only behind the last S of the segment before), then the rest.
+#pragma unroll 1
+                for (int i = 0; i < n; ++i) {
+                    const int key = (t0 + i) * kTileKeys, left = t0 + i == nt - 1 ? 0 : min(kTileKeys, Pb - key);
+#pragma unroll 1
+                    for (int from = 0; from < left; from += kStageKeys) {
+                        const int blocks = min(kStageKeys / kBlock, (left - from + kBlock - 1) / kBlock);
+                        const bool copies = lane * per < blocks;
+                        const unsigned char* src = nullptr;
+                        if (copies) {
+                            const int blk = (key + from) / kBlock + lane * per;
+                            const int index = P.page_shift_blocks >= 0 ? blk >> P.page_shift_blocks : blk / P.blocks_per_page;
+                            int page = __ldg(table + index);
+                            if (page < 0 || page >= P.n_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
+                            src = P.pages + page * P.page_bytes + ((long long)g * P.blocks_per_page + blk - index * P.blocks_per_page) * Layout<D>::kBytes;
+                        }
+                        if (lead) ok = mbar_wait_while(ok, &st.bar_stempty[st_slot], st_par);
+                        ok = __shfl_sync(kFull, ok, 0);
+                        if (!ok) break;                              // (the ring's position stays that of the last load)
+                        if (lead) mbar_arrive_expect_tx(&st.bar_stfull[st_slot], blocks * Layout<D>::kBytes);
+                        __syncwarp();
+                        if (copies)
+                            bulk_load(sS + st_slot * SM::kStageBytes + lane * per * Layout<D>::kBytes, src, min(per, blocks - lane * per) * Layout<D>::kBytes, &st.bar_stfull[st_slot]);
+                        if (++st_slot == RS) { st_slot = 0; st_par ^= 1; }
+                    }
+                    if (i == 0 && lead) {
+                        ok = mbar_wait_while(ok, &st.bar_qempty, (seg & 1) ^ 1);
+                        const int blocks = two ? 2 : 1, node0 = b * P.nodes + pp * P.n_blk * P.nodes_per_rb;
+                        if (ok) {
+                            st.q_last = seg & 1;
+                            mbar_arrive_expect_tx(&st.bar_qfull, blocks * P.rb_rows * D * 2);   // rows past rb_rows stay stale: never read back
+                            for (int q = 0; q < blocks; ++q)
+                                for (int h = 0; h < H; ++h)
+                                    tma_load_4d(sQ + q * SM::kQBlock + h * (128 * 128), &tmQ, &st.bar_qfull, h * 64, g * G, node0 + q * P.nodes_per_rb, 0);
+                        }
+                        // ... so the next segment's Q waits for it in L2
+                        if (cur.valid()) {
+                            const int next0 = cur.b * P.nodes + pp * P.n_blk * P.nodes_per_rb;
+                            for (int q = 0; q < (TWO && cur.two_rb(P) ? 2 : 1); ++q)
+                                for (int h = 0; h < H; ++h) tma_prefetch_4d(&tmQ, h * 64, cur.g * G, next0 + q * P.nodes_per_rb, 0);
+                        }
+                    }
+                    ok = __shfl_sync(kFull, ok, 0);
+                    if (!ok) break;
+                }
+            }
+            __syncwarp();
+            write_cut_unit(P, ci, cut);
+            if (lead) st.st_next = st_slot | st_par << 8;
+            __syncwarp();
+        } else if (warp == kMmaWarp) {
+            // =================================== MMA issuer ===================================
+            // The warp runs converged: every lane waits on the barriers and executes the same straight-line issue
+            // sequences with warp-uniform descriptor words, and the elected lane issues the instructions and the
+            // commits (predicated, no branch around them).  Whatever this warp executes between two MMAs costs
+            // tensor-pipe time, so no control flow depends on a wait's outcome: after a wait that ran out the
+            // predicate is off and the loops run dry.
+            constexpr uint32_t idesc_s128 = idesc_bf16_f32(128, kTileKeys, false, false);
+            constexpr uint32_t idesc_s64 = idesc_bf16_f32(128, kTreeKeys, false, false);
+            constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, false, true);
+            // high word of every shared-memory descriptor (stride between 8-row groups 1024 B, version, swizzle)
+            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            const uint32_t q_lo = ((smem_u32(sQ) & 0x3ffff) >> 4) | (1u << 16);
+            const uint32_t k_lo = ((smem_u32(sK) & 0x3ffff) >> 4) | (1u << 16);
+            const uint32_t v_lo = (smem_u32(sV) & 0x3ffff) >> 4;
+            const uint32_t elected = elect_one();
+            uint32_t k_next = 0, k_par = 0, v_next = 0, v_par = 0;   // ring slot to take next and its phase parity
+            uint32_t p_par[2] = {0, 0};              // phase parity of the next P tile per group
+            // The segment's shape comes from memory; passing it through a broadcast from lane 0 tells the
+            // compiler that it is the same in every lane, so that the loops below and the descriptor arithmetic in
+            // them stay on the uniform datapath (this warp's own instruction stream is what bounds the issue rate).
+            auto uni = [](int v) { return __shfl_sync(kFull, v, 0); };
+            Segment s;
+            for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+                const int seg_t0 = uni(s.t0), n = uni(s.n), M = uni(s.M), Pb = uni(s.Pb), last = uni(s.nt) - 1;
+                const bool two = TWO && uni(s.rows) > P.rb_rows;
+                ok = mbar_wait_while(ok, &st.bar_qfull, seg & 1);
+                uint32_t k_slot = 0, v_slot = 0;      // ring slots of the K and V tiles in use
+                bool acc[2] = {false, false};         // accumulator holds a product of this segment
+                auto take_v = [&]() {
+                    v_slot = v_next;
+                    ok = mbar_wait_while(ok, &st.bar_vfull[v_slot], v_par);
+                    if (++v_next == RV) { v_next = 0; v_par ^= 1; }
+                };
+                auto take_k = [&]() {
+                    k_slot = k_next;
+                    ok = mbar_wait_while(ok, &st.bar_kfull[k_slot], k_par);
+                    if (++k_next == RK) { k_next = 0; k_par ^= 1; }
+                };
+                // the accumulator's first product of the segment: the epilogue of the previous one has read it
+                auto take_o = [&](const int q) {
+                    if (!acc[q]) ok = mbar_wait_while(ok, &st.bar_ofree[q], (seg & 1) ^ 1);
+                };
+
+                // ---- O[q] (+)= P[q] V for tile i (q is a literal at every call site) ----
+                auto pv = [&](const int q, const int i, const bool fresh_v, const bool release_v) {
+                    const bool tree = seg_t0 + i == last;
+                    const int nk = tree ? kTreeKeys : kTileKeys;
+                    const int valid = tree ? M : min(kTileKeys, Pb - (seg_t0 + i) * kTileKeys);
+                    const int ksteps = (valid + 15) >> 4;
+                    if (fresh_v) {
+                        take_v();
+                        if (tree && valid < ksteps * 16) {
+                            // rows past the last live key meet P = 0; they must not hold NaN/Inf bit patterns
+                            unsigned char* vtile = sV + v_slot * SM::kTileBytes;
+                            const int nrows = ksteps * 16 - valid;
+#pragma unroll 1
+                            for (int e = lane; e < nrows * 8 * H; e += 32) {
+                                const int h = e / (nrows * 8), rem = e % (nrows * 8);
+                                const int r = valid + rem / 8, c = rem % 8;
+                                *reinterpret_cast<uint4*>(vtile + h * (nk * 128) + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                    }
+                    take_o(q);
+                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    p_par[q] ^= 1;
+                    tc_fence_after_sync();
+                    const uint32_t go = ok ? elected : 0u;
+                    // V is consumed N-major: 16 keys are 2048 B; 64-column blocks are nk * 128 B apart
+                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(nk * 128 >> 4) << 16);
+                    mma_ts_x4(go, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
+                    mma_ts_x4(go, ksteps - 4, tmem + 256 + q * 128, tmem + q * 128 + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
+                    acc[q] = true;
+                    if (release_v) mma_commit_if(go, &st.bar_vempty[v_slot]);
+                    if (two ? i == n - 1 : i + 2 >= n) mma_commit_if(go, &st.bar_odone[q]);
+                };
+                // ---- S[q] = Q K^T for tile si.  Nothing in tensor memory changes hands here: K arrives through the
+                // async proxy, and the buffer was last read by this thread's own P V, which runs first. ----
+                auto qk = [&](const int q, const int si, const bool fresh_k, const bool release_k) {
+                    if (fresh_k) take_k();
+                    const uint32_t go = ok ? elected : 0u;
+                    const bool tree = seg_t0 + si == last;
+                    const uint32_t a0 = q_lo + (two ? q : 0) * (SM::kQBlock >> 4);
+                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
+                    const uint32_t idesc = tree ? idesc_s64 : idesc_s128;
+                    mma_ss_x4(go, tmem + q * 128, a0, b0, kDescHi, idesc, false);
+                    if (D == 128)                     // second 64-column block of Q and K
+                        mma_ss_x4(go, tmem + q * 128, a0 + (128 * 128 >> 4), b0 + ((uint32_t)((tree ? kTreeKeys : kTileKeys) * 128) >> 4),
+                                  kDescHi, idesc, true);
+                    if (release_k) mma_commit_if(go, &st.bar_kempty[k_slot]);
+                    mma_commit_if(go, &st.bar_sfull[q]);
+                    // the last S of the segment: Q may be overwritten once it has run
+                    if (si == n - 1 && release_k) mma_commit_if(go, &st.bar_qempty);
+                };
+                // Schedule.  Two live row blocks: group s owns row block s; per tile PV0(i) S0(i+1) PV1(i) S1(i+1),
+                // both groups sharing K(i+1) and V(i).  One live row block: the groups take alternate tiles,
+                // PV(i) S(i+2) for group i & 1.  S of the first tile(s) comes from the iterations with i < 0.
+                // Steady state (all tiles involved are full prefix tiles): the same steps with nothing to decide,
+                // so that the issuing warp executes as few instructions per MMA as possible.  The waits for K and V, which are
+                // there most of the time, stand where the warp would wait for P.
+                auto full = [&](const int q, const uint32_t a0, const bool fresh, const bool release) {
+                    static_assert(kFirstKeys == 64 && kTileKeys == 128, "four steps before and behind the second wait");
+                    const uint32_t o_col = tmem + 256 + q * 128, p_col = tmem + q * 128;
+                    if (fresh) take_v();
+                    take_o(q);
+                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(kTileKeys * 128 >> 4) << 16);
+                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
+                    tc_fence_after_sync();
+                    mma_ts_x4(ok ? elected : 0u, o_col, p_col, b_lo, kDescHi, idesc_pv, acc[q]);
+                    if (fresh) take_k();
+                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
+                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    p_par[q] ^= 1;
+                    acc[q] = true;
+                    tc_fence_after_sync();
+                    const uint32_t go = ok ? elected : 0u;
+                    mma_ts_x4(go, o_col, p_col + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
+                    if (release) mma_commit_if(go, &st.bar_vempty[v_slot]);
+                    mma_ss_x4(go, p_col, a0, b0, kDescHi, idesc_s128, false);
+                    if (D == 128) mma_ss_x4(go, p_col, a0 + (128 * 128 >> 4), b0 + (kTileKeys * 128 >> 4), kDescHi, idesc_s128, true);
+                    mma_commit_if(go, &st.bar_sfull[q]);
+                    if (release) mma_commit_if(go, &st.bar_kempty[k_slot]);
+                };
+                const uint32_t a_q0 = q_lo, a_q1 = q_lo + (SM::kQBlock >> 4);
+                const int n_full = min(n, Pb / kTileKeys - seg_t0);   // tiles [0, n_full) of the segment are full prefix tiles
+                if (two) {
+#pragma unroll 1
+                    for (int i = -1; i < n; ++i) {
+                        if (i >= 0 && i + 2 < n_full) {           // tiles i and i+1 full, and S(i+1) is not the segment's last
+                            full(0, a_q0, true, false);
+                            full(1, a_q1, false, true);
+                        } else {
+                            if (i >= 0) pv(0, i, true, false);
+                            if (i + 1 < n) qk(0, i + 1, true, false);
+                            if (i >= 0) pv(1, i, false, true);
+                            if (i + 1 < n) qk(1, i + 1, false, true);
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = -2; i < n; i += 2) {
+                        if (i >= 0 && i + 4 < n_full) {           // tiles i to i+3 full, S(i+3) not the last
+                            full(0, a_q0, true, true);
+                            full(1, a_q0, true, true);
+                        } else {
+                            if (i >= 0) pv(0, i, true, true);
+                            if (i + 2 < n) qk(0, i + 2, true, true);
+                            if (i >= 0 && i + 1 < n) pv(1, i + 1, true, true);
+                            if (i + 3 < n) qk(1, i + 3, true, true);
+                        }
+                    }
+                }
+            }
+            // no product may read shared memory or write tensor memory that the CTA has given back
+            mma_commit_if(elected, &st.bar_idle);
+            ok &= mbar_drain(&st.bar_idle, 0);
+            __syncwarp();
+        }
+    }
+
+    // ---- teardown ----
+    if (!ok) st.abort = 1;
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        if (lane == 0 && st.abort) {
+            // No load may land in shared memory that the CTA has left.  (Without an abort the roles have waited for every
+            // one.)
+            const uint32_t n = st.st_next;
+            mbar_drain(&st.bar_qfull, st.q_last);
+            for (int i = 0; i < RS; ++i) mbar_drain(&st.bar_stfull[i], last_armed_parity(i, n & 255, n >> 8));
+            if (st.k_tree & 1) mbar_drain(&st.bar_kfull[st.k_tree >> 8 & 255], st.k_tree >> 16);
+            if (st.v_tree & 1) mbar_drain(&st.bar_vfull[st.v_tree >> 8 & 255], st.v_tree >> 16);
+            set_status(P.status, RADAR_ERR_TIMEOUT);
+        }
+        __syncwarp();
+        tmem_dealloc(st.tmem_base, 512);
+    }
+}
+
+
+template <int D, bool TWO>
+int launch_tc(radar_ctx* ctx, const radar_cache_attn_args& c, TcParams& P, cudaStream_t stream) {
+    using SM = Smem<D, TWO>;
+    CUtensorMap tmQ, tmKt, tmVt;
+    const long long tree_rows = (long long)c.B * c.rows;
+    if (!make_map(&tmQ, c.Q, D, c.Hq, tree_rows, P.G, P.nodes_per_rb, 1, 0, c.q_row_stride) ||
+        !make_map(&tmKt, c.Kt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride) ||
+        !make_map(&tmVt, c.Vt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride))
+        return RADAR_ERR_CUDA;
+    auto* const kernel = cache_attn_tc_kernel<D, TWO>;
+    RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_ATTN_TC + 2 * (D == 128) + TWO, kernel, (size_t)SM::kDynamic));
+    {
+        radar_launch_scope scope(ctx, RADAR_K_CACHE_ATTN, stream);
+        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)(P.n_cls * P.ncc)), dim3(kTcThreads), (size_t)SM::kDynamic, stream, tmQ, tmKt, tmVt, P));
+    }
+    {
+        radar_launch_scope scope(ctx, RADAR_K_CACHE_COMBINE, stream);
+        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, false, kFourBit>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
+    }
+    RADAR_CUDA_CHECK(cudaGetLastError());
+    return RADAR_OK;
+}
+
+size_t tc_partial_bytes(size_t grid, int d) {
+    const size_t rec = grid * 2 * kPairRows;
+    return align_up(rec * sizeof(float2), 256) + align_up(rec * d * sizeof(float), 256) + align_up(grid * sizeof(CutUnit), 256);
+}
+
+}  // namespace
+
+size_t cache_attn_tc_workspace_bytes(const radar_ctx* ctx, int d) { return tc_partial_bytes((size_t)ctx->sm_count, d); }
+
+int cache_attn_tc_launch(radar_ctx* ctx, const radar_cache_attn_args* c, cudaStream_t stream) {
+    if (!encode_fn()) return RADAR_ERR_CUDA;
+    TcParams P = {};
+    radar_attn_args& a = P.a;
+    a.B = c->B; a.Hq = c->Hq; a.Hkv = c->Hkv; a.d = c->d;
+    a.n_nodes = c->n_nodes; a.mask = c->mask; a.O = c->O; a.lse = c->lse;
+    a.prefix_len = c->cache_len; a.max_prefix_len = c->max_cache_len;
+    a.block_table = c->block_table; a.max_pages = c->max_pages; a.page_size = c->page_size;
+    P.G = c->Hq / c->Hkv;
+    P.g_magic = (65536u + P.G - 1) / P.G;
+    P.nodes_per_rb = 128 / P.G;
+    P.rb_rows = P.nodes_per_rb * P.G;
+    P.scale_log2 = (c->scale > 0.f ? c->scale : 1.f / sqrtf((float)c->d)) * 1.4426950408889634f;
+    P.status = ctx->d_status;
+    P.n_layers = 1;
+    P.nodes = c->rows;
+    P.pages = reinterpret_cast<const unsigned char*>(c->pages);
+    P.n_pages = c->n_pages;
+    P.page_bytes = page_bytes(c->Hkv, c->d, c->page_size);
+    P.blocks_per_page = c->page_size / kBlock;
+    P.page_shift_blocks = -1;
+    for (int s = 0; s < 28; ++s)
+        if (P.blocks_per_page == 1 << s) P.page_shift_blocks = s;
+    bool whole;
+    plan_grid(ctx, c->B, c->Hq, c->Hkv, c->max_cache_len, 1, &P.n_blk, &P.n_cls, &P.ncc, &whole, c->rows);
+    P.pair_rows = P.n_blk * P.rb_rows;
+    const TileCosts tc = tile_costs(P.n_cls);
+    P.cost_one = tc.one; P.cost_two = tc.two; P.unit_cost = whole ? 0 : tc.unit;
+    const size_t grid = (size_t)P.n_cls * P.ncc;
+    if (tc_partial_bytes(grid, c->d) > c->workspace_bytes) return RADAR_ERR_WORKSPACE;
+    const size_t rec = grid * 2 * kPairRows;
+    P.part_ml = reinterpret_cast<float2*>(c->workspace);
+    P.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(c->workspace) + align_up(rec * sizeof(float2), 256));
+    P.cut = reinterpret_cast<CutUnit*>(reinterpret_cast<char*>(P.part_o) + align_up(rec * c->d * sizeof(float), 256));
+    const bool two = P.n_blk > 1 && P.nodes_per_rb < c->rows;         // some unit can have two live row blocks
+    if (c->d == 128) return two ? launch_tc<128, true>(ctx, *c, P, stream) : launch_tc<128, false>(ctx, *c, P, stream);
+    return two ? launch_tc<64, true>(ctx, *c, P, stream) : launch_tc<64, false>(ctx, *c, P, stream);
+}
+
+}  // namespace radar

@@ -32,14 +32,11 @@
 // cache all along, and 8.5 thousand cycles lay between a segment's last product and the next one's first.
 // Every mbarrier wait is bounded; a wait that runs out sets RADAR_ERR_TIMEOUT on the device status
 // word, the CTA drains, frees its tensor memory and returns.
-#include <cuda.h>
-
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
-#include "common.cuh"
-#include "tc05.cuh"
+#include "tree_tiles.cuh"
 
 namespace radar {
 namespace {
@@ -52,276 +49,7 @@ constexpr int kEpilogueWarp = 8, kProducerWarp = 12, kMmaWarp = 13;
 constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
 static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
 constexpr int kStaticSmem = 3072;    // barriers and exchange arrays: with the tiles exactly the 227 KB a block may have
-constexpr int kTileKeys = 128;       // keys per prefix tile
-constexpr int kFirstKeys = 64;       // keys of a tile whose products start before the rest of its probabilities is there
-constexpr int kTreeKeys = 64;        // keys of the tree tile (RADAR_MAX_NODES)
-constexpr int kPairRows = 256;       // query rows of a row-block pair (and the stride of partial records)
 constexpr long long kLatencyWork = 9 << 15;   // sequences x query heads x keys x head dimension: tree_attn_tc_supported
-constexpr float kRescaleThreshold = 8.f;   // in log2 units: P stays below 2^8
-
-// Written by every CTA of the attention kernel, read by the combine kernel: the pieces are worked out by the producer warp
-// behind its last load, where nothing waits for it, and not by every warp of the combine (two 64-bit divisions a piece).
-constexpr int kMaxPerClass = 160;    // CTAs of a class at most (plan_grid)
-struct __align__(16) CutUnit {
-    int valid;           // 1: this CTA's last segment starts a unit that continues in the following CTAs
-    int b, g, layer;     // the unit
-    int slot;            // partial slot of that first piece in this CTA (0 or 1)
-    int rows;            // live query rows of the unit
-    int n_pieces;        // CTAs of the class from this one on whose range begins before the unit's end
-    uint32_t live[kMaxPerClass / 32];    // bit j: piece j's range holds the start of a tile of the unit
-};
-
-// ... and what its table of pieces follows from.
-struct Cut {
-    CutUnit unit;
-    long long u0, tot;   // start of the unit, size of the class's space (all layers)
-    int nt, w;           // tiles of the unit and their cost
-};
-
-struct TcParams {
-    radar_attn_args a;
-    int G, nodes_per_rb; // a row block holds whole nodes: nodes_per_rb = 128 / G (rounded down) of them
-    int rb_rows;         // ... so rb_rows = nodes_per_rb * G of its 128 rows can be live (all of them if G divides 128)
-    uint32_t g_magic;    // ceil(2^16 / G): row / G == row * g_magic >> 16 for row < 128 and G <= 128
-    int n_blk;           // row blocks of a class's units: 2 (they share each K/V tile) or 1
-    int pair_rows;       // query rows of a class's units: n_blk * rb_rows
-    int n_layers;        // layers run by this launch (the same tree, masks and prefix lengths for all)
-    long long o_ls, lse_ls;   // elements between consecutive layers of O and of lse
-    int n_cls;           // classes = units per KV head
-    int ncc;             // CTAs per class; grid = n_cls * ncc
-    int cost_one, cost_two, unit_cost;   // tile_costs(n_cls)
-    float scale_log2;
-    float scale_log2_lo; // two parts of P: what scale_log2 is below the scale itself (positive)
-    long long cache_rows;
-    float2* part_ml;     // [grid][2][256]     (m in natural-log units, with two parts of P in log2 units; l)
-    float* part_o;       // [grid][2][256][D]
-    CutUnit* cut;        // [grid]
-    int* status;
-};
-
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float y;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-    return y;
-}
-// one 32-byte store: a whole sector per lane (the epilogue's lanes write to different rows, so every store
-// instruction is split into one transaction per lane; with 16-byte stores each of them filled half a sector)
-__device__ __forceinline__ void st_global_32b(void* p, const uint32_t (&w)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// the same and the other steps of a probability, kept in the order in which they are written
-__device__ __forceinline__ float ex2_in_order(float x) {
-    float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float2 fma2_in_order(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm volatile("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-                 "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-                 : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 add2_in_order(float2 a, float2 b) {
-    float2 d;
-    asm volatile("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-                 : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ uint32_t bf16x2_in_order(float lo, float hi) {
-    uint32_t d;
-    asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// m ln 2 + ln l, m in log2 units
-__device__ __forceinline__ float lse_of(float m, float l) {
-    constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
-    return fmaf(m, kHi, fmaf(m, kLo, logf(l)));
-}
-
-// ---- the tile space of one class (unit index pp within a KV head) ---------------------------------
-// Positions are in cost units: a tile of a unit with two live row blocks (four MMAs) weighs cost_two, a tile of
-// a unit with one live row block cost_one, and every unit books cost_unit in front of its first tile for what it
-// costs beside its tiles (pipeline fill, epilogue), so that a CTA whose range holds several unit starts gets fewer
-// tiles; equal position ranges are then about equal amounts of time.  A tile belongs to the CTA whose range
-// contains the tile's start position.  The weights are measured, not derived (us a launch with its combine, against 3 : 5 without
-// the unit term): several classes per KV head, 3 : 5 + 15: 32 / 8 heads, B = 1, 2048 tokens 18.7 -> 17.1; 64 / 8 heads, B = 8, 2000
-// to 8192 tokens, trees of two calls 114 -> 111; one class, 2 : 4 + 12: 32 / 8 heads, B = 32, 4096 to 32768 tokens 780 -> 772.
-// It is the unit term that counts; 2 : 4 + 12 everywhere gives 17.3, 103 to 108 and 764, other sets lie within 2 %.
-struct TileCosts { int one, two, unit; };
-inline TileCosts tile_costs(int n_cls) { return n_cls == 1 ? TileCosts{2, 4, 12} : TileCosts{3, 5, 15}; }
-
-struct SeqInfo {
-    int M, Pb, nt;       // tree rows, prefix length, tiles of a unit (prefix tiles + the tree tile)
-    int rows;            // live query rows of this class's unit (0: it does not exist for this sequence)
-    int w;               // cost of one tile
-    long long kv0;
-};
-
-template <bool PAGED>
-__device__ __forceinline__ SeqInfo seq_info(const TcParams& P, int b, int pp) {
-    const radar_attn_args& a = P.a;
-    SeqInfo s;
-    s.M = min(max(a.n_nodes[b], 0), kMaxNodes);
-    s.Pb = a.prefix_len[b];
-    s.kv0 = PAGED ? 0 : a.kv_start[b];          // paged: the host has checked max_pages * page_size >= max_prefix_len
-    const bool ok = s.Pb >= 0 && s.Pb <= a.max_prefix_len && s.kv0 >= 0 && s.kv0 + s.Pb <= P.cache_rows;
-    s.rows = ok ? min(max(s.M * P.G - pp * P.pair_rows, 0), P.pair_rows) : 0;
-    s.nt = (max(s.Pb, 0) + kTileKeys - 1) / kTileKeys + 1;
-    s.w = s.rows > P.rb_rows ? P.cost_two : P.cost_one;
-    return s;
-}
-template <bool PAGED>
-__device__ __forceinline__ long long seq_cost(const TcParams& P, int b, int pp) {
-    const SeqInfo s = seq_info<PAGED>(P, b, pp);
-    return s.rows > 0 ? (long long)P.a.Hkv * (s.nt * s.w + P.unit_cost) : 0;
-}
-// number of tiles of a unit (start position U, nt tiles of cost w) that start before position x
-__device__ __forceinline__ int tiles_before(long long x, long long U, int nt, int w, int unit_cost) {
-    const long long d = x - U - unit_cost;           // clamped first, so that the division is a 32-bit one
-    if (d <= 0) return 0;
-    if (d >= (long long)nt * w) return nt;
-    return ((int)d + w - 1) / w;
-}
-
-// One CTA's walk over its range [.., hi) of the class's space: segments (sequence b, KV head g, tiles [t0, t1)).
-template <bool PAGED>
-struct Cursor {
-    int b, g, t0, t1;
-    int layer;           // layers follow one another in the space, each with the same sequence of units
-    long long U, hi;     // start position of the current unit, end of the CTA's range
-    int unit_cost;
-    SeqInfo s;
-    __device__ __forceinline__ bool valid() const { return t1 > t0; }
-    __device__ __forceinline__ void clip() { t1 = tiles_before(hi, U, s.nt, s.w, unit_cost); }
-    __device__ __forceinline__ void next_unit(const TcParams& P, int pp) {
-        U += (long long)s.nt * s.w + unit_cost;
-        t0 = 0;
-        if (++g == P.a.Hkv) {
-            g = 0;
-            do {
-                if (++b >= P.a.B) {                               // the next layer starts over at the first sequence
-                    if (++layer >= P.n_layers) { t1 = 0; return; }
-                    b = 0;
-                }
-                s = seq_info<PAGED>(P, b, pp);
-            } while (s.rows == 0);
-        }
-        clip();
-    }
-    __device__ __forceinline__ void next(const TcParams& P, int pp) {
-        if (t1 < s.nt) { t0 = t1; return; }                  // the range ended inside this unit
-        next_unit(P, pp);
-    }
-    __device__ __forceinline__ bool complete() const { return t0 == 0 && t1 == s.nt; }
-    __device__ __forceinline__ bool two_rb(const TcParams& P) const { return s.rows > P.rb_rows; }
-};
-
-// The first segment of CTA ci of a class, by a whole warp: the unit that contains the start of its range, from the unit's first
-// tile that starts at or after it.  tot_all: size of the class's space (all layers).
-template <bool PAGED>
-__device__ __forceinline__ Cursor<PAGED> first_segment(const TcParams& P, int pp, int ci, long long& tot_all) {
-    const radar_attn_args& a = P.a;
-    const int lane = threadIdx.x & 31;
-    long long tot = 0;
-#pragma unroll 1
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int b = b0 + lane;
-        if (pp == 0 && ci == 0 && b < a.B) {
-            const int Pb = a.prefix_len[b];
-            const long long kv0 = PAGED ? 0 : a.kv_start[b];
-            if (Pb < 0 || Pb > a.max_prefix_len || kv0 < 0 || kv0 + Pb > P.cache_rows) set_status(P.status, RADAR_ERR_INVALID_ARG);
-        }
-        tot += warp_sum(b < a.B ? seq_cost<PAGED>(P, b, pp) : 0ll);
-    }
-    // the space of all layers: layer l occupies [l * tot, (l + 1) * tot)
-    tot_all = tot * P.n_layers;
-    const long long lo_all = tot_all * ci / P.ncc;
-    Cursor<PAGED> cur;
-    cur.hi = tot_all * (ci + 1) / P.ncc;
-    cur.unit_cost = P.unit_cost;
-    cur.layer = tot > 0 ? (int)(lo_all / tot) : 0;
-    cur.t0 = cur.t1 = 0;
-    cur.b = -1;
-    cur.g = 0;
-    cur.U = 0;
-    const long long lo = lo_all - (long long)cur.layer * tot;
-    long long cum = 0;
-#pragma unroll 1
-    for (int b0 = 0; b0 < a.B && cur.b < 0; b0 += 32) {
-        const int b = b0 + lane;
-        const long long sz = b < a.B ? seq_cost<PAGED>(P, b, pp) : 0;
-        long long incl = sz;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(kFull, incl, o);
-            if (lane >= o) incl += v;
-        }
-        const unsigned hit = __ballot_sync(kFull, cum + incl > lo);
-        if (hit) {
-            const int src = __ffs(hit) - 1;
-            const long long before = cum + __shfl_sync(kFull, incl - sz, src);
-            cur.b = b0 + src;
-            cur.s = seq_info<PAGED>(P, cur.b, pp);
-            const long long unit = (long long)cur.s.nt * cur.s.w + P.unit_cost;
-            cur.g = (int)((lo - before) / unit);
-            cur.U = before + cur.g * unit + (long long)cur.layer * tot;
-        }
-        cum += __shfl_sync(kFull, incl, 31);
-    }
-    if (cur.b >= 0 && cur.layer < P.n_layers) {
-        cur.t0 = tiles_before(lo_all, cur.U, cur.s.nt, cur.s.w, P.unit_cost);
-        if (cur.t0 >= cur.s.nt) cur.next_unit(P, pp);       // every tile of that unit starts before the range
-        else cur.clip();
-    }
-    return cur;
-}
-
-// What a CTA leaves to the combine, by a whole warp that agrees on `cut`.
-__device__ __forceinline__ void write_cut_unit(const TcParams& P, int ci, const Cut& cut) {
-    const int lane = threadIdx.x & 31;
-    CutUnit* out = P.cut + blockIdx.x;
-    int n_pieces = 0;
-    if (cut.unit.valid) {
-        const long long u0 = cut.u0, tot = cut.tot;
-        const int nt = cut.nt, w = cut.w;
-        const long long u1 = u0 + (long long)nt * w + P.unit_cost;
-#pragma unroll 1
-        for (int k = 0; k < kMaxPerClass / 32; ++k) {
-            const int c = ci + k * 32 + lane;
-            const long long lo = tot * c / P.ncc, hi = tot * (c + 1) / P.ncc;
-            const bool piece = c < P.ncc && lo < u1;
-            const bool live = piece && tiles_before(hi, u0, nt, w, P.unit_cost) > tiles_before(lo, u0, nt, w, P.unit_cost);
-            const uint32_t pieces = __ballot_sync(kFull, piece), bits = __ballot_sync(kFull, live);
-            n_pieces += __popc(pieces);
-            if (lane == 0) out->live[k] = bits;
-            if (pieces != 0xffffffffu) break;
-        }
-    }
-    if (lane == 0) {
-        const CutUnit& u = cut.unit;
-        out->valid = u.valid; out->b = u.b; out->g = u.g; out->layer = u.layer;
-        out->slot = u.slot; out->rows = u.rows; out->n_pieces = n_pieces;
-    }
-}
-
-// What the other warps know of a segment.
-constexpr int kSegRing = 4;
-struct __align__(16) Segment {
-    int n;                               // tiles; 0: there is no further segment
-    int t0, nt, Pb, M, rows;             // first tile, tiles of the unit, prefix length, tree rows, live query rows
-    int b, g, layer;
-    int pad[3];
-};
 
 template <int D, bool TWO>
 struct Smem {
@@ -1700,187 +1428,6 @@ tree_attn_tc_fine_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     }
 }
 
-// Merges the pieces of the units that were cut across CTAs.  Blocks (c, *): CTA c of the attention kernel holds the first
-// piece of a cut unit (or the blocks exit); the following CTAs of the same class hold the rest, each as its first
-// segment.  A warp merges one query row, every piece of it in flight together: the work is a chain of three trips to L2,
-// and many warps hide it better than many rows a warp do (148 cut units of 256 rows: 17.1 us event-timed with one row a
-// warp, 18.4 with two, 20.6 with four; 72 cut units of 128 rows: 10.0, 10.8, 14.7).
-template <int D, bool FINE>
-__global__ void __launch_bounds__(256) tree_attn_tc_combine_kernel(const TcParams P) {
-    chain_wait();
-    auto weight = [](float d) { return FINE ? ex2(d) : __expf(d); };      // of two pieces' maxima that differ by d
-    const radar_attn_args& a = P.a;
-    const CutUnit& cu = P.cut[blockIdx.x];
-    const int valid = cu.valid, b = cu.b, g = cu.g, layer = cu.layer, slot = cu.slot, rows = cu.rows, n_pieces = cu.n_pieces;
-    const uint32_t live0 = cu.live[0];
-    if (!valid) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int r = blockIdx.y * 8 + warp;
-    if (r >= rows) return;                                   // rows of a unit are live from 0 up
-    constexpr int E = D / 32;                                // output elements per lane
-    // the row's record in piece j's partials (row blocks start 128 records apart, whatever part of them is live)
-    const int blk = r < P.rb_rows ? 0 : 1, in_blk = r - blk * P.rb_rows;
-    auto rec_of = [&](int j) {
-        const int64_t cta = (int64_t)blockIdx.x + (int64_t)j * P.n_cls;
-        return (cta * 2 + (j == 0 ? slot : 0)) * kPairRows + blk * 128 + in_blk;
-    };
-    auto store_row = [&](const float (&o)[E], float mx, float den) {
-        const float inv = 1.f / den;
-        const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
-        const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.O) + layer * P.o_ls + (((int64_t)b * kMaxNodes + node) * a.Hq + hq) * D + lane * E;
-        __nv_bfloat162 w[E / 2];
-#pragma unroll
-        for (int q = 0; q < E; q += 2) w[q / 2] = __floats2bfloat162_rn(o[q] * inv, o[q + 1] * inv);
-        if (E == 4) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(w);
-        else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(w);
-        if (a.lse != nullptr && lane == 0) a.lse[layer * P.lse_ls + ((int64_t)b * a.Hq + hq) * kMaxNodes + node] = FINE ? lse_of(mx, den) : mx + logf(den);
-    };
-    auto load_row = [&](const float* src, float (&v)[E]) {
-        if (E == 4) {
-            const float4 t = *reinterpret_cast<const float4*>(src);
-            v[0] = t.x; v[1] = t.y; v[E - 2] = t.z; v[E - 1] = t.w;
-        } else {
-            const float2 t = *reinterpret_cast<const float2*>(src);
-            v[0] = t.x; v[1] = t.y;
-        }
-    };
-
-    if (n_pieces <= 4) {
-        // ---- the usual case: a unit spread over a few CTAs.  (A CTA whose range holds no tile start has no piece.) ----
-        float2 ml[4];
-        float v[4][E], o[E];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool on = ((live0 >> j) & 1u) && j < n_pieces;
-            const int64_t rec = rec_of(on ? j : 0);
-            ml[j] = P.part_ml[rec];
-            load_row(P.part_o + rec * D + lane * E, v[j]);
-            if (!on) ml[j] = make_float2(-CUDART_INF_F, 0.f);
-        }
-        const float mx = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
-        float den = 0.f;
-#pragma unroll
-        for (int q = 0; q < E; ++q) o[q] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (ml[j].x == -CUDART_INF_F) continue;
-            const float w = weight(ml[j].x - mx);
-            den = fmaf(ml[j].y, w, den);
-#pragma unroll
-            for (int q = 0; q < E; ++q) o[q] = fmaf(v[j][q], w, o[q]);
-        }
-        store_row(o, mx, den);
-        return;
-    }
-
-    // ---- a unit spread over many CTAs (few units, long prefixes): lane j holds piece j's (m, l) ----
-    float den = 0.f, mx = -CUDART_INF_F, o[E];
-#pragma unroll
-    for (int q = 0; q < E; ++q) o[q] = 0.f;
-    for (int j0 = 0; j0 < n_pieces; j0 += 32) {
-        const int jl = j0 + lane;
-        const uint32_t live = cu.live[j0 >> 5];
-        float2 ml = make_float2(-CUDART_INF_F, 0.f);
-        if (jl < n_pieces && ((live >> lane) & 1u)) ml = P.part_ml[rec_of(jl)];
-        const float mnew = fmaxf(mx, warp_max(ml.x));
-        if (mnew == -CUDART_INF_F) continue;
-        const float rescale = weight(mx - mnew);             // 0 on the first live batch
-        den *= rescale;
-#pragma unroll
-        for (int q = 0; q < E; ++q) o[q] *= rescale;
-        mx = mnew;
-        const float wl = ml.x == -CUDART_INF_F ? 0.f : weight(ml.x - mx);
-        den += warp_sum(ml.y * wl);
-        const int nb = min(32, n_pieces - j0);
-        for (int u0 = 0; u0 < nb; u0 += 4) {
-            float v[4][E], w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                w[u] = u0 + u < nb ? __shfl_sync(kFull, wl, u0 + u) : 0.f;
-                if (w[u] != 0.f) {
-                    load_row(P.part_o + rec_of(j0 + u0 + u) * D + lane * E, v[u]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < E; ++q) v[u][q] = 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int q = 0; q < E; ++q) o[q] = fmaf(v[u][q], w[u], o[q]);
-        }
-    }
-    store_row(o, mx, den);
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = []() -> EncodeTiledFn {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess) return nullptr;
-        return q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
-    }();
-    return fn;
-}
-
-// [layers][rows][heads][d] bf16 tensor (layer_stride elements between layers), box = (64 elements, box_heads,
-// box_rows, one layer), 128-byte swizzle, zero fill
-bool make_map(CUtensorMap* tm, const void* base, int d, int heads, long long rows, int box_heads, int box_rows, int layers,
-              long long layer_stride) {
-    EncodeTiledFn enc = encode_fn();
-    if (!enc) return false;
-    if (layers <= 1) { layers = 1; layer_stride = rows * heads * d; }
-    cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)rows, (cuuint64_t)layers};
-    cuuint64_t strides[3] = {(cuuint64_t)d * 2, (cuuint64_t)d * 2 * heads, (cuuint64_t)layer_stride * 2};
-    cuuint32_t box[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows, 1};
-    cuuint32_t es[4] = {1, 1, 1, 1};
-    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Grid shape.  A class is one row-block pair (256 query rows: both row blocks share every K/V tile in
-// shared memory) or, when such fused units would leave most SMs without work, one row block (128 rows).
-// CTAs per class: the grid is one CTA per SM, but at least two tiles per CTA when every sequence has the longest prefix (four
-// instead of two, us: 32 / 8 heads, 1000 tokens 16.0 / 14.6; 4 / 4 heads, d = 64, 500 tokens 13.6 / 11.5; 16 / 16 heads, 1000 tokens
-// 14.5 / 13.6; but 32 / 8 heads, 2048 tokens 16.5 / 17.1).  Both decisions look at the tiles of the whole launch, all its
-// layers: 32 layers of one sequence with 2048 tokens (32 / 8 heads, d = 128) run as 148 CTAs of fused units, where one layer
-// alone would be split into half units on 128 CTAs.
-void plan_grid(const radar_ctx* ctx, int B, int Hq, int Hkv, int max_prefix_len, int layers, int* n_blk, int* n_cls, int* ncc,
-               bool* whole) {
-    const int G = Hq / Hkv;
-    const int blocks = (kMaxNodes + 128 / G - 1) / (128 / G);         // row blocks of a full tree
-    const long long unit_tiles = (long long)layers * B * Hkv * ((max_prefix_len + kTileKeys - 1) / kTileKeys + 1);
-    int nb = 2;
-    if (blocks > 1 && unit_tiles * ((blocks + 1) / 2) < 4LL * ctx->sm_count) nb = 1;
-    const int cls = (blocks + nb - 1) / nb;
-    long long per = std::min(ctx->sm_count / cls, kMaxPerClass);
-    const long long cap = (unit_tiles + 1) / 2;
-    if (per > cap) per = cap;
-    if (per < 1) per = 1;
-    // All units of one sequence are alike, so where they are no more than the CTAs of a class a grid can be chosen in
-    // which every CTA has one piece of one unit and pays for one segment (fill and epilogue, what tile_costs books per
-    // unit) and not for two.  Not where that leaves so many CTAs unused that the pieces get longer than what it saves.
-    // (Attention + combine, d = 128: 40 / 40 heads, 2048 tokens 22.9 -> 19.6 us; 16 / 16 heads, 1000 tokens 14.8 -> 13.6.)
-    const long long units = (long long)layers * Hkv, tiles = unit_tiles / (B * units);
-    *whole = false;
-    if (B == 1 && units <= per) {
-        const TileCosts tc = tile_costs(cls);
-        const int w = nb > 1 && blocks > 1 ? tc.two : tc.one;
-        const long long pieces = std::max(1ll, std::min(tiles / 2, per / units));
-        *whole = (tiles + pieces - 1) / pieces * w <= units * (tiles * w + tc.unit) / per + 2 * tc.unit / 3;
-        if (*whole) per = units * pieces;
-    }
-    *n_blk = nb;
-    *n_cls = cls;
-    *ncc = (int)per;
-}
-
 }  // namespace
 
 bool tree_attn_tc_supported(const radar_attn_args* a) {
@@ -1943,7 +1490,7 @@ static int launch_tc(radar_ctx* ctx, TcParams& P, cudaStream_t stream) {
     RADAR_CUDA_CHECK(cudaGetLastError());
     {
         radar_launch_scope scope(ctx, RADAR_K_ATTN_COMBINE, stream);
-        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, FINE>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
+        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, FINE, kPaged>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
     }
     RADAR_CUDA_CHECK(cudaGetLastError());
     return RADAR_OK;

@@ -37,6 +37,9 @@ def tree_masks(rng, B, rows):
     return mask
 
 
+held_to = []         # of each sequence of the last check_attention: (O in float64, what O may be off)
+
+
 def workspace(n):
     w = torch.zeros(n + 256, dtype=torch.uint8, device="cuda")
     return w[(-w.data_ptr()) % 256:][:n]
@@ -90,6 +93,7 @@ def check_attention(ctx, rng, lens, Hq, Hkv, d, page, rows, n_nodes=None, mask="
     o_gpu, lse_gpu = O.double().cpu().numpy(), lse.double().cpu().numpy()
     q64 = qkv.double().numpy()
     sc = scale if scale > 0 else d ** -0.5
+    held_to.clear()
     for b in range(B):
         m, n = int(M[b]), int(lens[b])
         K, V = rows_of(pool, table[b], n, page, Hkv, d)
@@ -102,7 +106,9 @@ def check_attention(ctx, rng, lens, Hq, Hkv, d, page, rows, n_nodes=None, mask="
         o, l = C.attention(q, k, v, see, sc)
         size, _ = C.attention(q, k, np.abs(v), see, sc)
         move = 2.0 ** -23 * d * sc * (np.abs(q).max() if q.size else 0) * (np.abs(k).max() if k.size else 0)
-        assert np.all(np.abs(o_gpu[b, :m] - o) <= (1.1 * 2.0 ** -7 + 2 * move) * size + len(v) * 2.0 ** -118 * np.abs(v).max(initial=0)), (b, np.max(np.abs(o_gpu[b, :m] - o) / (size + 1e-30)))
+        bound = (1.1 * 2.0 ** -7 + 2 * move) * size + len(v) * 2.0 ** -118 * np.abs(v).max(initial=0)
+        held_to.append((o, bound))
+        assert np.all(np.abs(o_gpu[b, :m] - o) <= bound), (b, np.max(np.abs(o_gpu[b, :m] - o) / (size + 1e-30)))
         assert np.all(o_gpu[b, m:] == 7.0)
         if want_lse:
             got, empty = lse_gpu[b, :, :m], np.isneginf(l)

@@ -308,18 +308,19 @@ def test_attention_reports_what_is_out_of_range(ctx):
     from paper_2512_14069_b200 import binding as rb
     for rows in (1, 64):
         kw = T.check_attention(ctx, np.random.default_rng(9), [300, 40], 8, 2, 64, 16, rows, n_nodes=[rows, rows])
-        good = kw["O"][1].clone()
+        o, bound = T.held_to[1]
+        good = lambda: bool(np.all(np.abs(kw["O"][1].double().cpu().numpy() - o) <= bound))       # (not bit for bit: without the first sequence the keys are shared out differently)
         for name, value in (("cache_len", [301, 40]), ("cache_len", [-1, 40]), ("n_nodes", [rows + 1, rows]), ("n_nodes", [-1, rows])):
             kw["O"].zero_()
             rb.radar_cache_attention(ctx, **dict(kw, **{name: T.dev(value, torch.int32)}))
             assert ctx.read_device_status() == -1, name
-            assert float(kw["O"][0].float().abs().max()) == 0.0 and torch.equal(kw["O"][1], good)
+            assert float(kw["O"][0].float().abs().max()) == 0.0 and good()
         for page in (-1, kw["pages"].shape[0]):
             table = kw["block_table"].clone()
             table[0, 3] = page
             rb.radar_cache_attention(ctx, **dict(kw, block_table=table))
             assert ctx.read_device_status() == -1
-            assert torch.equal(kw["O"][1], good)
+            assert good()
         with pytest.raises(rb.RadarError) as e:
             rb.radar_cache_attention(ctx, **dict(kw, max_cache_len=20000))
         assert e.value.status == -1                              # the table is too narrow
