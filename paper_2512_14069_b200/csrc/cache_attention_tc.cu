@@ -2,14 +2,20 @@
 //
 // The tile space, the softmax groups, the issuing warp and the epilogue are those of tree_attention_tc.cu: units of (sequence, KV head,
 // pair of row blocks of 128 query rows), their tiles of 128 keys laid end to end and cut into equal ranges, one thread a query
-// row.  What differs is where a tile comes from: the producer fetches blocks as they lie in the cache (bulk copies, 64 keys of a
-// head a stage, K and V together), and four warps decode them into the bf16 tiles that the products read, exactly (cache.cuh).
-// These warps also do the epilogue, which falls to them once a segment.
+// row.  What differs is where a tile comes from: the producer fetches a tile's keys, then its values, as they lie in the cache (by TMA:
+// a block's keys, or its values, are a row of bytes), and eight warps decode them into the bf16 tiles that the products read,
+// exactly (cache.cuh).
 //   warps 0-3 / 4-7  softmax groups 0 / 1
-//   warps 8-11       decoders: a block of 16 keys of every stage each; tree rows by TMA; epilogue
-//   warp 12          producer: segments, stages, Q
-//   warp 13          issues the products
-// K and V have two tiles each (three are worth no more, and the stages need the room).
+//   warps 8-11       decoders of values, two blocks of a tile each; the tree's V by TMA; epilogue
+//   warps 12-15      decoders of keys, the same; the tree's K by TMA
+//   warp 16          producer: segments, stages, Q
+//   warp 17          issues the products
+// What bounds the kernel is the issue of instructions: decoding takes twelve for eight values, a tile some 2300 by all warps, as many as
+// its softmax for one row block, and a warp issues one about every five cycles here.  So what surrounds the decoding is kept to a
+// few waits a tile, and everything in the steady state is a small loop (with the softmax of tree_attention_tc.cu beside it, 128 scores
+// in line, instructions were fetched anew all along): scores are read from tensor memory twice, 32 at a time, and keys and
+// values are decoded by the same code.  That also makes room for eight decoders at 96 registers a thread.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -21,14 +27,11 @@ namespace {
 
 using namespace cache4;
 
-constexpr int kTcThreads = 512;
-constexpr int kEpilogueWarp = 8, kDecodeWarps = 4, kProducerWarp = 12, kMmaWarp = 13;
-// Registers a thread: 128 at launch, then shared out by warpgroup (two of softmax; what they take the other two give).
-constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
-static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
+constexpr int kTcThreads = 576;      // 18 warps are allocated as 20: 96 registers a thread
+constexpr int kEpilogueWarp = 8, kKeyWarp = 12, kProducerWarp = 16, kMmaWarp = 17, kDecoders = 4;    // decoders of either kind
 constexpr int kStaticSmem = 3072;
-constexpr int kStageKeys = 64;       // keys of a stage: a block for each decoder
-static_assert(kStageKeys == kDecodeWarps * kBlock && 2 * kStageKeys == kTileKeys, "two stages a tile, a block a warp");
+constexpr int kTileBlocks = kTileKeys / kBlock;
+static_assert(kTileBlocks == 2 * kDecoders, "two blocks of a tile a decoder");
 
 template <int D, bool TWO>
 struct Smem {
@@ -36,62 +39,71 @@ struct Smem {
     static constexpr int kQBlock = 128 * D * 2;
     static constexpr int kQBytes = (TWO ? 2 : 1) * kQBlock;
     static constexpr int kTileBytes = kTileKeys * D * 2;
-    static constexpr int kStageBytes = kStageKeys / kBlock * Layout<D>::kBytes;
+    static constexpr int kPartBytes = Layout<D>::kBytes / 2;             // a block's keys, or its values
+    // A copy's target is on a 128-byte boundary: where every part is a copy of its own (pages of one block) they lie this far apart.
+    static constexpr int kSinglePitch = (kPartBytes + 127) / 128 * 128;
+    static_assert(2 * kPartBytes % 128 == 0, "two parts end on a boundary");
+    static constexpr int kStageBytes = kTileBlocks * kSinglePitch;      // a tile's keys, or its values
     static constexpr int kRingK = 2, kRingV = 2;
-    static constexpr int kRoom = 227 * 1024 - kStaticSmem - kQBytes - (kRingK + kRingV) * kTileBytes;
-    static constexpr int kRingS = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
-    static_assert(kRingS >= 2, "both halves of a tile are in the ring together");
-    static constexpr int kDynamic = kQBytes + (kRingK + kRingV) * kTileBytes + kRingS * kStageBytes;
+    static constexpr int kRoom = (227 * 1024 - kStaticSmem - kQBytes - (kRingK + kRingV) * kTileBytes) / kStageBytes;
+    static constexpr int kStages = kRoom < 8 ? kRoom : 8;
+    static_assert(kStages >= 3, "keys and values of a tile, and a stage to go on with");
+    static constexpr int kDynamic = kQBytes + (kRingK + kRingV) * kTileBytes + kStages * kStageBytes;
 };
 
-// 32 channels of a row, two groups: four chunks of 16 bytes of the swizzled row, from chunk `chunk` on.
-__device__ __forceinline__ void store_channels(const uint4 w, uint32_t byte0, uint32_t byte1, unsigned char* row, int chunk, int key7) {
-    const uint32_t s0 = scale_pair(byte0), s1 = scale_pair(byte1), f0 = offset_pair(s0), f1 = offset_pair(s1);
-    auto put = [&](int c, uint32_t x, uint32_t s, uint32_t f) {
-        *reinterpret_cast<uint4*>(row + (((chunk + c) ^ key7) << 4)) = make_uint4(decode<0>(x, s, f), decode<1>(x, s, f), decode<2>(x, s, f), decode<3>(x, s, f));
-    };
-    put(0, w.x, s0, f0);
-    put(1, w.y, s0, f0);
-    put(2, w.z, s1, f1);
-    put(3, w.w, s1, f1);
-}
+// Place in a ring and the phase to wait for.
+template <int N>
+struct Ring {
+    uint32_t slot = 0, par;
+    __device__ __forceinline__ explicit Ring(uint32_t p) : par(p) {}
+    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; par ^= 1; } }
+    __device__ __forceinline__ void next_but_one() { slot += 2; if (slot >= N) { slot -= N; par ^= 1; } }
+};
 
-// One block's keys into rows key0 .. key0 + 15 of a K-major tile with the 128-byte swizzle.  A lane takes 32 channels of a row.
+// A decoder's lane takes 32 channels of a row of a block's keys or values (at D = 128 of rows `row` and row + 8), which it stores as
+// four chunks of the 128-byte swizzle.  The lanes are dealt out over rows and channels so that the eight lanes of a phase of a
+// 16-byte store write to eight different chunks.
+struct Share {
+    int codes, scale0, scale1;       // offsets in the block's part: codes, the words with the scales of the two groups
+    int pick0, pick1;                // selectors of their bytes (two further on for the second row)
+    uint32_t to[4];                  // offsets of the chunks in the tile, from the row of the block's first key
+};
 template <int D>
-__device__ __forceinline__ void decode_keys(const unsigned char* block, unsigned char* tile, int key0) {
-    const int lane = threadIdx.x & 31;
-    constexpr int kPasses = D / 64, kRows = 16 / kPasses;
-    const int q = D == 128 ? (lane & 1) | (lane >> 4) << 1 : lane & 1, r0 = (lane >> 1) & (kRows - 1);
-#pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
-        const int r = r0 + pass * kRows;
-        const uint4 w = *reinterpret_cast<const uint4*>(block + r * Layout<D>::kRow + q * 16);
-        uint32_t b0, b1;
-        if (D == 128) {
-            const uint32_t sc = *reinterpret_cast<const uint16_t*>(block + Layout<D>::kKScales + (r & 7) * 16 + q * 4 + (r >> 3) * 2);
-            b0 = __byte_perm(sc, 0, 0x4040);
-            b1 = __byte_perm(sc, 0, 0x4141);
-        } else {
-            const unsigned char* sc = block + Layout<D>::kKScales + (r & 7) * 8 + q * 4 + (r >> 3);
-            b0 = sc[0] * 0x10001u;
-            b1 = sc[2] * 0x10001u;
-        }
-        store_channels(w, b0, b1, tile + (q >> 1) * (kTileKeys * 128) + (key0 + r) * 128, (q & 1) * 4, r & 7);
-    }
+__device__ __forceinline__ Share share_of(const bool values) {
+    const int lane = threadIdx.x & 31, q = D == 128 ? (lane & 1) | (lane >> 4) << 1 : lane & 1;      // channels 32q ..
+    // keys lie row by row; a value's place p is where its row stands
+    const int p = values ? ((lane >> 1) & 1) | ((lane >> 2) & 1) << 2 | ((lane >> 3) & 1) << 1 | (D == 64 ? (lane >> 4) << 3 : 0) : (D == 128 ? (lane >> 1) & 7 : lane >> 1);
+    const int row = values ? (p & 3) << 1 | ((p >> 2) & 1) | (p & 8) : p;
+    Share s;
+    s.codes = p * Layout<D>::kRow + ((q * 16) ^ (values && D == 128 && (p & 2) ? 32 : 0));
+    s.scale0 = Layout<D>::kKScales + (values ? q * 32 + (p & 3) * 4 : (row & 7) * (D / 8) + q * 4);
+    s.scale1 = s.scale0 + (values ? 16 : 0);
+    s.pick0 = 0x4040 + 0x101 * (values ? p >> 2 : row >> 3);
+    s.pick1 = 0x4040 + 0x101 * (values ? p >> 2 : D == 128 ? 1 : 2 + (row >> 3));
+    for (int c = 0; c < 4; ++c) s.to[c] = (q >> 1) * (kTileKeys * 128) + row * 128 + ((((q & 1) * 4 + c) ^ (row & 7)) << 4);
+    return s;
 }
-// ... and its values, whose rows stand in the order of their places.
+// A block's keys or values into the tile whose row of the block's first key is at `tile_at_key0`.
 template <int D>
-__device__ __forceinline__ void decode_values(const unsigned char* block, unsigned char* tile, int key0) {
-    const int lane = threadIdx.x & 31;
-    constexpr int kPasses = D / 64;
-    const int q = D == 128 ? (lane & 1) | (lane >> 4) << 1 : lane & 1;
-    const int p0 = ((lane >> 1) & 1) | ((lane >> 2) & 1) << 2 | ((lane >> 3) & 1) << 1 | (D == 64 ? (lane >> 4) << 3 : 0);
+__device__ __forceinline__ void decode_part(const unsigned char* part, uint32_t tile_at_key0, const Share& sh) {
+    constexpr int kRows = D / 64;
+    uint4 w[kRows];
 #pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
-        const int p = p0 + pass * 8, r = (p & 3) << 1 | ((p >> 2) & 1) | (p & 8);
-        const uint4 w = *reinterpret_cast<const uint4*>(block + Layout<D>::kVCodes + p * Layout<D>::kRow + ((q * 16) ^ (D == 128 && (p & 2) ? 32 : 0)));
-        const unsigned char* sc = block + Layout<D>::kVScales + q * 32 + (p & 3) * 4 + (p >> 2);
-        store_channels(w, sc[0] * 0x10001u, sc[16] * 0x10001u, tile + (q >> 1) * (kTileKeys * 128) + (key0 + r) * 128, (q & 1) * 4, r & 7);
+    for (int i = 0; i < kRows; ++i) w[i] = *reinterpret_cast<const uint4*>(part + sh.codes + 8 * i * Layout<D>::kRow);
+    uint32_t sc0 = *reinterpret_cast<const uint32_t*>(part + sh.scale0), sc1 = *reinterpret_cast<const uint32_t*>(part + sh.scale1);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const uint32_t s0 = scale_pair(__byte_perm(sc0, 0, sh.pick0)), s1 = scale_pair(__byte_perm(sc1, 0, sh.pick1)), f0 = offset_pair(s0), f1 = offset_pair(s1);
+        auto put = [&](const uint32_t at, uint32_t x, uint32_t s, uint32_t f) {
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + i * 8 * 128), "r"(decode<0>(x, s, f)), "r"(decode<1>(x, s, f)), "r"(decode<2>(x, s, f)),
+                         "r"(decode<3>(x, s, f)) : "memory");
+        };
+        put(tile_at_key0 + sh.to[0], w[i].x, s0, f0);
+        put(tile_at_key0 + sh.to[1], w[i].y, s0, f0);
+        put(tile_at_key0 + sh.to[2], w[i].z, s1, f1);
+        put(tile_at_key0 + sh.to[3], w[i].w, s1, f1);
+        sc0 >>= 16;
+        sc1 >>= 16;
     }
 }
 
@@ -99,12 +111,12 @@ __device__ __forceinline__ void decode_values(const unsigned char* block, unsign
 template <int D, bool TWO>
 __global__ void __launch_bounds__(kTcThreads, 1)
 cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKt,
-                     const __grid_constant__ CUtensorMap tmVt, const TcParams P) {
+                     const __grid_constant__ CUtensorMap tmVt, const __grid_constant__ CUtensorMap tmCache, const TcParams P) {
     chain_trigger();                     // every warp waits for the predecessor where its role begins; the barrier,
                                          // tensor-memory and descriptor set-up needs nothing from global memory
     using SM = Smem<D, TWO>;
     constexpr int H = SM::kHalves;
-    constexpr int RK = SM::kRingK, RV = SM::kRingV, RS = SM::kRingS;
+    constexpr int RK = SM::kRingK, RV = SM::kRingV, RS = SM::kStages;
     const radar_attn_args& a = P.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int pp = blockIdx.x % P.n_cls;                    // class
@@ -115,7 +127,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     // swizzled tiles need a 1024-byte boundary and there is no room left for alignment slack.
     struct __align__(1024) Static {
         uint64_t bar_qfull, bar_qempty, bar_kfull[RK], bar_kempty[RK], bar_vfull[RV], bar_vempty[RV];
-        uint64_t bar_stfull[RS], bar_stempty[RS];      // the cache's bytes as they lie there, 64 keys a stage
+        uint64_t bar_stfull[RS], bar_stempty[RS];      // stages: the cache's bytes as they lie there, keys and values in turn
         uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2];
         uint64_t bar_idle;               // every product issued has run
         uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
@@ -124,7 +136,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
         Segment seg[kSegRing];
         float2 ml[2][128];               // per group: (m in log2 units, l) of the rows at the end of a segment
-        uint32_t q_last, st_next, k_tree, v_tree;    // what is in flight at the end: phase parity of the last Q, ...
+        uint32_t q_last, st_next, k_tree, v_tree;   // phase parity of the last Q, slot and parity of the next stage, the last tree tiles
         uint32_t tmem_base;
         int abort;
     };
@@ -136,6 +148,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     unsigned char* sK = sQ + SM::kQBytes;
     unsigned char* sV = sK + RK * SM::kTileBytes;
     unsigned char* sS = sV + RV * SM::kTileBytes;
+    const int pitch = P.blocks_per_page == 1 ? SM::kSinglePitch : SM::kPartBytes;
 
     // ---- set-up ----
     if (warp == 0) {
@@ -143,9 +156,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             st.abort = 0;
             mbar_init(&st.bar_qfull, 1);
             mbar_init(&st.bar_qempty, 1);
-            for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], kDecodeWarps); mbar_init(&st.bar_kempty[i], 1); }
-            for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecodeWarps); mbar_init(&st.bar_vempty[i], 1); }
-            for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[i], 1); mbar_init(&st.bar_stempty[i], kDecodeWarps); }
+            for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], kDecoders); mbar_init(&st.bar_kempty[i], 1); }
+            for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecoders); mbar_init(&st.bar_vempty[i], 1); }
+            for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[i], 1); mbar_init(&st.bar_stempty[i], kDecoders); }
             for (int i = 0; i < 2; ++i) {
                 mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
                 mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
@@ -153,7 +166,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
             mbar_init(&st.bar_idle, 1);
             st.q_last = 1;
-            st.st_next = st.k_tree = st.v_tree = 0;
+            st.st_next = 1u << 8; st.k_tree = st.v_tree = 0;
             mbar_init(&st.bar_mlfull, 8);
             mbar_init(&st.bar_mlempty, 4);
             fence_barrier_init();
@@ -162,7 +175,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         tmem_alloc(&st.tmem_base, 512);
         tmem_relinquish();
         if (lane == 0) {
-            tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmKt); tma_prefetch_desc(&tmVt);
+            tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmCache); tma_prefetch_desc(&tmKt); tma_prefetch_desc(&tmVt);
         }
     }
     tc_fence_before_sync();
@@ -185,14 +198,23 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         return ok && s.n > 0;
     };
 
+    // The tree's own keys or values, by one lane of the decoders: `last` keeps slot and phase of what is in flight.
+    auto tree_tile = [&](unsigned char* to, const CUtensorMap* tm, uint64_t* full, const Segment& s, const bool issues, uint32_t& last, const uint32_t where) {
+        ok = __all_sync(kFull, ok);
+        if (lane != 0 || !ok) return;
+        if (issues) {
+            mbar_arrive_expect_tx(full, kTreeKeys * D * 2);
+            for (int h = 0; h < H; ++h) tma_load_4d(to + h * (kTreeKeys * 128), tm, full, h * 64, s.g, s.b * P.nodes, 0);
+            last = 1u << 16 | where;
+        } else {
+            mbar_arrive(full);
+        }
+    };
+
     if (warp < kEpilogueWarp) {
-        regs_inc<kSoftmaxRegs>();
         chain_sync();
         // =================================== softmax groups ===================================
-        // One thread per query row, which holds the tile's 128 scores in registers: tensor memory is read once and no two
-        // threads have to agree on a maximum.  (Two threads a row, 64 scores each read twice for want of registers, was the
-        // form before: 32 layers, 8 sequences of 6000 to 8192 tokens, 64 / 8 heads 4118 -> 3930 us; one layer of it within a
-        // step 307 -> 295; 32 layers of one sequence of 2048 tokens, 32 / 8 heads 105 -> 101.)
+        // One thread per query row.
         const int grp = warp >> 2;
         const int row = (warp & 3) * 32 + lane;                 // row of the block == tensor-memory lane
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
@@ -229,12 +251,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 ++sc;
                 tc_fence_after_sync();
                 if (ok && warp_live) {
-                    uint32_t sv[4][32];
+                    uint32_t va[32], vb[32];
                     const int valid = s.Pb - t * kTileKeys;
                     if (t == s.nt - 1 || valid < kTileKeys) {
                         // Keys that the row may not attend to (and, of the tree tile, which has 64, the columns that are stale)
-                        // become -inf in tensor memory, 32 at a time: one tile of a unit or two need it, and an unrolled path
-                        // for them would be fetched into the instruction cache anew each time.
+                        // become -inf in tensor memory.
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             uint32_t al;
@@ -245,28 +266,35 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                                 const int lim = valid - c * 32;
                                 al = lim >= 32 ? 0xffffffffu : (lim <= 0 ? 0u : ((1u << lim) - 1u));
                             }
-                            tmem_ld32(tS + c * 32, sv[0]);
+                            tmem_ld32(tS + c * 32, va);
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (!((al >> e) & 1u)) sv[0][e] = 0xff800000u;     // -inf
-                            tmem_st32(tS + c * 32, sv[0]);
+                                if (!((al >> e) & 1u)) va[e] = 0xff800000u;     // -inf
+                            tmem_st32(tS + c * 32, va);
                         }
                         tmem_wait_st();
                     }
+                    // ---- maximum: 32 scores at a time, the next 32 on their way ----
+                    float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+                    auto maxima = [&](const uint32_t (&v)[32]) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sv[c]);
-                    tmem_wait_ld();
-                    float mxa[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        mxa[c] = __uint_as_float(sv[c][0]);
-#pragma unroll
-                        for (int e = 1; e < 31; e += 2)                     // three-input maxima: half the instructions
-                            mxa[c] = max3(mxa[c], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
-                        mxa[c] = fmaxf(mxa[c], __uint_as_float(sv[c][31]));
+                        for (int e = 0; e < 32; e += 4) {                   // three-input maxima: half the instructions
+                            mx0 = max3(mx0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+                            mx1 = max3(mx1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+                        }
+                    };
+                    tmem_ld32(tS, va);
+#pragma unroll 1
+                    for (int c = 0; c < 4; c += 2) {
+                        tmem_wait_ld();
+                        tmem_ld32(tS + (c + 1) * 32, vb);
+                        maxima(va);
+                        tmem_wait_ld();
+                        if (c == 0) tmem_ld32(tS + 64, va);
+                        maxima(vb);
                     }
-                    const float mx = fmaxf(max3(mxa[0], mxa[1], mxa[2]), mxa[3]);
+                    const float mx = fmaxf(mx0, mx1);
                     // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
                     const float m_tile = mx * P.scale_log2;
                     float factor = 1.f;
@@ -288,37 +316,47 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             tmem_st16(tO + c, o);
                         }
                     }
+                    tmem_ld32(tS, va);           // (not ahead of the rescaling: nothing may look at these registers before the wait)
                     // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
                     // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
                     // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
                     // two of them.
                     float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
-                    uint32_t pk[16];
-                    auto scale = [&](const int p) {
-                        uint32_t &x = sv[p >> 4][2 * (p & 15)], &y = sv[p >> 4][2 * (p & 15) + 1];
-                        const float2 s2 = make_float2(__uint_as_float(x), __uint_as_float(y));
-                        const float2 t2 = fma2_in_order(s2, sc2, nm2);
-                        x = __float_as_uint(t2.x);
-                        y = __float_as_uint(t2.y);
-                    };
-                    auto finish = [&](const int p) {
-                        const float p0 = __uint_as_float(sv[p >> 4][2 * (p & 15)]), p1 = __uint_as_float(sv[p >> 4][2 * (p & 15) + 1]);
-                        ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
-                        pk[p & 15] = bf16x2_in_order(p0, p1);
-                        if ((p & 15) == 15) tmem_st16(tS + (p >> 4) * 16, pk);
-                    };
-                    // pairs that the scaling is ahead, that the rest is behind, and that the first stores are given to land in
-                    constexpr int kAhead = 2, kLag = 4, kLanding = 4;
+                    auto exponentials = [&](uint32_t (&v)[32], const uint32_t to) {
+                        uint32_t pk[16];
+                        auto scale = [&](const int p) {
+                            const float2 t2 = fma2_in_order(make_float2(__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])), sc2, nm2);
+                            v[2 * p] = __float_as_uint(t2.x);
+                            v[2 * p + 1] = __float_as_uint(t2.y);
+                        };
+                        auto finish = [&](const int p) {
+                            const float p0 = __uint_as_float(v[2 * p]), p1 = __uint_as_float(v[2 * p + 1]);
+                            ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
+                            pk[p] = bf16x2_in_order(p0, p1);
+                        };
+                        // pairs that the scaling is ahead, and that the rest is behind
+                        constexpr int kAhead = 2, kLag = 3;
 #pragma unroll
-                    for (int p = 0; p < kAhead; ++p) scale(p);
+                        for (int p = 0; p < kAhead; ++p) scale(p);
 #pragma unroll
-                    for (int p = 0; p < 64 + kLag; ++p) {
-                        if (p < 64) sv[p >> 4][2 * (p & 15)] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15)])));
-                        if (p + kAhead < 64) scale(p + kAhead);
-                        if (p < 64) sv[p >> 4][2 * (p & 15) + 1] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15) + 1])));
-                        if (p >= kLag) finish(p - kLag);
-                        if (p == kFirstKeys / 2 - 1 + kLag + kLanding) {
+                        for (int p = 0; p < 16 + kLag; ++p) {
+                            if (p < 16) v[2 * p] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p])));
+                            if (p + kAhead < 16) scale(p + kAhead);
+                            if (p < 16) v[2 * p + 1] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p + 1])));
+                            if (p >= kLag) finish(p - kLag);
+                        }
+                        tmem_st16(to, pk);
+                    };
+#pragma unroll 1
+                    for (int c = 0; c < 4; c += 2) {
+                        tmem_wait_ld();
+                        tmem_ld32(tS + (c + 1) * 32, vb);
+                        exponentials(va, tS + c * 16);
+                        tmem_wait_ld();
+                        if (c == 0) tmem_ld32(tS + 64, va);
+                        exponentials(vb, tS + c * 16 + 16);
+                        if (c == 0) {
                             tmem_wait_st();
                             tc_fence_before_sync();
                             __syncwarp();
@@ -343,12 +381,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if (lane == 0) mbar_arrive(&st.bar_mlfull);
         }
     } else if (warp < kProducerWarp) {
-        regs_dec<kEpilogueRegs>();
-        chain_sync();
+        chain_sync();                            // every global access of the CTA comes behind one
         // =================================== decoders, and epilogue ===================================
-        // A warp takes one block of 16 keys of every stage.  Its lanes are dealt out over rows and channels so that the eight
-        // lanes of a phase of a 16-byte store write to eight different chunks of the 128-byte swizzle.  The epilogue of a segment
-        // comes behind the first tile of the next one, when its last product is about done: the products have a tile to go on with.
+        // The epilogue of a segment, by the decoders of values, comes behind the first tile of the next one, when its last product is
+        // about done: the products have a tile to go on with.
         const int row = (warp - kEpilogueWarp) * 32 + lane;
         const uint32_t tO = tmem + 256 + ((uint32_t)((warp - kEpilogueWarp) * 32) << 16);
         const int rb_node = (int)(((uint32_t)row * P.g_magic) >> 16);        // row / G
@@ -448,74 +484,54 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 if (lane == 0) mbar_arrive(&st.bar_ofree[blk]);
             }
         };
-        uint32_t k_slot = 0, k_par = 1, v_slot = 0, v_par = 1, st_slot = 0, st_par = 0;
-        const int blk16 = warp - kEpilogueWarp;
-        auto next_stage = [&](uint32_t& slot, uint32_t& par) { if (++slot == RS) { slot = 0; par ^= 1; } };
-        // one tile: both halves of K, then both of V
-        auto decode_tile = [&](const Segment& s, const int t) {
-            const bool tree = t == s.nt - 1;
-            if (tree) {
-                for (int is_v = 0; is_v < 2; ++is_v) {
-                    uint32_t &slot = is_v ? v_slot : k_slot, &par = is_v ? v_par : k_par;
-                    ok = mbar_wait_while(ok, is_v ? &st.bar_vempty[slot] : &st.bar_kempty[slot], par);
-                    ok = __all_sync(kFull, ok);
-                    uint64_t* full = is_v ? &st.bar_vfull[slot] : &st.bar_kfull[slot];
-                    if (lane == 0) {
-                        if (blk16 == 0 && ok) {
-                            mbar_arrive_expect_tx(full, kTreeKeys * D * 2);
-                            for (int h = 0; h < H; ++h)
-                                tma_load_4d((is_v ? sV : sK) + slot * SM::kTileBytes + h * (kTreeKeys * 128), is_v ? &tmVt : &tmKt, full, h * 64, s.g, s.b * P.nodes, 0);
-                            (is_v ? st.v_tree : st.k_tree) = 1u | slot << 8 | (par ^ 1) << 16;
-                        } else if (ok) {
-                            mbar_arrive(full);
-                        }
-                    }
-                    if (++slot == (uint32_t)(is_v ? RV : RK)) { slot = 0; par ^= 1; }
-                }
-                return;
-            }
-            const int halves = min(2, (s.Pb - t * kTileKeys + kStageKeys - 1) / kStageKeys);
-            ok = mbar_wait_while(ok, &st.bar_kempty[k_slot], k_par);
-            uint32_t sl = st_slot, pr = st_par;
-            for (int half = 0; half < halves; ++half) {
-                ok = mbar_wait_while(ok, &st.bar_stfull[sl], pr);
-                decode_keys<D>(sS + sl * SM::kStageBytes + blk16 * Layout<D>::kBytes, sK + k_slot * SM::kTileBytes, half * kStageKeys + blk16 * 16);
-                next_stage(sl, pr);
-            }
-            fence_proxy_async_smem();
-            ok = __all_sync(kFull, ok);
-            if (lane == 0 && ok) mbar_arrive(&st.bar_kfull[k_slot]);
-            if (++k_slot == RK) { k_slot = 0; k_par ^= 1; }
-            ok = mbar_wait_while(ok, &st.bar_vempty[v_slot], v_par);
-            for (int half = 0; half < halves; ++half) {
-                decode_values<D>(sS + st_slot * SM::kStageBytes + blk16 * Layout<D>::kBytes, sV + v_slot * SM::kTileBytes, half * kStageKeys + blk16 * 16);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&st.bar_stempty[st_slot]);
-                next_stage(st_slot, st_par);
-            }
-            fence_proxy_async_smem();
-            ok = __all_sync(kFull, ok);
-            if (lane == 0 && ok) mbar_arrive(&st.bar_vfull[v_slot]);
-            if (++v_slot == RV) { v_slot = 0; v_par ^= 1; }
-        };
+        const bool values = warp < kKeyWarp;
+        const int mine = (warp - kEpilogueWarp) & (kDecoders - 1);
+        const Share share = share_of<D>(values);
+        uint64_t* const tiles_full = values ? st.bar_vfull : st.bar_kfull;
+        uint64_t* const tiles_empty = values ? st.bar_vempty : st.bar_kempty;
+        unsigned char* const tiles = values ? sV : sK;
+        static_assert(RK == RV, "one ring's length for both");
+        Ring<RV> out(1);
+        Ring<RS> in(0);
+        if (values) in.next();
         Segment s, done;
         done.n = 0;
         uint32_t seg = 0;
         for (; take_segment(seg, s); ++seg) {
-            decode_tile(s, s.t0);
-            if (seg > 0) epilogue(done, seg - 1);
 #pragma unroll 1
-            for (int i = 1; i < s.n; ++i) decode_tile(s, s.t0 + i);
-            done = s;
+            for (int i = 0; i < s.n; ++i) {
+                const int t = s.t0 + i;
+                ok = mbar_wait_while(ok, &tiles_empty[out.slot], out.par);
+                unsigned char* to = tiles + out.slot * SM::kTileBytes;
+                if (t == s.nt - 1) {
+                    tree_tile(to, values ? &tmVt : &tmKt, &tiles_full[out.slot], s, mine == 0, values ? st.v_tree : st.k_tree, out.slot | (out.par ^ 1) << 8);
+                } else {
+                    const int blocks = min((s.Pb - t * kTileKeys + kBlock - 1) / kBlock, kTileBlocks);
+                    ok = mbar_wait_while(ok, &st.bar_stfull[in.slot], in.par);
+                    const uint32_t at = smem_addr(to);
+                    const unsigned char* from = sS + in.slot * SM::kStageBytes;
+#pragma unroll 1
+                    for (int k = mine; k < blocks; k += kDecoders) decode_part<D>(from + k * pitch, at + k * (kBlock * 128), share);
+                    fence_proxy_async_smem();
+                    ok = __all_sync(kFull, ok);
+                    if (lane == 0) {
+                        mbar_arrive(&st.bar_stempty[in.slot]);
+                        if (ok) mbar_arrive(&tiles_full[out.slot]);
+                    }
+                    in.next_but_one();
+                }
+                out.next();
+                if (i == 0 && values && seg > 0) epilogue(done, seg - 1);
+            }
+            if (values) done = s;
         }
-        if (seg > 0) epilogue(done, seg - 1);
+        if (values && seg > 0) epilogue(done, seg - 1);
     } else {
-        regs_dec<kIssueRegs>();
-        chain_sync();                            // every global access of the CTA comes behind one
+        chain_sync();
         if (warp == kProducerWarp) {
             // =================================== TMA producer ===================================
-            // The whole warp walks the tiles: lane c fetches copy c of a stage (a page holds 64 keys of a head in one piece, or fewer),
-            // the leading lane does the waits, the byte counts and Q.
+            // The whole warp walks the tiles: lane c looks up and fetches piece c of a stage (the blocks of one page), the leading lane
+            // does the waits, the byte counts and Q.
             const bool lead = lane == 0;
             const bool usable = (smem_u32(smem_raw) & 1023u) == 0 && st.tmem_base == 0;     // (else the tiles would not sit on their swizzle boundary)
             if (!usable && lead) set_status(P.status, RADAR_ERR_CUDA);
@@ -525,8 +541,20 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             Cut cut;
             cut.unit.valid = 0;
             cut.tot = tot_all;
-            uint32_t st_slot = 0, st_par = 1;
-            const int per = min(P.blocks_per_page, kStageKeys / kBlock);          // blocks of a copy
+            Ring<RS> out(1);
+            const int per = min(P.blocks_per_page, kTileBlocks);         // blocks of a piece
+            // Where the pieces are: lane l looks up piece l of a window of 32, the window after next at a time (a lookup is a trip to L2,
+            // and one on the way of every stage was what bounded the kernel).
+            const int tile_pieces = kTileBlocks / per, window_tiles = 32 / tile_pieces;
+            auto look_up = [&](int b, int g, int key0, int key_end) {    // of the window that begins with key0
+                const int blk = key0 / kBlock + lane * per;
+                if (blk * kBlock >= key_end) return 0;
+                const int index = P.page_shift_blocks >= 0 ? blk >> P.page_shift_blocks : blk / P.blocks_per_page;
+                int page = __ldg(a.block_table + (long long)b * a.max_pages + index);
+                if (page < 0 || page >= P.n_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
+                return (page * a.Hkv + g) * P.blocks_per_page + blk - index * P.blocks_per_page;
+            };
+            int next_window = cur.valid() ? look_up(cur.b, cur.g, cur.t0 * kTileKeys, min(cur.t1 * kTileKeys, cur.s.Pb)) : 0;    // the next segment's first
             for (uint32_t seg = 0;; ++seg) {
                 const bool on = cur.valid();
                 const int b = cur.b, g = cur.g, n = cur.t1 - cur.t0, t0 = cur.t0, nt = cur.s.nt, Pb = cur.s.Pb;
@@ -538,37 +566,38 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     st.seg[seg % kSegRing] = s;
                     mbar_arrive(&st.bar_segfull[seg % kSegRing]);
                 }
+                ok = __shfl_sync(kFull, ok, 0);
                 if (!on) break;
                 if (t0 == 0 && n < nt) {                             // necessarily the last segment of this CTA
                     cut.unit.valid = 1; cut.unit.b = b; cut.unit.g = g; cut.unit.slot = seg == 0 ? 0 : 1; cut.unit.layer = 0; cut.unit.rows = cur.s.rows;
                     cut.nt = nt; cut.w = cur.s.w; cut.u0 = cur.U;
                 }
                 cur.next(P, pp);
-                const int32_t* table = a.block_table + (long long)b * a.max_pages;
+                const int key_end = min((t0 + n) * kTileKeys, Pb);
+                int window = next_window, window2 = look_up(b, g, (t0 + window_tiles) * kTileKeys, key_end);
+                if (cur.valid()) next_window = look_up(cur.b, cur.g, cur.t0 * kTileKeys, min(cur.t1 * kTileKeys, cur.s.Pb));
                 // The segment's first tile, then Q (its slot is free only behind the last S of the segment before), then the rest.
 #pragma unroll 1
-                for (int i = 0; i < n; ++i) {
+                for (int i = 0; i < n && ok; ++i) {
                     const int key = (t0 + i) * kTileKeys, left = t0 + i == nt - 1 ? 0 : min(kTileKeys, Pb - key);
-#pragma unroll 1
-                    for (int from = 0; from < left; from += kStageKeys) {
-                        const int blocks = min(kStageKeys / kBlock, (left - from + kBlock - 1) / kBlock);
-                        const bool copies = lane * per < blocks;
-                        const unsigned char* src = nullptr;
-                        if (copies) {
-                            const int blk = (key + from) / kBlock + lane * per;
-                            const int index = P.page_shift_blocks >= 0 ? blk >> P.page_shift_blocks : blk / P.blocks_per_page;
-                            int page = __ldg(table + index);
-                            if (page < 0 || page >= P.n_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
-                            src = P.pages + page * P.page_bytes + ((long long)g * P.blocks_per_page + blk - index * P.blocks_per_page) * Layout<D>::kBytes;
+                    if (left > 0) {
+                        const int in_window = i & (window_tiles - 1);
+                        if (in_window == 0 && i > 0) {
+                            window = window2;
+                            window2 = look_up(b, g, key + window_tiles * kTileKeys, key_end);
                         }
-                        if (lead) ok = mbar_wait_while(ok, &st.bar_stempty[st_slot], st_par);
-                        ok = __shfl_sync(kFull, ok, 0);
-                        if (!ok) break;                              // (the ring's position stays that of the last load)
-                        if (lead) mbar_arrive_expect_tx(&st.bar_stfull[st_slot], blocks * Layout<D>::kBytes);
-                        __syncwarp();
-                        if (copies)
-                            bulk_load(sS + st_slot * SM::kStageBytes + lane * per * Layout<D>::kBytes, src, min(per, blocks - lane * per) * Layout<D>::kBytes, &st.bar_stfull[st_slot]);
-                        if (++st_slot == RS) { st_slot = 0; st_par ^= 1; }
+                        const int at = __shfl_sync(kFull, window, (in_window * tile_pieces + lane) & 31);     // block of the pool
+                        const int pieces = per == kTileBlocks ? 1 : (left + per * kBlock - 1) / (per * kBlock);
+#pragma unroll 1
+                        for (int v = 0; v < 2; ++v) {                    // keys, then values
+                            ok = mbar_wait_while(ok, &st.bar_stempty[out.slot], out.par);
+                            ok = __all_sync(kFull, ok);
+                            if (!ok) break;                              // (the ring's position stays that of the last load)
+                            if (lead) mbar_arrive_expect_tx(&st.bar_stfull[out.slot], pieces * per * SM::kPartBytes);
+                            __syncwarp();
+                            if (lane < pieces) tma_load_3d(sS + out.slot * SM::kStageBytes + lane * per * pitch, &tmCache, &st.bar_stfull[out.slot], 0, v, at);
+                            out.next();
+                        }
                     }
                     if (i == 0 && lead) {
                         ok = mbar_wait_while(ok, &st.bar_qempty, (seg & 1) ^ 1);
@@ -588,12 +617,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                     }
                     ok = __shfl_sync(kFull, ok, 0);
-                    if (!ok) break;
                 }
             }
             __syncwarp();
             write_cut_unit(P, ci, cut);
-            if (lead) st.st_next = st_slot | st_par << 8;
+            if (lead) st.st_next = out.slot | out.par << 8;
             __syncwarp();
         } else if (warp == kMmaWarp) {
             // =================================== MMA issuer ===================================
@@ -766,11 +794,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         if (lane == 0 && st.abort) {
             // No load may land in shared memory that the CTA has left.  (Without an abort the roles have waited for every
             // one.)
-            const uint32_t n = st.st_next;
             mbar_drain(&st.bar_qfull, st.q_last);
-            for (int i = 0; i < RS; ++i) mbar_drain(&st.bar_stfull[i], last_armed_parity(i, n & 255, n >> 8));
-            if (st.k_tree & 1) mbar_drain(&st.bar_kfull[st.k_tree >> 8 & 255], st.k_tree >> 16);
-            if (st.v_tree & 1) mbar_drain(&st.bar_vfull[st.v_tree >> 8 & 255], st.v_tree >> 16);
+            for (int i = 0; i < RS; ++i) mbar_drain(&st.bar_stfull[i], last_armed_parity(i, st.st_next & 255, st.st_next >> 8));
+            if (st.k_tree >> 16) mbar_drain(&st.bar_kfull[st.k_tree & 255], st.k_tree >> 8 & 1);
+            if (st.v_tree >> 16) mbar_drain(&st.bar_vfull[st.v_tree & 255], st.v_tree >> 8 & 1);
             set_status(P.status, RADAR_ERR_TIMEOUT);
         }
         __syncwarp();
@@ -779,20 +806,31 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 }
 
 
+// a pool as [blocks][keys or values][bytes], in numbers of eight bytes; box: that of `box_blocks` blocks
+template <int D>
+bool make_cache_map(CUtensorMap* tm, const void* pages, long long blocks, int box_blocks) {
+    constexpr int kPart = Layout<D>::kBytes / 2;
+    cuuint64_t dims[3] = {kPart / 8, 2, (cuuint64_t)blocks}, strides[2] = {kPart, 2 * kPart};
+    cuuint32_t box[3] = {kPart / 8, 1, (cuuint32_t)box_blocks}, es[3] = {1, 1, 1};
+    return encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 3, const_cast<void*>(pages), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool TWO>
 int launch_tc(radar_ctx* ctx, const radar_cache_attn_args& c, TcParams& P, cudaStream_t stream) {
     using SM = Smem<D, TWO>;
-    CUtensorMap tmQ, tmKt, tmVt;
+    CUtensorMap tmQ, tmKt, tmVt, tmCache;
     const long long tree_rows = (long long)c.B * c.rows;
     if (!make_map(&tmQ, c.Q, D, c.Hq, tree_rows, P.G, P.nodes_per_rb, 1, 0, c.q_row_stride) ||
         !make_map(&tmKt, c.Kt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride) ||
-        !make_map(&tmVt, c.Vt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride))
+        !make_map(&tmVt, c.Vt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride) ||
+        !make_cache_map<D>(&tmCache, c.pages, std::max<long long>(c.n_pages, 1) * c.Hkv * P.blocks_per_page, std::min(P.blocks_per_page, kTileBlocks)))
         return RADAR_ERR_CUDA;
     auto* const kernel = cache_attn_tc_kernel<D, TWO>;
     RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_ATTN_TC + 2 * (D == 128) + TWO, kernel, (size_t)SM::kDynamic));
     {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_ATTN, stream);
-        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)(P.n_cls * P.ncc)), dim3(kTcThreads), (size_t)SM::kDynamic, stream, tmQ, tmKt, tmVt, P));
+        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)(P.n_cls * P.ncc)), dim3(kTcThreads), (size_t)SM::kDynamic, stream, tmQ, tmKt, tmVt, tmCache, P));
     }
     {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_COMBINE, stream);
