@@ -571,36 +571,24 @@ def radar_cache_attn_workspace_bytes(ctx: Context, B, Hq, Hkv, d, rows, max_cach
     return int(lib().radar_cache_attn_workspace_bytes(ctx.handle, B, Hq, Hkv, d, rows, max_cache_len))
 
 
-_cache_extend = _Call(
-    "radar_cache_extend", CacheExtendArgs,
-    dict({f: _i32 for f in ("cache_len", "new_len", "block_table", "free_pages", "free_count", "cache_len_out", "free_count_out", "start", "path_nodes",
-                            "src_row")}, granted=_u8, slots=_i64),
-    ("extra", "path_nodes", "path_stride", "rows", "src_row"))
-_cache_store = _Call("radar_cache_store", CacheStoreArgs, dict(slots=_i64, src_row=_i32, pages=_u8), ("src_row",), ("K", "V"))
-_cache_load = _Call("radar_cache_load", CacheLoadArgs, dict(block_table=_i32, first=_i32, start=_i32, pages=_u8), ())
-_cache_attention = _Call(
-    "radar_cache_attention", CacheAttnArgs,
-    dict(mask=_i64, n_nodes=_i32, pages=_u8, block_table=_i32, cache_len=_i32, O=torch.bfloat16, lse=_f32), ("mask", "n_nodes", "scale", "lse"), ("Q", "Kt", "Vt"))
+class _CacheCall:
+    """An entry point of the 4-bit cache: the marshaller's function of that name reads, checks and fills in its arguments."""
+
+    def __init__(self, name):
+        self.name, self.call, self.address = name, None, 0
+
+    def __call__(self, ctx, stream, *args):
+        if self.call is None:
+            self.address = ctypes.cast(getattr(lib(), self.name), _vp).value
+            from . import _marshal
+            self.call = getattr(_marshal, self.name[len("radar_"):])             # last: another thread may test it
+        handle = ctx.handle
+        status = self.call(self.address, handle.value if handle else 0, _raw_stream(stream), *args)
+        if status != RADAR_OK:
+            raise RadarError(self.name, status)
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _strided_rows(name, t, lead):
-    """Address of rows [..., heads, d] whose `lead` leading dimensions may have any strides, the last two lie together."""
-    _need(t.is_cuda and t.dim() == lead + 2 and t.stride(-1) == 1 and (t.stride(-2) == t.shape[-1] or t.shape[-2] == 1),
-          "%s: expected a CUDA tensor of %d dimensions whose last two are contiguous" % (name, lead + 2))
-    return t.data_ptr()
-
-
-def _pool(pages, page_size, Hkv, d, n_layers):
-    """(pages of a pool, bytes between pools) of `pages` [n_pages, page bytes] or [n_layers, n_pages, page bytes]."""
-    size = radar_cache_page_bytes(Hkv, d, page_size)
-    _need(pages.dim() in (2, 3) and pages.shape[-1] == size and (pages.shape[0] if pages.dim() == 3 else 1) == n_layers,
-          "pages: expected [%s n_pages, %d], got %s" % ("%d," % n_layers if pages.dim() == 3 or n_layers > 1 else "", size, tuple(pages.shape)))
-    return pages.shape[-2], pages.shape[-2] * size
+_cache_extend, _cache_store, _cache_load, _cache_attention = (_CacheCall("radar_cache_" + n) for n in ("extend", "store", "load", "attention"))
 
 
 def radar_cache_extend(ctx: Context, *, page_size, cache_len, new_len, block_table, free_pages, free_count, slots, start, granted, cache_len_out=None,
@@ -609,46 +597,21 @@ def radar_cache_extend(ctx: Context, *, page_size, cache_len, new_len, block_tab
     block_table [B, max_pages], free_pages [capacity], free_count [1], start [B + 1] int32, granted [B] uint8, slots [capacity]
     int64; without cache_len_out and free_count_out, cache_len and free_count are updated in place.  path_nodes
     [B, columns] with `rows` and src_row [capacity] int32: the row of each added token in [B, rows, ...] tensors."""
-    B, capacity = cache_len.numel(), slots.numel()
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and new_len.numel() == B and granted.numel() == B and start.numel() == B + 1,
-          "radar_cache_extend: cache_len, new_len, granted [B], block_table [B, max_pages] and start [B + 1] disagree about B")
-    kw = dict(B=B, page_size=page_size, max_pages=block_table.shape[1], cache_len=cache_len, new_len=new_len, extra=extra, block_table=block_table,
-              free_pages=free_pages, free_count=free_count, free_capacity=free_pages.numel(), cache_len_out=cache_len if cache_len_out is None else cache_len_out,
-              free_count_out=free_count if free_count_out is None else free_count_out, granted=granted, start=start, slots=slots, slot_capacity=capacity)
-    if path_nodes is not None:
-        _need(path_nodes.dim() == 2 and path_nodes.shape[0] == B and src_row is not None and src_row.numel() >= capacity,
-              "radar_cache_extend: path_nodes [B, columns] needs src_row of at least the slots' size")
-        kw.update(path_nodes=path_nodes, path_stride=path_nodes.shape[1], rows=rows, src_row=src_row)
-    _cache_extend(ctx, stream, kw)
+    _cache_extend(ctx, stream, page_size, cache_len, new_len, extra, block_table, free_pages, free_count, slots, start, granted, cache_len_out, free_count_out,
+                  path_nodes, rows, src_row)
 
 
 def radar_cache_store(ctx: Context, *, K, V, slots, pages, page_size, src_row=None, stream=None):
     """Rows of K and V ([rows, Hkv, d], or [layers, rows, Hkv, d] for all layers at once; float32 or bfloat16, any strides between
     rows and layers) into the slots of `pages` (uint8, [n_pages, page bytes] or with a leading layer dimension).  Token i is row
     src_row[i], or row i."""
-    lead = K.dim() - 2
-    _need(lead in (1, 2) and K.shape == V.shape and K.dtype == V.dtype and K.stride() == V.stride(), "K and V must share shape, dtype and strides")
-    layers, rows, (Hkv, d) = (K.shape[0] if lead == 2 else 1), K.shape[-3], K.shape[-2:]
-    n_pages, layer_bytes = _pool(pages, page_size, Hkv, d, layers)
-    n = slots.numel()
-    _need((src_row is None and rows >= n) or (src_row is not None and src_row.numel() >= n), "fewer rows (or entries of src_row) than slots")
-    _cache_store(ctx, stream, dict(n_layers=layers, Hkv=Hkv, d=d, page_size=page_size, dtype=dtype_code(K), n_tokens=n, n_rows=rows, n_pages=n_pages,
-                                   K=_strided_rows("K", K, lead), V=_strided_rows("V", V, lead), row_stride=K.stride(-3) if rows > 1 else Hkv * d,
-                                   row_layer_stride=K.stride(0) if lead == 2 else 0, slots=slots, src_row=src_row, pages=pages, page_layer_stride=layer_bytes))
+    _cache_store(ctx, stream, K, V, slots, pages, page_size, src_row)
 
 
 def radar_cache_load(ctx: Context, *, pages, page_size, block_table, first, start, K, V, stream=None):
     """Cached tokens first[b] .. of each request as rows start[b] .. start[b + 1] of K and V ([rows, Hkv, d], or with a leading
     layer dimension; float32 or bfloat16)."""
-    lead = K.dim() - 2
-    _need(lead in (1, 2) and K.shape == V.shape and K.dtype == V.dtype, "K and V must share shape and dtype")
-    layers, rows, (Hkv, d) = (K.shape[0] if lead == 2 else 1), K.shape[-3], K.shape[-2:]
-    n_pages, layer_bytes = _pool(pages, page_size, Hkv, d, layers)
-    B = first.numel()
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and start.numel() == B + 1, "block_table [B, max_pages], first [B] and start [B + 1] disagree about B")
-    _cache_load(ctx, stream, dict(n_layers=layers, B=B, Hkv=Hkv, d=d, page_size=page_size, max_pages=block_table.shape[1], dtype=dtype_code(K), n_rows=rows,
-                                  n_pages=n_pages, pages=pages, page_layer_stride=layer_bytes, block_table=block_table, first=first, start=start, K=K, V=V,
-                                  row_layer_stride=rows * Hkv * d))
+    _cache_load(ctx, stream, pages, page_size, block_table, first, start, K, V)
 
 
 def radar_cache_attention(ctx: Context, *, Q, Kt, Vt, pages, page_size, block_table, cache_len, max_cache_len, O, workspace, mask=None, n_nodes=None, lse=None,
@@ -656,21 +619,7 @@ def radar_cache_attention(ctx: Context, *, Q, Kt, Vt, pages, page_size, block_ta
     """One layer's attention over the 4-bit cache.  Q [B, rows, Hq, d], Kt, Vt [B, rows, Hkv, d] bfloat16 (parts of a fused projection as
     they are: equal strides between all rows), pages [n_pages, page bytes] uint8, block_table [B, max_pages], cache_len [B]
     int32, mask [B, rows] int64 or None (a chain), n_nodes [B] int32 or None (all rows); O [B, rows, Hq, d], lse [B, Hq, rows]."""
-    _need(Q.dim() == 4 and Kt.dim() == 4 and Q.dtype == Kt.dtype == Vt.dtype == torch.bfloat16, "Q, Kt and Vt: expected bfloat16 [B, rows, heads, d]")
-    B, rows, Hq, d = Q.shape
-    Hkv = Kt.shape[2]
-    _need(Kt.shape == Vt.shape and Kt.shape == (B, rows, Hkv, d) and O.shape == Q.shape and Kt.stride() == Vt.stride(), "Q, O, Kt and Vt disagree in shape or strides")
-    for name, t in (("Q", Q), ("Kt", Kt)):
-        _need(B == 1 or rows == 1 or t.stride(0) == rows * t.stride(1), "%s: the rows of a sequence must follow those of the one before" % name)
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and cache_len.numel() == B and (n_nodes is None or n_nodes.numel() == B) and
-          (mask is None or mask.shape == (B, rows)) and (lse is None or lse.shape == (B, Hq, rows)), "block_table, cache_len, n_nodes, mask or lse disagree with Q")
-    n_pages, _ = _pool(pages, page_size, Hkv, d, 1)
-    stride = lambda t, heads: t.stride(1) if rows > 1 else t.stride(0) if B > 1 else heads * d
-    _cache_attention(ctx, stream, dict(
-        B=B, Hq=Hq, Hkv=Hkv, d=d, rows=rows, dtype=RADAR_BF16, Q=_strided_rows("Q", Q, 2), Kt=_strided_rows("Kt", Kt, 2), Vt=_strided_rows("Vt", Vt, 2),
-        q_row_stride=stride(Q, Hq), kv_row_stride=stride(Kt, Hkv), mask=mask, n_nodes=n_nodes, pages=pages, n_pages=n_pages, page_size=page_size,
-        max_pages=block_table.shape[1], block_table=block_table, cache_len=cache_len, max_cache_len=max_cache_len, scale=scale, O=O, lse=lse,
-        workspace=workspace, workspace_bytes=workspace.numel() * workspace.element_size()))
+    _cache_attention(ctx, stream, Q, Kt, Vt, pages, page_size, block_table, cache_len, max_cache_len, O, workspace, mask, n_nodes, lse, scale)
 
 
 def radar_policy_param_count(k: int) -> int:

@@ -17,6 +17,7 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std
 
 MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")
 MARSHAL = os.path.join(HERE, "_marshal.so")
+HEADER = os.path.join(os.path.dirname(HERE), "include", "radar.h")
 
 
 def _torch_dir() -> str:
@@ -34,7 +35,7 @@ def marshal_tag() -> str:
 
 
 def _marshal_is_current() -> bool:
-    if not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < os.path.getmtime(MARSHAL_SRC):
+    if not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < max(os.path.getmtime(MARSHAL_SRC), os.path.getmtime(HEADER)):
         return False
     with open(MARSHAL, "rb") as f:                   # the module carries its tag as a string
         return marshal_tag().encode() + b"\0" in f.read()
@@ -67,7 +68,7 @@ def _finish_marshal(started):
 def _deps():
     out = [os.path.join(CSRC, s) for s in SOURCES]
     out += [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
-    out.append(os.path.join(os.path.dirname(HERE), "include", "radar.h"))
+    out.append(HEADER)
     return out
 
 
