@@ -221,97 +221,164 @@ __global__ void __launch_bounds__(kExtendThreads) cache_lengths_kernel(const Ext
     }
 }
 
-// ---- radar_cache_store --------------------------------------------------------------------------------------------------
+// ---- radar_cache_store and radar_cache_load -----------------------------------------------------------------------------
+// A warp takes a window of consecutive tokens and one KV head: a lane a group of 16 channels of every 32 / (d / 16)-th of them.  Where
+// the tokens are is worked out once a window, by a lane for each token, and handed round.  All loads of K, then of V, are in
+// flight together.
+template <int D>
+struct Window {
+    static constexpr int kGroups = D / 16, kSide = 32 / kGroups;         // lanes of a row, and rows side by side
+    int64_t block;           // of this lane's token: offset of its block in a layer's pool, -1: none
+    int row, r;              // row of K and V, row of the block
+
+    // token `t` of the window, from the lane that knows it
+    __device__ __forceinline__ Window of(int t) const {
+        Window w;
+        w.block = __shfl_sync(kFull, block, t);
+        w.row = __shfl_sync(kFull, row, t);
+        w.r = __shfl_sync(kFull, r, t);
+        return w;
+    }
+};
+
 struct StoreParams {
     radar_cache_store_args a;
     int64_t page_bytes;
+    int64_t windows;
     int shift;
     int* status;
 };
 
-__device__ __forceinline__ void load_group(const float* p, float (&x)[16]) {
+// 16 channels as they are loaded
+template <typename T>
+struct Group {
+    uint4 w[sizeof(T)];                                                  // two of bf16, four of fp32
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float4 t = __ldcs(reinterpret_cast<const float4*>(p) + i);
-        x[4 * i] = t.x; x[4 * i + 1] = t.y; x[4 * i + 2] = t.z; x[4 * i + 3] = t.w;
+        for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
     }
-}
-__device__ __forceinline__ void load_group(const __nv_bfloat16* p, float (&x)[16]) {
+    __device__ __forceinline__ uint32_t word(int i) const { return (&w[i >> 2].x)[i & 3]; }
+    __device__ __forceinline__ float value(int c) const {
+        if (sizeof(T) == 4) return __uint_as_float(word(c));
+        return __uint_as_float((c & 1) ? word(c >> 1) & 0xffff0000u : word(c >> 1) << 16);
+    }
+    // the largest magnitude, its bits as those of a float32: an infinity or a NaN is the largest
+    __device__ __forceinline__ uint32_t top() const {
+        if (sizeof(T) == 4) {
+            uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint4 t = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
-            x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            for (int i = 0; i < 16; ++i) m = max(m, word(i) & 0x7fffffffu);
+            return m;
         }
+        uint32_t m = 0;                                                  // two bf16 side by side
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7fff7fffu);
+        return max(m << 16, m & 0xffff0000u);
     }
-}
+};
 
-// A group's codes (two words) and scale byte.
-__device__ __forceinline__ uint2 quantise(float (&x)[16], uint32_t& scale, bool& nan) {
-    float top = 0.f;
-    nan = false;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) nan |= x[i] != x[i];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        if (nan && x[i] != x[i]) x[i] = 0.f;
-        top = fmaxf(top, fabsf(x[i]));
-    }
+// A group's codes (two words) and scale byte.  x / s is the quotient rounded to fp32, by one step of Markstein's correction
+// (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): with y = 1 / s rounded,
+// q = x y, the remainder x - q s is exact in a fused multiply-add and q + (x - q s) y rounds to the quotient.  So what lies in
+// the middle between two codes comes out there.  Adding 1.5 2^23 + 8 rounds it to an integer (to even), whose low bits are
+// the code; |x / s| is below 7.5, as s is at least 16 / 17 of max / 7, but for scales at the end of their range and for
+// values that are no numbers, which take the other branch.
+__device__ __forceinline__ int scale_number(float top) {                 // not yet within 0 .. 255
     const uint32_t bits = __float_as_uint(__fdiv_rn(top, 7.f));
-    const int number = (int)((bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20) - 107 * 8;
-    scale = (uint32_t)max(0, min(number, 255));
-    const float s = __uint_as_float((scale + 107 * 8) << 20);
+    return (int)((bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20) - 107 * 8;
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + 107 * 8) << 20); }
+
+template <typename T>
+__device__ __forceinline__ uint2 quantise(const Group<T>& x, uint32_t& scale, bool& nan) {
+    const int number = scale_number(__uint_as_float(x.top()));
     uint32_t w[2] = {0, 0};
+    if (number <= 255) {
+        scale = (uint32_t)max(0, number);
+        const float s = scale_value(scale), y = __frcp_rn(s);
+        constexpr float kRound = 12582912.f + 8.f;
+        constexpr uint32_t kBits = 0x4B400000u;                          // of 1.5 2^23; what they add up to comes off below
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float q = fminf(fmaxf(rintf(__fdiv_rn(x[i], s)), -8.f), 7.f);
-        const int c = i & 7, nibble = (c >> 1) + 4 * (c & 1);
-        w[i >> 3] |= (uint32_t)((int)q + 8) << (4 * nibble);
+        for (int i = 0; i < 16; ++i) {
+            const float v = x.value(i), q = v * y, t = fmaf(fmaf(-q, s, v), y, q) + kRound;
+            const int c = i & 7, nibble = (c >> 1) + 4 * (c & 1);
+            w[i >> 3] += __float_as_uint(t) << (4 * nibble);
+        }
+        constexpr uint32_t kOff = kBits * 0x11111111u;
+        w[0] -= kOff;
+        w[1] -= kOff;
+    } else {                                                             // saturated, infinite or NaN
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x.value(i)));        // (of the numbers among them)
+        scale = (uint32_t)max(0, min(scale_number(top), 255));
+        const float s = scale_value(scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v = x.value(i), q = v != v ? 0.f : fminf(fmaxf(rintf(__fdiv_rn(v, s)), -8.f), 7.f);
+            nan |= v != v;
+            const int c = i & 7, nibble = (c >> 1) + 4 * (c & 1);
+            w[i >> 3] |= (uint32_t)((int)q + 8) << (4 * nibble);
+        }
     }
     return make_uint2(w[0], w[1]);
 }
 
-// One thread takes a group of K and the same of V.
-template <typename T, int D>
+template <typename T, int D, int PASSES>
 __global__ void __launch_bounds__(256) cache_store_kernel(const StoreParams P) {
     chain_wait();
+    using W = Window<D>;
     const radar_cache_store_args& a = P.a;
-    constexpr int kGroups = D / 16;
-    const int per_token = a.Hkv * kGroups;
-    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t i = item / per_token;
-    if (i >= a.n_tokens) return;
-    const int u = (int)(item - i * per_token), h = u / kGroups, g = u % kGroups, l = blockIdx.y;
-    const int64_t slot = a.slots[i], row = a.src_row != nullptr ? (int64_t)a.src_row[i] : i;
-    if (slot < 0) return;
-    const int64_t page = P.shift >= 0 ? slot >> P.shift : slot / a.page_size;
-    if (page >= a.n_pages || row < 0 || row >= a.n_rows) {
-        if (u == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
-        return;
+    const int lane = threadIdx.x & 31, g = lane % W::kGroups, side = lane / W::kGroups, l = blockIdx.y;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), window = item / a.Hkv;
+    if (window >= P.windows) return;
+    const int h = (int)(item - window * a.Hkv);
+    W mine;
+    mine.block = -1; mine.row = 0; mine.r = 0;
+    const int64_t i = window * (W::kSide * PASSES) + lane;
+    if (lane < W::kSide * PASSES && i < a.n_tokens) {
+        const int64_t slot = a.slots[i], row = a.src_row != nullptr ? (int64_t)a.src_row[i] : i;
+        if (slot >= 0) {
+            const int64_t page = P.shift >= 0 ? slot >> P.shift : slot / a.page_size;
+            if (page >= a.n_pages || row < 0 || row >= a.n_rows) {
+                set_status(P.status, RADAR_ERR_INVALID_ARG);
+            } else {
+                const int in_page = (int)(slot - page * a.page_size);
+                mine.block = page * P.page_bytes + ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
+                mine.r = in_page & 15;
+                mine.row = (int)row;
+            }
+        }
     }
-    const int in_page = (int)(slot - page * a.page_size), r = in_page & 15;
-    unsigned char* block = reinterpret_cast<unsigned char*>(a.pages) + l * a.page_layer_stride + page * P.page_bytes +
-                           ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
-    const int64_t from = l * a.row_layer_stride + row * a.row_stride + h * D + g * 16;
-    float x[16], y[16];
-    load_group(reinterpret_cast<const T*>(a.K) + from, x);
-    load_group(reinterpret_cast<const T*>(a.V) + from, y);
-    uint32_t sk, sv;
-    bool nan_k, nan_v;
-    *reinterpret_cast<uint2*>(block + k_codes_at<D>(r, g)) = quantise(x, sk, nan_k);
-    *reinterpret_cast<uint2*>(block + v_codes_at<D>(r, g)) = quantise(y, sv, nan_v);
-    block[k_scale_at<D>(r, g)] = (unsigned char)sk;
-    block[v_scale_at<D>(r, g)] = (unsigned char)sv;
-    if (nan_k || nan_v) set_status(P.status, RADAR_ERR_NUMERIC);
+    W at[PASSES];
+    Group<T> x[PASSES];
+    unsigned char* pool = reinterpret_cast<unsigned char*>(a.pages) + l * a.page_layer_stride;
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) at[k] = mine.of(side + k * W::kSide);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const T* from = reinterpret_cast<const T*>(v ? a.V : a.K) + l * a.row_layer_stride + h * D + g * 16;
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k)
+            if (at[k].block >= 0) x[k].load(from + at[k].row * a.row_stride);
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            if (at[k].block < 0) continue;
+            unsigned char* block = pool + at[k].block;
+            uint32_t scale;
+            const uint2 codes = quantise(x[k], scale, nan);
+            *reinterpret_cast<uint2*>(block + (v ? v_codes_at<D>(at[k].r, g) : k_codes_at<D>(at[k].r, g))) = codes;
+            block[v ? v_scale_at<D>(at[k].r, g) : k_scale_at<D>(at[k].r, g)] = (unsigned char)scale;
+        }
+    }
+    if (nan) set_status(P.status, RADAR_ERR_NUMERIC);
 }
 
-// ---- radar_cache_load ---------------------------------------------------------------------------------------------------
 struct LoadParams {
     radar_cache_load_args a;
     int64_t page_bytes;
+    int64_t windows;
     int shift;
     int* status;
 };
@@ -332,37 +399,68 @@ __device__ __forceinline__ void decode_group(uint2 w, uint32_t byte, uint32_t (&
     v[4] = decode<0>(w.y, s, off); v[5] = decode<1>(w.y, s, off); v[6] = decode<2>(w.y, s, off); v[7] = decode<3>(w.y, s, off);
 }
 
-template <typename T, int D>
+template <typename T, int D, int PASSES>
 __global__ void __launch_bounds__(256) cache_load_kernel(const LoadParams P) {
     chain_wait();
+    using W = Window<D>;
     const radar_cache_load_args& a = P.a;
-    constexpr int kGroups = D / 16;
-    const int per_token = a.Hkv * kGroups;
-    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t i = item / per_token;
-    const int64_t n = a.start[a.B];
-    if (i >= n || i >= a.n_rows) {
-        if (n > a.n_rows && item == a.n_rows * per_token) set_status(P.status, RADAR_ERR_INVALID_ARG);
-        return;
+    const int lane = threadIdx.x & 31, g = lane % W::kGroups, side = lane / W::kGroups, l = blockIdx.y;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), window = item / a.Hkv;
+    if (window >= P.windows) return;
+    const int h = (int)(item - window * a.Hkv);
+    W mine;
+    mine.block = -1; mine.row = 0; mine.r = 0;
+    const int64_t i = window * (W::kSide * PASSES) + lane;
+    if (lane < W::kSide * PASSES) {
+        const int n = a.start[a.B];
+        if (i < n && i >= a.n_rows) set_status(P.status, RADAR_ERR_INVALID_ARG);
+        if (i < n && i < a.n_rows) {
+            const int b = owner(a.start, a.B, (int)i);
+            const int64_t at = (int64_t)a.first[b] + (i - a.start[b]);
+            const int index = P.shift >= 0 ? (int)(at >> P.shift) : (int)(at / a.page_size);
+            const bool in_table = at >= 0 && at < (int64_t)a.max_pages * a.page_size;
+            const int page = in_table ? a.block_table[(int64_t)b * a.max_pages + index] : -1;
+            if (page < 0 || page >= a.n_pages) {
+                set_status(P.status, RADAR_ERR_INVALID_ARG);
+            } else {
+                const int in_page = (int)(at - (int64_t)index * a.page_size);
+                mine.block = page * P.page_bytes + ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
+                mine.r = in_page & 15;
+                mine.row = (int)i;
+            }
+        }
     }
-    const int u = (int)(item - i * per_token), h = u / kGroups, g = u % kGroups, l = blockIdx.y;
-    const int b = owner(a.start, a.B, (int)i);
-    const int64_t at = (int64_t)a.first[b] + (i - a.start[b]);
-    if (at < 0 || at >= (int64_t)a.max_pages * a.page_size) { if (u == 0) set_status(P.status, RADAR_ERR_INVALID_ARG); return; }
-    const int index = P.shift >= 0 ? (int)(at >> P.shift) : (int)(at / a.page_size);
-    const int page = a.block_table[(int64_t)b * a.max_pages + index];
-    if (page < 0 || page >= a.n_pages) { if (u == 0) set_status(P.status, RADAR_ERR_INVALID_ARG); return; }
-    const int in_page = (int)(at - (int64_t)index * a.page_size), r = in_page & 15;
-    const unsigned char* block = reinterpret_cast<const unsigned char*>(a.pages) + l * a.page_layer_stride + page * P.page_bytes +
-                                 ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
-    const uint2 kc = *reinterpret_cast<const uint2*>(block + k_codes_at<D>(r, g)), vc = *reinterpret_cast<const uint2*>(block + v_codes_at<D>(r, g));
-    const uint32_t ks = block[k_scale_at<D>(r, g)], vs = block[v_scale_at<D>(r, g)];
-    const int64_t to = l * a.row_layer_stride + (i * a.Hkv + h) * D + g * 16;
-    uint32_t v[8];
-    decode_group(kc, ks, v);
-    store_group(reinterpret_cast<T*>(a.K) + to, v);
-    decode_group(vc, vs, v);
-    store_group(reinterpret_cast<T*>(a.V) + to, v);
+    W at[PASSES];
+    const unsigned char* pool = reinterpret_cast<const unsigned char*>(a.pages) + l * a.page_layer_stride;
+    uint2 codes[2][PASSES];
+    uint32_t scale[2][PASSES];
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+        at[k] = mine.of(side + k * W::kSide);
+        if (at[k].block < 0) continue;
+        const unsigned char* block = pool + at[k].block;
+        const int r = at[k].r;
+        codes[0][k] = *reinterpret_cast<const uint2*>(block + k_codes_at<D>(r, g));
+        codes[1][k] = *reinterpret_cast<const uint2*>(block + v_codes_at<D>(r, g));
+        scale[0][k] = block[k_scale_at<D>(r, g)];
+        scale[1][k] = block[v_scale_at<D>(r, g)];
+    }
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+        if (at[k].block < 0) continue;
+        const int64_t to = l * a.row_layer_stride + ((int64_t)at[k].row * a.Hkv + h) * D + g * 16;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            uint32_t out[8];
+            decode_group(codes[v][k], scale[v][k], out);
+            store_group(reinterpret_cast<T*>(v ? a.V : a.K) + to, out);
+        }
+    }
+}
+
+// Passes of a warp: all 16 tokens of its window where that leaves every SM warps enough, one where there are few tokens.
+int window_passes(const radar_ctx* ctx, int64_t tokens, int Hkv, int d, int layers) {
+    return tokens * Hkv * layers >= (int64_t)ctx->sm_count * 16 * 32 ? 16 / (32 / (d / 16)) : 1;
 }
 
 int log2_of(int x) {
@@ -443,11 +541,15 @@ extern "C" int radar_cache_store(radar_ctx* ctx, const radar_cache_store_args* a
     P.page_bytes = page_bytes(a->Hkv, a->d, a->page_size);
     P.shift = log2_of(a->page_size);
     P.status = ctx->d_status;
-    const int64_t items = a->n_tokens * a->Hkv * (a->d / 16), blocks = (items + 255) / 256;
-    if (blocks > INT32_MAX) return RADAR_ERR_UNSUPPORTED;
+    const int passes = window_passes(ctx, a->n_tokens, a->Hkv, a->d, a->n_layers), tokens = 32 / (a->d / 16) * passes;
+    P.windows = (a->n_tokens + tokens - 1) / tokens;
+    const int64_t blocks = (P.windows * a->Hkv + 7) / 8;
+    if (blocks > INT32_MAX || a->n_rows > INT32_MAX) return RADAR_ERR_UNSUPPORTED;
     return by_type(a->dtype, a->d, [&](auto t, auto d) -> int {
+        constexpr int D = decltype(d)::value;
         radar_launch_scope scope(ctx, RADAR_K_CACHE_STORE, stream);
-        RADAR_CUDA_CHECK(launch_chained(cache_store_kernel<decltype(t), decltype(d)::value>, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
+        auto* const kernel = passes > 1 ? cache_store_kernel<decltype(t), D, D / 32> : cache_store_kernel<decltype(t), D, 1>;
+        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
         return RADAR_OK;
     });
 }
@@ -469,11 +571,15 @@ extern "C" int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* a, 
     P.page_bytes = page_bytes(a->Hkv, a->d, a->page_size);
     P.shift = log2_of(a->page_size);
     P.status = ctx->d_status;
-    const int64_t items = a->n_rows * a->Hkv * (a->d / 16) + 1, blocks = (items + 255) / 256;    // (one more: it sees rows that do not fit)
+    const int passes = window_passes(ctx, a->n_rows, a->Hkv, a->d, a->n_layers), tokens = 32 / (a->d / 16) * passes;
+    P.windows = (a->n_rows + 1 + tokens - 1) / tokens;           // (one token more: it sees rows that do not fit)
+    const int64_t blocks = (P.windows * a->Hkv + 7) / 8;
     if (blocks > INT32_MAX) return RADAR_ERR_UNSUPPORTED;
     return by_type(a->dtype, a->d, [&](auto t, auto d) -> int {
+        constexpr int D = decltype(d)::value;
         radar_launch_scope scope(ctx, RADAR_K_CACHE_LOAD, stream);
-        RADAR_CUDA_CHECK(launch_chained(cache_load_kernel<decltype(t), decltype(d)::value>, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
+        auto* const kernel = passes > 1 ? cache_load_kernel<decltype(t), D, D / 32> : cache_load_kernel<decltype(t), D, 1>;
+        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
         return RADAR_OK;
     });
 }

@@ -7,11 +7,12 @@ namespace radar {
 struct CacheAttnParams {
     radar_cache_attn_args a;
     int G;
-    int n_tiles, n_splits, split_len;            // row tiles, splits of a unit, keys of a split
+    int blocks, cluster;                         // of the launch; of a unit, in the form for little work
     int blocks_per_page, page_shift_blocks;      // log2 of it, -1: no power of two
     int64_t page_bytes;
     float scale_log2;
-    float2* part_ml;                             // [B][rows][Hq][n_splits] (maximum in log2 units, sum)
+    // [blocks][2][8 or 16 rows]: a block's share of the unit that its range begins in, and of the one that it ends in
+    float2* part_ml;                             // (maximum in log2 units, sum)
     float* part_o;                               // ... [D], not normalised
     int* status;
 };

@@ -51,7 +51,8 @@ enum radar_smem_slot {
     RADAR_SMEM_CACHE_ATTN = RADAR_SMEM_ATTN_TC + 16,   // + 4 * (d == 128) + row tiles of eight - 1
     RADAR_SMEM_CACHE_EXTEND = RADAR_SMEM_CACHE_ATTN + 8,   // + (several blocks)
     RADAR_SMEM_CACHE_ATTN_TC = RADAR_SMEM_CACHE_EXTEND + 2,   // + 2 * (d == 128) + two
-    RADAR_SMEM_COUNT = RADAR_SMEM_CACHE_ATTN_TC + 4
+    RADAR_SMEM_CACHE_SMALL = RADAR_SMEM_CACHE_ATTN_TC + 4,    // + 2 * (d == 128) + row tiles of eight - 1
+    RADAR_SMEM_COUNT = RADAR_SMEM_CACHE_SMALL + 4
 };
 
 struct radar_ctx {
