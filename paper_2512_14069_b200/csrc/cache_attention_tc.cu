@@ -12,9 +12,9 @@
 //   warp 17          issues the products
 // What bounds the kernel is the issue of instructions: decoding takes twelve for eight values, a tile some 2300 by all warps, as many as
 // its softmax for one row block, and a warp issues one about every five cycles here.  So what surrounds the decoding is kept to a
-// few waits a tile, and everything in the steady state is a small loop (with the softmax of tree_attention_tc.cu beside it, 128 scores
-// in line, instructions were fetched anew all along): scores are read from tensor memory twice, 32 at a time, and keys and
-// values are decoded by the same code.  That also makes room for eight decoders at 96 registers a thread.
+// few waits a tile, and everything in the steady state is a small loop, keys and values decoded by the same code (with the
+// softmax of tree_attention_tc.cu beside it, 128 scores in line, instructions were fetched anew all along).  A thread takes its
+// row's scores 64 at a time, which also makes room for eight decoders at 96 registers; the maximum is looked at for each 64.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -131,6 +131,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2];
         uint64_t bar_idle;               // every product issued has run
         uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
+        uint64_t bar_pv[2];              // ... and their product has run
         uint64_t bar_pready[2];          // ... all of them
         uint64_t bar_mlfull, bar_mlempty;
         uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
@@ -160,7 +161,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecoders); mbar_init(&st.bar_vempty[i], 1); }
             for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[i], 1); mbar_init(&st.bar_stempty[i], kDecoders); }
             for (int i = 0; i < 2; ++i) {
-                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
+                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pv[i], 1); mbar_init(&st.bar_pready[i], 4);
                 mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
             }
             for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
@@ -250,127 +251,104 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 ok = __all_sync(kFull, ok);                      // warp-uniform: guards .aligned ops
                 ++sc;
                 tc_fence_after_sync();
-                if (ok && warp_live) {
-                    uint32_t va[32], vb[32];
-                    const int valid = s.Pb - t * kTileKeys;
-                    if (t == s.nt - 1 || valid < kTileKeys) {
-                        // Keys that the row may not attend to (and, of the tree tile, which has 64, the columns that are stale)
-                        // become -inf in tensor memory.
+                const int keys = t == s.nt - 1 ? s.M : min(kTileKeys, s.Pb - t * kTileKeys);
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t al;
-                            if (t == s.nt - 1) {
-                                const int live = s.M - c * 32;
-                                al = row < rows_here && c < 2 && live > 0 ? (c == 0 ? mask_lo : mask_hi) & (live >= 32 ? 0xffffffffu : (1u << live) - 1u) : 0u;
-                            } else {
+                for (int half = 0; half < 2; ++half) {
+                    const int valid = keys - half * kFirstKeys;
+                    if (ok && warp_live && valid > 0) {
+                        const uint32_t tH = tS + half * kFirstKeys;
+                        uint32_t va[32], vb[32];
+                        if (t == s.nt - 1 || valid < kFirstKeys) {
+                            // Keys that the row may not attend to, and columns that are stale, become -inf in tensor memory.
+#pragma unroll 1
+                            for (int c = 0; c < 2; ++c) {
                                 const int lim = valid - c * 32;
-                                al = lim >= 32 ? 0xffffffffu : (lim <= 0 ? 0u : ((1u << lim) - 1u));
-                            }
-                            tmem_ld32(tS + c * 32, va);
-                            tmem_wait_ld();
+                                uint32_t al = lim >= 32 ? 0xffffffffu : (lim <= 0 ? 0u : ((1u << lim) - 1u));
+                                if (t == s.nt - 1) al &= row < rows_here ? (c == 0 ? mask_lo : mask_hi) : 0u;
+                                tmem_ld32(tH + c * 32, va);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!((al >> e) & 1u)) va[e] = 0xff800000u;     // -inf
-                            tmem_st32(tS + c * 32, va);
+                                for (int e = 0; e < 32; ++e)
+                                    if (!((al >> e) & 1u)) va[e] = 0xff800000u;     // -inf
+                                tmem_st32(tH + c * 32, va);
+                            }
+                            tmem_wait_st();
                         }
+                        tmem_ld32(tH, va);
+                        tmem_ld32(tH + 32, vb);
+                        tmem_wait_ld();
+                        float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {                       // three-input maxima: half the instructions
+                            mx0 = max3(mx0, __uint_as_float(va[e]), __uint_as_float(va[e + 1]));
+                            mx1 = max3(mx1, __uint_as_float(vb[e]), __uint_as_float(vb[e + 1]));
+                        }
+                        // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
+                        const float m_half = fmaxf(mx0, mx1) * P.scale_log2;
+                        const bool first = j == 0 && half == 0;
+                        float factor = 1.f;
+                        if (first) {
+                            m_run = m_half;
+                        } else if (m_half > m_run + kRescaleThreshold) {
+                            factor = ex2(m_run - m_half);           // m_run may be -inf: factor 0 clears O and l
+                            m_run = m_half;
+                        }
+                        if (!first && __any_sync(kFull, factor != 1.f)) {
+                            // (in the second half, the first one's product may still be under way)
+                            if (half == 1) {
+                                ok = mbar_wait_while(ok, &st.bar_pv[grp], (sc - 1) & 1);
+                                tc_fence_after_sync();
+                            }
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(tO + c, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                                tmem_st16(tO + c, o);
+                            }
+                        }
+                        const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
+                        // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
+                        // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
+                        // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
+                        // two of them.
+                        float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
+                        auto exponentials = [&](uint32_t (&v)[32], const uint32_t to) {
+                            uint32_t pk[16];
+                            auto scale = [&](const int p) {
+                                const float2 t2 = fma2_in_order(make_float2(__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])), sc2, nm2);
+                                v[2 * p] = __float_as_uint(t2.x);
+                                v[2 * p + 1] = __float_as_uint(t2.y);
+                            };
+                            auto finish = [&](const int p) {
+                                const float p0 = __uint_as_float(v[2 * p]), p1 = __uint_as_float(v[2 * p + 1]);
+                                ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
+                                pk[p] = bf16x2_in_order(p0, p1);
+                            };
+                            // pairs that the scaling is ahead, and that the rest is behind
+                            constexpr int kAhead = 2, kLag = 3;
+#pragma unroll
+                            for (int p = 0; p < kAhead; ++p) scale(p);
+#pragma unroll
+                            for (int p = 0; p < 16 + kLag; ++p) {
+                                if (p < 16) v[2 * p] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p])));
+                                if (p + kAhead < 16) scale(p + kAhead);
+                                if (p < 16) v[2 * p + 1] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p + 1])));
+                                if (p >= kLag) finish(p - kLag);
+                            }
+                            tmem_st16(to, pk);
+                        };
+                        exponentials(va, tS + half * 32);
+                        exponentials(vb, tS + half * 32 + 16);
+                        l_run = l_run * factor + ((ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
                         tmem_wait_st();
                     }
-                    // ---- maximum: 32 scores at a time, the next 32 on their way ----
-                    float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
-                    auto maxima = [&](const uint32_t (&v)[32]) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {                   // three-input maxima: half the instructions
-                            mx0 = max3(mx0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-                            mx1 = max3(mx1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
-                        }
-                    };
-                    tmem_ld32(tS, va);
-#pragma unroll 1
-                    for (int c = 0; c < 4; c += 2) {
-                        tmem_wait_ld();
-                        tmem_ld32(tS + (c + 1) * 32, vb);
-                        maxima(va);
-                        tmem_wait_ld();
-                        if (c == 0) tmem_ld32(tS + 64, va);
-                        maxima(vb);
-                    }
-                    const float mx = fmaxf(mx0, mx1);
-                    // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
-                    const float m_tile = mx * P.scale_log2;
-                    float factor = 1.f;
-                    if (j == 0) {
-                        m_run = m_tile;
-                    } else if (m_tile > m_run + kRescaleThreshold) {
-                        factor = ex2(m_run - m_tile);           // m_run may be -inf: factor 0 clears O and l
-                        m_run = m_tile;
-                    }
-                    const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
-                    if (j > 0 && __any_sync(kFull, factor != 1.f)) {
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(tO + c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                            tmem_st16(tO + c, o);
-                        }
-                    }
-                    tmem_ld32(tS, va);           // (not ahead of the rescaling: nothing may look at these registers before the wait)
-                    // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
-                    // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
-                    // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
-                    // two of them.
-                    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
-                    auto exponentials = [&](uint32_t (&v)[32], const uint32_t to) {
-                        uint32_t pk[16];
-                        auto scale = [&](const int p) {
-                            const float2 t2 = fma2_in_order(make_float2(__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])), sc2, nm2);
-                            v[2 * p] = __float_as_uint(t2.x);
-                            v[2 * p + 1] = __float_as_uint(t2.y);
-                        };
-                        auto finish = [&](const int p) {
-                            const float p0 = __uint_as_float(v[2 * p]), p1 = __uint_as_float(v[2 * p + 1]);
-                            ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
-                            pk[p] = bf16x2_in_order(p0, p1);
-                        };
-                        // pairs that the scaling is ahead, and that the rest is behind
-                        constexpr int kAhead = 2, kLag = 3;
-#pragma unroll
-                        for (int p = 0; p < kAhead; ++p) scale(p);
-#pragma unroll
-                        for (int p = 0; p < 16 + kLag; ++p) {
-                            if (p < 16) v[2 * p] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p])));
-                            if (p + kAhead < 16) scale(p + kAhead);
-                            if (p < 16) v[2 * p + 1] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p + 1])));
-                            if (p >= kLag) finish(p - kLag);
-                        }
-                        tmem_st16(to, pk);
-                    };
-#pragma unroll 1
-                    for (int c = 0; c < 4; c += 2) {
-                        tmem_wait_ld();
-                        tmem_ld32(tS + (c + 1) * 32, vb);
-                        exponentials(va, tS + c * 16);
-                        tmem_wait_ld();
-                        if (c == 0) tmem_ld32(tS + 64, va);
-                        exponentials(vb, tS + c * 16 + 16);
-                        if (c == 0) {
-                            tmem_wait_st();
-                            tc_fence_before_sync();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&st.bar_pfirst[grp]);
-                        }
-                    }
-                    l_run = l_run * factor + ((ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
-                    tmem_wait_st();
-                }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    if (!(ok && warp_live)) mbar_arrive(&st.bar_pfirst[grp]);
-                    mbar_arrive(&st.bar_pready[grp]);
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(half == 0 ? &st.bar_pfirst[grp] : &st.bar_pready[grp]);
                 }
             }
 
@@ -690,13 +668,16 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                     }
                     take_o(q);
+                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
+                    tc_fence_after_sync();
+                    // V is consumed N-major: 16 keys are 2048 B; 64-column blocks are nk * 128 B apart
+                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(nk * 128 >> 4) << 16);
+                    mma_ts_x4(ok ? elected : 0u, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
+                    mma_commit_if(ok ? elected : 0u, &st.bar_pv[q]);
                     ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
                     p_par[q] ^= 1;
                     tc_fence_after_sync();
                     const uint32_t go = ok ? elected : 0u;
-                    // V is consumed N-major: 16 keys are 2048 B; 64-column blocks are nk * 128 B apart
-                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(nk * 128 >> 4) << 16);
-                    mma_ts_x4(go, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
                     mma_ts_x4(go, ksteps - 4, tmem + 256 + q * 128, tmem + q * 128 + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
                     acc[q] = true;
                     if (release_v) mma_commit_if(go, &st.bar_vempty[v_slot]);
@@ -735,6 +716,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
                     tc_fence_after_sync();
                     mma_ts_x4(ok ? elected : 0u, o_col, p_col, b_lo, kDescHi, idesc_pv, acc[q]);
+                    mma_commit_if(ok ? elected : 0u, &st.bar_pv[q]);
                     if (fresh) take_k();
                     const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
                     ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
