@@ -222,32 +222,42 @@ __global__ void __launch_bounds__(kExtendThreads) cache_lengths_kernel(const Ext
 }
 
 // ---- radar_cache_store and radar_cache_load -----------------------------------------------------------------------------
-// A warp takes a window of consecutive tokens and one KV head: a lane a group of 16 channels of every 32 / (d / 16)-th of them.  Where
-// the tokens are is worked out once a window, by a lane for each token, and handed round.  All loads of K, then of V, are in
-// flight together.
+// A lane takes 16 channels of a token's K and V: a warp one KV head of 32 / (d / 16) consecutive tokens.  Each lane looks up for itself
+// where its token lies (the token's lanes share the loads), and nothing passes between lanes.
 template <int D>
-struct Window {
-    static constexpr int kGroups = D / 16, kSide = 32 / kGroups;         // lanes of a row, and rows side by side
-    int64_t block;           // of this lane's token: offset of its block in a layer's pool, -1: none
-    int row, r;              // row of K and V, row of the block
-
-    // token `t` of the window, from the lane that knows it
-    __device__ __forceinline__ Window of(int t) const {
-        Window w;
-        w.block = __shfl_sync(kFull, block, t);
-        w.row = __shfl_sync(kFull, row, t);
-        w.r = __shfl_sync(kFull, r, t);
-        return w;
-    }
+struct Lanes {
+    static constexpr int kGroups = D / 16, kTokens = 32 / kGroups;       // lanes of a token, and tokens of a warp
 };
 
 struct StoreParams {
     radar_cache_store_args a;
     int64_t page_bytes;
-    int64_t windows;
+    int64_t warps;                   // of one KV head
     int shift;
     int* status;
 };
+
+// Rows are read and written once.  A lane's 32 bytes go in one access of 256 bits: in two of 128 bits each takes half of every
+// sector that the warp touches.  Rows that are only 16-byte aligned take the two.
+__device__ __forceinline__ bool wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
+__device__ __forceinline__ void load_row32(const void* p, uint4& a, uint4& b) {
+    if (wide(p)) {
+        asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
+    } else {
+        a = __ldcs(reinterpret_cast<const uint4*>(p));
+        b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    }
+}
+__device__ __forceinline__ void store_row32(void* p, const uint4& a, const uint4& b) {
+    if (wide(p)) {
+        asm volatile("st.global.cs.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                     :: "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w), "l"(p) : "memory");
+    } else {
+        __stcs(reinterpret_cast<uint4*>(p), a);
+        __stcs(reinterpret_cast<uint4*>(p) + 1, b);
+    }
+}
 
 // 16 channels as they are loaded
 template <typename T>
@@ -255,7 +265,7 @@ struct Group {
     uint4 w[sizeof(T)];                                                  // two of bf16, four of fp32
     __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+        for (int i = 0; i < (int)sizeof(T); i += 2) load_row32(p + i * 16 / (int)sizeof(T), w[i], w[i + 1]);
     }
     __device__ __forceinline__ uint32_t word(int i) const { return (&w[i >> 2].x)[i & 3]; }
     __device__ __forceinline__ float value(int c) const {
@@ -270,24 +280,48 @@ struct Group {
             for (int i = 0; i < 16; ++i) m = max(m, word(i) & 0x7fffffffu);
             return m;
         }
-        uint32_t m = 0;                                                  // two bf16 side by side
+        uint32_t m = word(0) & 0x7fff7fffu;                              // two bf16 side by side
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7fff7fffu);
+        for (int i = 1; i < 7; i += 2) m = __vimax3_u16x2(m, word(i) & 0x7fff7fffu, word(i + 1) & 0x7fff7fffu);
+        m = __vmaxu2(m, word(7) & 0x7fff7fffu);
         return max(m << 16, m & 0xffff0000u);
     }
 };
 
-// A group's codes (two words) and scale byte.  x / s is the quotient rounded to fp32, by one step of Markstein's correction
-// (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): with y = 1 / s rounded,
-// q = x y, the remainder x - q s is exact in a fused multiply-add and q + (x - q s) y rounds to the quotient.  So what lies in
-// the middle between two codes comes out there.  Adding 1.5 2^23 + 8 rounds it to an integer (to even), whose low bits are
-// the code; |x / s| is below 7.5, as s is at least 16 / 17 of max / 7, but for scales at the end of their range and for
-// values that are no numbers, which take the other branch.
+// A group's codes (two words) and scale byte.  Ties go to even, so x / s has to come out exact where it lies in the middle between
+// two codes; y = 1 / s rounded is off by up to 2^-24 of itself.
+// fp32: the quotient rounded to fp32, by one step of Markstein's correction (P. Markstein, "Computation of elementary functions
+// on the IBM RISC System/6000 processor", 1990): with q = x y, the remainder x - q s is exact in a fused multiply-add and
+// q + (x - q s) y rounds to the quotient.
+// bf16: with integers V < 2^8 and 8 <= S < 16, x / s is V 2^k / S, and (for |x / s| >= 1 / 4, so 2^k >= 2^-7) off the nearest
+// middle by nothing or by 2^-7 / 30 at least.  x y + 384, rounded once, is a multiple of 2^-15, off by 2^-16 + 8 2^-24: what lies in a
+// middle comes out there, what does not stays on its side.  That takes half the instructions, which bound this kernel.
+// Adding 1.5 2^23 + 8 rounds it to an integer (to even), whose low bits are the code; |x / s| is below 7.5, as s is at least 16 / 17
+// of max / 7, but for scales at the end of their range and for values that are no numbers, which take the other branch.
 __device__ __forceinline__ int scale_number(float top) {                 // not yet within 0 .. 255
     const uint32_t bits = __float_as_uint(__fdiv_rn(top, 7.f));
     return (int)((bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20) - 107 * 8;
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + 107 * 8) << 20); }
+
+// two fp32 operations an instruction
+__device__ __forceinline__ uint64_t both(float2 a) { return (uint64_t)__float_as_uint(a.y) << 32 | __float_as_uint(a.x); }
+__device__ __forceinline__ float2 parts(uint64_t a) { return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(both(a)), "l"(both(b)), "l"(both(c)));
+    return parts(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(both(a)), "l"(both(b)));
+    return parts(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(both(a)), "l"(both(b)));
+    return parts(r);
+}
 
 template <typename T>
 __device__ __forceinline__ uint2 quantise(const Group<T>& x, uint32_t& scale, bool& nan) {
@@ -296,17 +330,23 @@ __device__ __forceinline__ uint2 quantise(const Group<T>& x, uint32_t& scale, bo
     if (number <= 255) {
         scale = (uint32_t)max(0, number);
         const float s = scale_value(scale), y = __frcp_rn(s);
-        constexpr float kRound = 12582912.f + 8.f;
-        constexpr uint32_t kBits = 0x4B400000u;                          // of 1.5 2^23; what they add up to comes off below
+        const float2 y2 = make_float2(y, y), s2 = make_float2(-s, -s);
+        constexpr float kRound = 12582912.f + 8.f, kCoarse = sizeof(T) == 2 ? 384.f : 0.f;
+        const float2 coarse = make_float2(kCoarse, kCoarse), round = make_float2(kRound - kCoarse, kRound - kCoarse);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float v = x.value(i), q = v * y, t = fmaf(fmaf(-q, s, v), y, q) + kRound;
-            const int c = i & 7, nibble = (c >> 1) + 4 * (c & 1);
-            w[i >> 3] += __float_as_uint(t) << (4 * nibble);
+        for (int i = 0; i < 16; i += 2) {
+            const float2 v = make_float2(x.value(i), x.value(i + 1));
+            float2 q;
+            if (sizeof(T) == 4) {
+                q = mul2(v, y2);
+                q = fma2(fma2(q, s2, v), y2, q);
+            } else {
+                q = fma2(v, y2, coarse);
+            }
+            const float2 t = add2(q, round);
+            // even channels' codes lie in the low half word, odd ones' in the high one
+            w[i >> 3] += __byte_perm(__float_as_uint(t.x), __float_as_uint(t.y), 0x5410) << (2 * (i & 7));
         }
-        constexpr uint32_t kOff = kBits * 0x11111111u;
-        w[0] -= kOff;
-        w[1] -= kOff;
     } else {                                                             // saturated, infinite or NaN
         float top = 0.f;
 #pragma unroll
@@ -324,53 +364,42 @@ __device__ __forceinline__ uint2 quantise(const Group<T>& x, uint32_t& scale, bo
     return make_uint2(w[0], w[1]);
 }
 
-template <typename T, int D, int PASSES>
-__global__ void __launch_bounds__(256) cache_store_kernel(const StoreParams P) {
+// What bounds it: memory where there is much to store (8 KV heads of 128 channels, 32 layers, 2048 tokens of bf16: 53 us, 6.5 TB/s;
+// fp32 90 us, 6.8 TB/s), else a lookup, a load and a launch behind one another.  bf16: 32 registers a thread for 64 warps an SM (with 48 warps
+// 66 us; two or four tokens a lane in flight took 60 to 108).  fp32 has twice the bytes in flight a lane, and small calls took 3.6 us
+// instead of 3.2 when held to as few registers.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 4) cache_store_kernel(const StoreParams P) {
     chain_wait();
-    using W = Window<D>;
+    using L = Lanes<D>;
     const radar_cache_store_args& a = P.a;
-    const int lane = threadIdx.x & 31, g = lane % W::kGroups, side = lane / W::kGroups, l = blockIdx.y;
-    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), window = item / a.Hkv;
-    if (window >= P.windows) return;
-    const int h = (int)(item - window * a.Hkv);
-    W mine;
-    mine.block = -1; mine.row = 0; mine.r = 0;
-    const int64_t i = window * (W::kSide * PASSES) + lane;
-    if (lane < W::kSide * PASSES && i < a.n_tokens) {
-        const int64_t slot = a.slots[i], row = a.src_row != nullptr ? (int64_t)a.src_row[i] : i;
-        if (slot >= 0) {
-            const int64_t page = P.shift >= 0 ? slot >> P.shift : slot / a.page_size;
-            if (page >= a.n_pages || row < 0 || row >= a.n_rows) {
-                set_status(P.status, RADAR_ERR_INVALID_ARG);
-            } else {
-                const int in_page = (int)(slot - page * a.page_size);
-                mine.block = page * P.page_bytes + ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
-                mine.r = in_page & 15;
-                mine.row = (int)row;
-            }
-        }
+    const int lane = threadIdx.x & 31, g = lane % L::kGroups, l = blockIdx.y;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), warp = item / a.Hkv;
+    if (warp >= P.warps) return;
+    const int h = (int)(item - warp * a.Hkv);
+    const int64_t i = warp * L::kTokens + lane / L::kGroups;
+    if (i >= a.n_tokens) return;
+    const int64_t slot = a.slots[i], row = a.src_row != nullptr ? (int64_t)a.src_row[i] : i;
+    if (slot < 0) return;
+    const int64_t page = P.shift >= 0 ? slot >> P.shift : slot / a.page_size;
+    if (page >= a.n_pages || row < 0 || row >= a.n_rows) {
+        set_status(P.status, RADAR_ERR_INVALID_ARG);
+        return;
     }
-    W at[PASSES];
-    Group<T> x[PASSES];
-    unsigned char* pool = reinterpret_cast<unsigned char*>(a.pages) + l * a.page_layer_stride;
+    const int in_page = (int)(slot - page * a.page_size), r = in_page & 15;
+    unsigned char* block = reinterpret_cast<unsigned char*>(a.pages) + l * a.page_layer_stride + page * P.page_bytes +
+                           ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
+    const int64_t from = l * a.row_layer_stride + row * a.row_stride + h * D + g * 16;
+    Group<T> x[2];
+    x[0].load(reinterpret_cast<const T*>(a.K) + from);
+    x[1].load(reinterpret_cast<const T*>(a.V) + from);
     bool nan = false;
 #pragma unroll
-    for (int k = 0; k < PASSES; ++k) at[k] = mine.of(side + k * W::kSide);
-#pragma unroll
     for (int v = 0; v < 2; ++v) {
-        const T* from = reinterpret_cast<const T*>(v ? a.V : a.K) + l * a.row_layer_stride + h * D + g * 16;
-#pragma unroll
-        for (int k = 0; k < PASSES; ++k)
-            if (at[k].block >= 0) x[k].load(from + at[k].row * a.row_stride);
-#pragma unroll
-        for (int k = 0; k < PASSES; ++k) {
-            if (at[k].block < 0) continue;
-            unsigned char* block = pool + at[k].block;
-            uint32_t scale;
-            const uint2 codes = quantise(x[k], scale, nan);
-            *reinterpret_cast<uint2*>(block + (v ? v_codes_at<D>(at[k].r, g) : k_codes_at<D>(at[k].r, g))) = codes;
-            block[v ? v_scale_at<D>(at[k].r, g) : k_scale_at<D>(at[k].r, g)] = (unsigned char)scale;
-        }
+        uint32_t scale;
+        const uint2 codes = quantise(x[v], scale, nan);
+        *reinterpret_cast<uint2*>(block + (v ? v_codes_at<D>(r, g) : k_codes_at<D>(r, g))) = codes;
+        block[v ? v_scale_at<D>(r, g) : k_scale_at<D>(r, g)] = (unsigned char)scale;
     }
     if (nan) set_status(P.status, RADAR_ERR_NUMERIC);
 }
@@ -378,20 +407,19 @@ __global__ void __launch_bounds__(256) cache_store_kernel(const StoreParams P) {
 struct LoadParams {
     radar_cache_load_args a;
     int64_t page_bytes;
-    int64_t windows;
+    int64_t warps;                   // of one KV head
     int shift;
     int* status;
 };
 
 __device__ __forceinline__ void store_group(float* p, const uint32_t (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        __stcs(reinterpret_cast<float4*>(p) + i, make_float4(__uint_as_float(v[2 * i] << 16), __uint_as_float(v[2 * i] & 0xffff0000u),
-                                                             __uint_as_float(v[2 * i + 1] << 16), __uint_as_float(v[2 * i + 1] & 0xffff0000u)));
+    for (int i = 0; i < 2; ++i)
+        store_row32(p + 8 * i, make_uint4(v[4 * i] << 16, v[4 * i] & 0xffff0000u, v[4 * i + 1] << 16, v[4 * i + 1] & 0xffff0000u),
+                    make_uint4(v[4 * i + 2] << 16, v[4 * i + 2] & 0xffff0000u, v[4 * i + 3] << 16, v[4 * i + 3] & 0xffff0000u));
 }
 __device__ __forceinline__ void store_group(__nv_bfloat16* p, const uint32_t (&v)[8]) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<uint4*>(p) + 1, make_uint4(v[4], v[5], v[6], v[7]));
+    store_row32(p, make_uint4(v[0], v[1], v[2], v[3]), make_uint4(v[4], v[5], v[6], v[7]));
 }
 __device__ __forceinline__ void decode_group(uint2 w, uint32_t byte, uint32_t (&v)[8]) {
     const uint32_t s = scale_pair(byte | byte << 16), off = offset_pair(s);
@@ -399,68 +427,43 @@ __device__ __forceinline__ void decode_group(uint2 w, uint32_t byte, uint32_t (&
     v[4] = decode<0>(w.y, s, off); v[5] = decode<1>(w.y, s, off); v[6] = decode<2>(w.y, s, off); v[7] = decode<3>(w.y, s, off);
 }
 
-template <typename T, int D, int PASSES>
+// What bounds it: memory (the sizes above: bf16 55 us, 6.2 TB/s; fp32 95 us, 6.4 TB/s).
+template <typename T, int D>
 __global__ void __launch_bounds__(256) cache_load_kernel(const LoadParams P) {
     chain_wait();
-    using W = Window<D>;
+    using L = Lanes<D>;
     const radar_cache_load_args& a = P.a;
-    const int lane = threadIdx.x & 31, g = lane % W::kGroups, side = lane / W::kGroups, l = blockIdx.y;
-    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), window = item / a.Hkv;
-    if (window >= P.windows) return;
-    const int h = (int)(item - window * a.Hkv);
-    W mine;
-    mine.block = -1; mine.row = 0; mine.r = 0;
-    const int64_t i = window * (W::kSide * PASSES) + lane;
-    if (lane < W::kSide * PASSES) {
-        const int n = a.start[a.B];
-        if (i < n && i >= a.n_rows) set_status(P.status, RADAR_ERR_INVALID_ARG);
-        if (i < n && i < a.n_rows) {
-            const int b = owner(a.start, a.B, (int)i);
-            const int64_t at = (int64_t)a.first[b] + (i - a.start[b]);
-            const int index = P.shift >= 0 ? (int)(at >> P.shift) : (int)(at / a.page_size);
-            const bool in_table = at >= 0 && at < (int64_t)a.max_pages * a.page_size;
-            const int page = in_table ? a.block_table[(int64_t)b * a.max_pages + index] : -1;
-            if (page < 0 || page >= a.n_pages) {
-                set_status(P.status, RADAR_ERR_INVALID_ARG);
-            } else {
-                const int in_page = (int)(at - (int64_t)index * a.page_size);
-                mine.block = page * P.page_bytes + ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
-                mine.r = in_page & 15;
-                mine.row = (int)i;
-            }
-        }
+    const int lane = threadIdx.x & 31, g = lane % L::kGroups, l = blockIdx.y;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), warp = item / a.Hkv;
+    if (warp >= P.warps) return;
+    const int h = (int)(item - warp * a.Hkv);
+    const int64_t i = warp * L::kTokens + lane / L::kGroups;
+    const int n = a.start[a.B];
+    if (i >= n) return;
+    if (i >= a.n_rows) {
+        set_status(P.status, RADAR_ERR_INVALID_ARG);
+        return;
     }
-    W at[PASSES];
-    const unsigned char* pool = reinterpret_cast<const unsigned char*>(a.pages) + l * a.page_layer_stride;
-    uint2 codes[2][PASSES];
-    uint32_t scale[2][PASSES];
-#pragma unroll
-    for (int k = 0; k < PASSES; ++k) {
-        at[k] = mine.of(side + k * W::kSide);
-        if (at[k].block < 0) continue;
-        const unsigned char* block = pool + at[k].block;
-        const int r = at[k].r;
-        codes[0][k] = *reinterpret_cast<const uint2*>(block + k_codes_at<D>(r, g));
-        codes[1][k] = *reinterpret_cast<const uint2*>(block + v_codes_at<D>(r, g));
-        scale[0][k] = block[k_scale_at<D>(r, g)];
-        scale[1][k] = block[v_scale_at<D>(r, g)];
+    const int b = owner(a.start, a.B, (int)i);
+    const int64_t at = (int64_t)a.first[b] + (i - a.start[b]);
+    const int index = P.shift >= 0 ? (int)(at >> P.shift) : (int)(at / a.page_size);
+    const bool in_table = at >= 0 && at < (int64_t)a.max_pages * a.page_size;
+    const int page = in_table ? a.block_table[(int64_t)b * a.max_pages + index] : -1;
+    if (page < 0 || page >= a.n_pages) {
+        set_status(P.status, RADAR_ERR_INVALID_ARG);
+        return;
     }
-#pragma unroll
-    for (int k = 0; k < PASSES; ++k) {
-        if (at[k].block < 0) continue;
-        const int64_t to = l * a.row_layer_stride + ((int64_t)at[k].row * a.Hkv + h) * D + g * 16;
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            uint32_t out[8];
-            decode_group(codes[v][k], scale[v][k], out);
-            store_group(reinterpret_cast<T*>(v ? a.V : a.K) + to, out);
-        }
-    }
-}
-
-// Passes of a warp: all 16 tokens of its window where that leaves every SM warps enough, one where there are few tokens.
-int window_passes(const radar_ctx* ctx, int64_t tokens, int Hkv, int d, int layers) {
-    return tokens * Hkv * layers >= (int64_t)ctx->sm_count * 16 * 32 ? 16 / (32 / (d / 16)) : 1;
+    const int in_page = (int)(at - (int64_t)index * a.page_size), r = in_page & 15;
+    const unsigned char* block = reinterpret_cast<const unsigned char*>(a.pages) + l * a.page_layer_stride + page * P.page_bytes +
+                                 ((int64_t)h * (a.page_size / kBlock) + (in_page >> 4)) * Layout<D>::kBytes;
+    const uint2 k = *reinterpret_cast<const uint2*>(block + k_codes_at<D>(r, g)), v = *reinterpret_cast<const uint2*>(block + v_codes_at<D>(r, g));
+    const uint32_t k_scale = block[k_scale_at<D>(r, g)], v_scale = block[v_scale_at<D>(r, g)];
+    const int64_t to = l * a.row_layer_stride + (i * a.Hkv + h) * D + g * 16;
+    uint32_t out[8];
+    decode_group(k, k_scale, out);
+    store_group(reinterpret_cast<T*>(a.K) + to, out);
+    decode_group(v, v_scale, out);
+    store_group(reinterpret_cast<T*>(a.V) + to, out);
 }
 
 int log2_of(int x) {
@@ -541,15 +544,14 @@ extern "C" int radar_cache_store(radar_ctx* ctx, const radar_cache_store_args* a
     P.page_bytes = page_bytes(a->Hkv, a->d, a->page_size);
     P.shift = log2_of(a->page_size);
     P.status = ctx->d_status;
-    const int passes = window_passes(ctx, a->n_tokens, a->Hkv, a->d, a->n_layers), tokens = 32 / (a->d / 16) * passes;
-    P.windows = (a->n_tokens + tokens - 1) / tokens;
-    const int64_t blocks = (P.windows * a->Hkv + 7) / 8;
+    const int tokens = 32 / (a->d / 16);
+    P.warps = (a->n_tokens + tokens - 1) / tokens;
+    const int64_t blocks = (P.warps * a->Hkv + 7) / 8;
     if (blocks > INT32_MAX || a->n_rows > INT32_MAX) return RADAR_ERR_UNSUPPORTED;
     return by_type(a->dtype, a->d, [&](auto t, auto d) -> int {
         constexpr int D = decltype(d)::value;
         radar_launch_scope scope(ctx, RADAR_K_CACHE_STORE, stream);
-        auto* const kernel = passes > 1 ? cache_store_kernel<decltype(t), D, D / 32> : cache_store_kernel<decltype(t), D, 1>;
-        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
+        RADAR_CUDA_CHECK(launch_chained(cache_store_kernel<decltype(t), D>, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
         return RADAR_OK;
     });
 }
@@ -571,15 +573,14 @@ extern "C" int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* a, 
     P.page_bytes = page_bytes(a->Hkv, a->d, a->page_size);
     P.shift = log2_of(a->page_size);
     P.status = ctx->d_status;
-    const int passes = window_passes(ctx, a->n_rows, a->Hkv, a->d, a->n_layers), tokens = 32 / (a->d / 16) * passes;
-    P.windows = (a->n_rows + 1 + tokens - 1) / tokens;           // (one token more: it sees rows that do not fit)
-    const int64_t blocks = (P.windows * a->Hkv + 7) / 8;
+    const int tokens = 32 / (a->d / 16);
+    P.warps = (a->n_rows + 1 + tokens - 1) / tokens;             // (one token more: it sees rows that do not fit)
+    const int64_t blocks = (P.warps * a->Hkv + 7) / 8;
     if (blocks > INT32_MAX) return RADAR_ERR_UNSUPPORTED;
     return by_type(a->dtype, a->d, [&](auto t, auto d) -> int {
         constexpr int D = decltype(d)::value;
         radar_launch_scope scope(ctx, RADAR_K_CACHE_LOAD, stream);
-        auto* const kernel = passes > 1 ? cache_load_kernel<decltype(t), D, D / 32> : cache_load_kernel<decltype(t), D, 1>;
-        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
+        RADAR_CUDA_CHECK(launch_chained(cache_load_kernel<decltype(t), D>, dim3((unsigned)blocks, (unsigned)a->n_layers), dim3(256), 0, stream, P));
         return RADAR_OK;
     });
 }
