@@ -14,14 +14,22 @@ using namespace cache4;
 // block works them out for itself in shared memory, and the blocks then share out pages and slots, each of which looks up its
 // request in the sums.  The stack as it is after the returns is never read back: an index at or beyond the old count is the
 // returned page of some request, looked up in its table.  So no block waits for another one.  What may overwrite the inputs
-// (lengths, free count) is written behind all reads: by the only block, or by a second kernel.
+// (lengths, free count) is written behind all reads: by the only block, or by a second kernel where there are several.
+// What bounds it is the chain of loads, sums, searches and loads behind one another, not their number: 3.0 us for one request, 3.6 for 32
+// that grow by 1 to 9 tokens, 10.1 for 512 admitted with 17 to 4096 tokens (a million slots; a launch that does nothing takes
+// 2.2).  The three sums run side by side in 32 bits and each value is loaded once; with three sums of 64 bits behind one another, and four
+// consecutive slots a thread, it was 5.7, 7.7 and 14.6 us.
 constexpr int kExtendThreads = 1024;
 constexpr int kMaxRequests = 8192;
-constexpr int kSlotsPerThread = 4;
+// A warp takes 32 consecutive slots, or this many times 32 where every warp of the grid has some: it then looks up the first and
+// the last one's request, and the others' between them.
+constexpr int kSlotRuns = 4;
+constexpr int kAloneSlots = 4096;        // that one block takes where a second kernel (2.2 us) would have to follow several
 
 struct ExtendParams {
     radar_cache_extend_args a;
     int shift;                       // log2(page_size), -1: no power of two
+    bool lengths_here;               // the first block writes lengths and free count
     int* status;
 };
 
@@ -41,72 +49,94 @@ __device__ __forceinline__ Request request(const ExtendParams& P, int b) {
     return r;
 }
 
-// exclusive sum of v over the block's threads, and the total
-__device__ __forceinline__ long long block_scan(long long v, long long* s_warp, long long& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(kFull, incl, o);
-        if (lane >= o) incl += u;
-    }
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
-    const long long w = s_warp[lane];                                 // 32 warps
-    long long wi = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(kFull, wi, o);
-        if (lane >= o) wi += u;
-    }
-    total = __shfl_sync(kFull, wi, 31);
-    const long long before = __shfl_sync(kFull, wi - w, warp);
-    __syncthreads();
-    return before + incl - v;
-}
-// Sums are held up to here: behind the largest slot, and more pages than a stack can have.
-__device__ __forceinline__ int clip(long long x) { return (int)min(x, (long long)INT32_MAX); }
+// Sums end here: behind the largest slot, and more pages than a stack can have.
+__device__ __forceinline__ int add_clipped(int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)INT32_MAX); }
 
-// the request whose share of the running sum holds i: the last b with sum[b] <= i
-__device__ __forceinline__ int owner(const int* sum, int B, int i) {
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (sum[mid] <= i) lo = mid; else hi = mid;
+// what a request adds to the three sums
+struct Sums {
+    int v[3];                            // tokens, pages lacked, pages given up
+    __device__ __forceinline__ explicit Sums(const Request& r) : v{max(r.n, 0), max(r.want - r.have, 0), max(r.have - r.want, 0)} {}
+};
+
+// Exclusive sums over the block's threads, behind `carry`, which the block's own are added to.
+__device__ __forceinline__ void block_scan(Sums& x, int (&carry)[3], int (*s_warp)[32]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    int incl[3] = {x.v[0], x.v[1], x.v[2]};
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int u = __shfl_up_sync(kFull, incl[k], o);
+            if (lane >= o) incl[k] = add_clipped(incl[k], u);
+        }
+    int before[3] = {0, 0, 0}, all[3];
+    if (warps == 1) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) all[k] = __shfl_sync(kFull, incl[k], 31);
+    } else {
+        if (lane == 31)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) s_warp[k][warp] = incl[k];
+        __syncthreads();
+        int w[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[k] = lane < warps ? s_warp[k][lane] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const int u = __shfl_up_sync(kFull, w[k], o);
+                if (lane >= o) w[k] = add_clipped(w[k], u);
+            }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            all[k] = __shfl_sync(kFull, w[k], 31);
+            before[k] = __shfl_sync(kFull, w[k], (warp - 1) & 31);
+            if (warp == 0) before[k] = 0;
+        }
+        __syncthreads();
     }
-    return lo;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const int u = __shfl_up_sync(kFull, incl[k], 1);
+        x.v[k] = add_clipped(carry[k], add_clipped(before[k], lane > 0 ? u : 0));
+        carry[k] = add_clipped(carry[k], all[k]);
+    }
 }
 
-template <bool ALONE>
+// the request whose share of the running sum holds i: the last one of b0 .. b1 - 1 with sum[b] <= i
+__device__ __forceinline__ int owner(const int* sum, int b0, int b1, int i) {
+    while (b1 - b0 > 1) {
+        const int mid = (b0 + b1) >> 1;
+        if (sum[mid] <= i) b0 = mid; else b1 = mid;
+    }
+    return b0;
+}
+
+template <int RUNS>
 __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const ExtendParams P) {
     chain_wait();
     extern __shared__ int s_sums[];                                  // three times B + 1
-    __shared__ long long s_warp[32];
+    __shared__ int s_warp[3][32];
     const radar_cache_extend_args& a = P.a;
-    const int B = a.B, tid = threadIdx.x;
+    const int B = a.B, tid = threadIdx.x, threads = blockDim.x;
     int *s_tok = s_sums, *s_grow = s_tok + B + 1, *s_back = s_grow + B + 1;
     const bool first = blockIdx.x == 0;
-
-    // a thread's consecutive requests
-    const int per = (B + kExtendThreads - 1) / kExtendThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
-    long long tok = 0, grow = 0, back = 0, tok_sum, grow_sum, back_sum;
-    for (int b = b0; b < b1; ++b) {
-        const Request r = request(P, b);
-        if (!r.ok && first) set_status(P.status, RADAR_ERR_INVALID_ARG);
-        tok += max(r.n, 0); grow += max(r.want - r.have, 0); back += max(r.have - r.want, 0);
-    }
-    tok = block_scan(tok, s_warp, tok_sum);
-    grow = block_scan(grow, s_warp, grow_sum);
-    back = block_scan(back, s_warp, back_sum);
-    for (int b = b0; b < b1; ++b) {
-        const Request r = request(P, b);
-        s_tok[b] = clip(tok); s_grow[b] = clip(grow); s_back[b] = clip(back);
-        tok += max(r.n, 0); grow += max(r.want - r.have, 0); back += max(r.have - r.want, 0);
-    }
-    const int tok_all = clip(tok_sum), grow_all = clip(grow_sum);
-    int back_all = clip(back_sum);
-    if (tid == 0) { s_tok[B] = tok_all; s_grow[B] = grow_all; s_back[B] = back_all; }
     int n0 = *a.free_count;
+
+    int sum[3] = {0, 0, 0};
+    for (int b0 = 0; b0 < B; b0 += threads) {
+        const int b = b0 + tid;
+        Request r = {0, 0, 0, 0, true};
+        if (b < B) r = request(P, b);
+        if (!r.ok && first) set_status(P.status, RADAR_ERR_INVALID_ARG);
+        Sums x(r);
+        block_scan(x, sum, s_warp);
+        if (b < B) { s_tok[b] = x.v[0]; s_grow[b] = x.v[1]; s_back[b] = x.v[2]; }
+    }
+    const int tok_all = sum[0], grow_all = sum[1];
+    int back_all = sum[2];
+    if (tid == 0) { s_tok[B] = tok_all; s_grow[B] = grow_all; s_back[B] = back_all; }
     if (n0 < 0 || n0 > a.free_capacity) {
         if (first && tid == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
         n0 = max(0, min(n0, a.free_capacity));
@@ -119,7 +149,7 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
     __syncthreads();
 
     auto given_up = [&](int i) {                                       // the i-th page that comes back
-        const int b = owner(s_back, B, i);
+        const int b = owner(s_back, 0, B, i);
         return a.block_table[(int64_t)b * a.max_pages + request(P, b).want + i - s_back[b]];
     };
     auto taken = [&](int i) {                                          // the i-th page from the top
@@ -127,97 +157,89 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
         return at < n0 ? a.free_pages[at] : given_up(at - n0);
     };
     auto granted = [&](int b, const Request& r) { return r.want <= r.have || s_grow[b + 1] <= n1; };
-    const int step = gridDim.x * kExtendThreads, me = blockIdx.x * kExtendThreads + tid;
     // tokens of ungranted requests still count in `start`; slots beyond the capacity are not written
-    if (first) {
-        for (int b = tid; b <= B; b += kExtendThreads) {
-            a.start[b] = s_tok[b];
-            if (b < B) {
-                const Request r = request(P, b);
-                a.granted[b] = r.ok && granted(b, r);
-            }
+    const int64_t tokens = min((int64_t)tok_all, a.slot_capacity);
+    const int lane = tid & 31, warps = threads >> 5;
+    constexpr int kRun = 32 * RUNS;
+    for (int64_t i0 = ((int64_t)blockIdx.x * warps + (tid >> 5)) * kRun; i0 < tokens; i0 += (int64_t)gridDim.x * warps * kRun) {
+        int lo = 0, hi = B;
+        if (RUNS > 1) {
+            lo = owner(s_tok, 0, B, (int)i0);
+            hi = owner(s_tok, 0, B, (int)min(i0 + kRun, tokens) - 1) + 1;
         }
-        if (tok_all > a.slot_capacity && tid == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
-    }
-    // slots, four consecutive tokens a thread
-    const long long tokens = min((long long)tok_all, (long long)a.slot_capacity);
-    for (long long i0 = (long long)me * kSlotsPerThread; i0 < tokens; i0 += (long long)step * kSlotsPerThread) {
-        int b = -1, end = 0, at = 0, page_at = -1, page = 0, have = 0;
+        int b = -1, end = 0, tok = 0, grow = 0;                        // the request looked up last, if any, and its last slot's successor
+        Request r;
         bool on = false;
-        int64_t out[kSlotsPerThread];
 #pragma unroll
-        for (int k = 0; k < kSlotsPerThread; ++k) {
-            const int i = (int)i0 + k;
-            out[k] = -1;
+        for (int k = 0; k < RUNS; ++k) {
+            const int64_t i = i0 + 32 * k + lane;
             if (i >= tokens) continue;
             if (i >= end) {
-                b = owner(s_tok, B, i);
-                end = s_tok[b + 1];
-                const Request r = request(P, b);
-                at = r.len + i - s_tok[b];
-                have = r.have;
+                b = owner(s_tok, lo, hi, (int)i);
+                tok = s_tok[b]; grow = s_grow[b]; end = s_tok[b + 1];
+                r = request(P, b);
                 on = granted(b, r);
-                page_at = -1;
             }
-            if (on) {
-                const int index = P.shift >= 0 ? at >> P.shift : at / a.page_size;
-                if (index != page_at) {
-                    page_at = index;
-                    page = index < have ? a.block_table[(int64_t)b * a.max_pages + index] : taken(s_grow[b] + index - have);
-                }
-                out[k] = (int64_t)page * a.page_size + (at - index * a.page_size);
-            }
+            const int j = (int)i - tok;
             if (a.path_nodes != nullptr) {
-                const int j = i - s_tok[b], row = j < a.path_stride ? a.path_nodes[(int64_t)b * a.path_stride + j] : -1;
+                const int row = j < a.path_stride ? a.path_nodes[(int64_t)b * a.path_stride + j] : -1;
                 const bool ok = row >= 0 && row < a.rows;
                 if (!ok) set_status(P.status, RADAR_ERR_INVALID_ARG);
                 a.src_row[i] = ok ? b * a.rows + row : -1;
             }
-            ++at;
+            int64_t slot = -1;
+            if (on) {
+                const int at = r.len + j, index = P.shift >= 0 ? at >> P.shift : at / a.page_size;
+                const int page = index < r.have ? a.block_table[(int64_t)b * a.max_pages + index] : taken(grow + index - r.have);
+                slot = (int64_t)page * a.page_size + (at - index * a.page_size);
+            }
+            a.slots[i] = slot;
         }
-#pragma unroll
-        for (int k = 0; k < kSlotsPerThread; ++k)
-            if (i0 + k < tokens) a.slots[i0 + k] = out[k];
     }
     // returned pages onto the stack, new ones into the tables
+    const int step = gridDim.x * threads, me = blockIdx.x * threads + tid;
     for (int i = me; i < back_all; i += step) a.free_pages[n0 + i] = given_up(i);
     for (int i = me; i < grow_all && i < n1; i += step) {
-        const int b = owner(s_grow, B, i);
+        const int b = owner(s_grow, 0, B, i);
         const Request r = request(P, b);
         if (granted(b, r)) a.block_table[(int64_t)b * a.max_pages + r.have + i - s_grow[b]] = taken(i);
     }
-    if (ALONE) {
-        __syncthreads();
-        long long used = 0, all;
-        for (int b = b0; b < b1; ++b) {
-            const Request r = request(P, b);
-            const bool on = granted(b, r);
-            if (on) used += max(r.want - r.have, 0);
-            a.cache_len_out[b] = on ? r.len + r.n : r.len;
-        }
-        block_scan(used, s_warp, all);
-        if (tid == 0) *a.free_count_out = n1 - (int)all;
+    if (!first) return;
+    if (tok_all > a.slot_capacity && tid == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
+    if (P.lengths_here) __syncthreads();
+    for (int b = tid; b <= B; b += threads) {
+        a.start[b] = s_tok[b];
+        // pages go to requests in order as long as there are enough: the largest sum that does not pass n1 is used up
+        if (P.lengths_here && s_grow[b] <= n1 && (b == B || s_grow[b + 1] > n1)) *a.free_count_out = n1 - s_grow[b];
+        if (b == B) break;
+        const Request r = request(P, b);
+        const bool on = granted(b, r);
+        a.granted[b] = r.ok && on;
+        if (P.lengths_here) a.cache_len_out[b] = on ? r.len + r.n : r.len;
     }
 }
 
-// Behind a launch of several blocks: what may overwrite their inputs.
+// Behind a launch of several blocks: what overwrites their inputs.
 __global__ void __launch_bounds__(kExtendThreads) cache_lengths_kernel(const ExtendParams P) {
     chain_wait();
-    __shared__ long long s_warp[32];
+    __shared__ int s_warp[3][32];
     const radar_cache_extend_args& a = P.a;
-    long long used = 0, back = 0, used_all, back_all;
-    for (int b = threadIdx.x; b < a.B; b += kExtendThreads) {
-        const Request r = request(P, b);
-        const bool on = a.granted[b];
-        if (on) used += max(r.want - r.have, 0);
-        back += max(r.have - r.want, 0);
-        a.cache_len_out[b] = on ? r.len + r.n : r.len;
+    int sum[3] = {0, 0, 0};
+    for (int b0 = 0; b0 < a.B; b0 += kExtendThreads) {
+        const int b = b0 + threadIdx.x;
+        Request r = {0, 0, 0, 0, true};
+        if (b < a.B) r = request(P, b);
+        Sums x(r);
+        if (b < a.B) {
+            const bool on = a.granted[b];
+            if (!on) x.v[1] = 0;                                       // (ungranted ones take none)
+            a.cache_len_out[b] = on ? r.len + r.n : r.len;
+        }
+        block_scan(x, sum, s_warp);
     }
-    block_scan(used, s_warp, used_all);
-    block_scan(back, s_warp, back_all);
     if (threadIdx.x == 0) {
         const int n0 = max(0, min(*a.free_count, a.free_capacity));
-        *a.free_count_out = n0 + (int)(min(back_all, (long long)(a.free_capacity - n0)) - used_all);
+        *a.free_count_out = n0 + min(sum[2], a.free_capacity - n0) - sum[1];
     }
 }
 
@@ -444,7 +466,7 @@ __global__ void __launch_bounds__(256) cache_load_kernel(const LoadParams P) {
         set_status(P.status, RADAR_ERR_INVALID_ARG);
         return;
     }
-    const int b = owner(a.start, a.B, (int)i);
+    const int b = owner(a.start, 0, a.B, (int)i);
     const int64_t at = (int64_t)a.first[b] + (i - a.start[b]);
     const int index = P.shift >= 0 ? (int)(at >> P.shift) : (int)(at / a.page_size);
     const bool in_table = at >= 0 && at < (int64_t)a.max_pages * a.page_size;
@@ -508,18 +530,26 @@ extern "C" int radar_cache_extend(radar_ctx* ctx, const radar_cache_extend_args*
     P.shift = log2_of(a->page_size);
     P.status = ctx->d_status;
     const size_t smem = 3 * (size_t)(a->B + 1) * sizeof(int);
-    const int64_t per = kExtendThreads * kSlotsPerThread;
-    const int blocks = (int)std::min<int64_t>(ctx->sm_count, (a->slot_capacity + per - 1) / per);
-    if (blocks <= 1) {
-        RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_EXTEND, cache_extend_kernel<true>, smem));
+    auto overlap = [](const void* p, const void* q, size_t n) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+        return x < y + n && y < x + n;
+    };
+    const size_t lens = (size_t)a->B * sizeof(int32_t);
+    const bool in_place = overlap(a->cache_len, a->cache_len_out, lens) || overlap(a->free_count, a->free_count_out, sizeof(int32_t)) ||
+                          overlap(a->new_len, a->cache_len_out, lens);
+    int64_t blocks = std::min<int64_t>(ctx->sm_count, (a->slot_capacity + kExtendThreads - 1) / kExtendThreads);
+    if (blocks < 1 || (in_place && a->slot_capacity <= kAloneSlots)) blocks = 1;
+    const bool runs = a->slot_capacity >= blocks * kExtendThreads * kSlotRuns;
+    const int64_t work = std::max<int64_t>(a->B, a->slot_capacity);
+    const int threads = blocks > 1 ? kExtendThreads : (int)std::min<int64_t>(kExtendThreads, (work + 31) / 32 * 32);
+    P.lengths_here = blocks == 1 || !in_place;
+    auto* const kernel = runs ? cache_extend_kernel<kSlotRuns> : cache_extend_kernel<1>;
+    RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_EXTEND + runs, kernel, smem));
+    {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_EXTEND, stream);
-        RADAR_CUDA_CHECK(launch_chained(cache_extend_kernel<true>, dim3(1), dim3(kExtendThreads), smem, stream, P));
-    } else {
-        RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_EXTEND + 1, cache_extend_kernel<false>, smem));
-        {
-            radar_launch_scope scope(ctx, RADAR_K_CACHE_EXTEND, stream);
-            RADAR_CUDA_CHECK(launch_chained(cache_extend_kernel<false>, dim3((unsigned)blocks), dim3(kExtendThreads), smem, stream, P));
-        }
+        RADAR_CUDA_CHECK(launch_chained(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), smem, stream, P));
+    }
+    if (!P.lengths_here) {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_LENGTHS, stream);
         RADAR_CUDA_CHECK(launch_chained(cache_lengths_kernel, dim3(1), dim3(kExtendThreads), 0, stream, P));
     }
