@@ -38,11 +38,22 @@ using tc05::mbar_drain;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kStageKeys = 32;       // keys of a stage: two blocks
-constexpr int kUnitCost = 5;         // of a unit beside its stages, in stages
-constexpr int kSmallStages = 4;      // of a warp, at most, in the form for little work
+// Of a unit beside its stages, in stages.  Lengths of 100 to 16384 tokens: 4 sequences, 40 heads, 16 rows 75 us (with 5: 128), 32
+// sequences, 32 / 8 heads, 1 row 81 (88); equal lengths do not depend on it.
+constexpr int kUnitCost = 16;
+// Stages a warp, at most, in the form for little work.  One sequence, 32 / 8 heads, 1 row, 7000 tokens: 12 us (in ranges 18), 9000 tokens
+// 14 (22); 8 rows (two row tiles), 12000 tokens 25 (24), 16384 tokens 32 (27).
+constexpr int kSmallStages = 12;
+// Blocks of a cluster; more than 8 where all clusters have an SM for each block.  One sequence, 32 / 8 heads, 1 row, 16384 tokens: 16 us
+// (with 8: 23), 9000 tokens 13 (14), below that the same; 8 rows, two clusters' blocks an SM, 9000 tokens 29 (20).
+constexpr int kMaxCluster = 16;
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 4 : 2; }
 constexpr float kMove = 8.f;         // log2 units
-constexpr int kTensorRows = 48;      // query rows of a KV head from which on the form of cache_attention_tc.cu takes them
+// Query rows of a KV head up to which this form takes all work; above, only what is little, and cache_attention_tc.cu the rest.  8
+// sequences of 4096 to 16384 tokens, 32 / 8 heads of 128: 16 rows 44 us (there 70), 32 rows 69 (70), 48 rows 96 (72), 64 rows 123 (72); of
+// 2048 tokens: 32 rows 26 us (33), 48 rows 31 (33), 64 rows 37 (33).  Little work: 64 rows over 300 tokens 11 us (20), one
+// sequence of 1000 tokens, 256 rows 14 us (17).
+constexpr int kTokenRows = 32;
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -833,11 +844,11 @@ Plan plan(const radar_ctx* ctx, int B, int Hkv, int G, int rows, int max_len) {
     p.nt = R > 8 ? 2 : 1;
     const int64_t units = (int64_t)B * Hkv * ((R + 8 * p.nt - 1) / (8 * p.nt)), stages = units * ((max_len + kStageKeys - 1) / kStageKeys + 1);
     p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count * blocks_per_sm(p.nt), (stages + kWarps - 1) / kWarps));
-    // A cluster a unit, as large as gives every warp about two stages, where that leaves no more than four stages a warp and the
+    // A cluster a unit, as large as gives every warp about two stages, where that leaves no more than kSmallStages a warp and the
     // blocks fit the SMs together.
     const int unit_stages = (max_len + kStageKeys - 1) / kStageKeys;
     int size = 1;
-    while (size < 8 && unit_stages > 2 * kWarps * size && 2 * size * units <= (int64_t)ctx->sm_count * 2) size *= 2;
+    while (size < kMaxCluster && unit_stages > 2 * kWarps * size && 2 * size * units <= (int64_t)ctx->sm_count * (size < 8 ? 2 : 1)) size *= 2;
     p.cluster = unit_stages <= kSmallStages * kWarps * size && size * units <= (int64_t)ctx->sm_count * 3 ? size : 0;
     return p;
 }
@@ -851,7 +862,9 @@ int launch(radar_ctx* ctx, const CacheAttnParams& P, cudaStream_t stream) {
     if (P.cluster > 0) {
         auto* const kernel = cache_attn_small_kernel<D, NT>;
         constexpr size_t smem = SmallPlan<D, NT>::kDynamic;
-        RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_SMALL + 2 * (D == 128) + NT - 1, kernel, smem));
+        constexpr int slot = RADAR_SMEM_CACHE_SMALL + 2 * (D == 128) + NT - 1;
+        if (ctx->smem_room[slot] == 0) RADAR_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, slot, kernel, smem));
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((int64_t)a.B * a.Hkv * ((a.rows * P.G + 8 * NT - 1) / (8 * NT)) * P.cluster));
         cfg.blockDim = dim3(kThreads);
@@ -911,8 +924,8 @@ extern "C" int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args
     CacheAttnParams P;
     P.a = *a;
     P.G = a->Hq / a->Hkv;
-    if (a->rows * P.G >= kTensorRows) return cache_attn_tc_launch(ctx, a, stream);
     const Plan p = plan(ctx, a->B, a->Hkv, P.G, a->rows, a->max_cache_len);
+    if (a->rows * P.G > kTokenRows && p.cluster == 0) return cache_attn_tc_launch(ctx, a, stream);
     P.blocks = p.blocks;
     P.cluster = p.cluster;
     P.blocks_per_page = a->page_size / kBlock;

@@ -340,3 +340,79 @@ def test_attention_reports_what_is_out_of_range(ctx):
         if rows > 1:
             with pytest.raises(ValueError, match="must follow"):
                 rb.radar_cache_attention(ctx, **dict(kw, Q=torch.zeros(2, 2 * rows, 8, 64, dtype=torch.bfloat16, device="cuda")[:, :rows]))
+
+
+# ---- attention by each of its forms --------------------------------------------------------------------------------------
+# Which form takes a call goes by max_cache_len, not by the lengths, which only the GPU knows: with a bound this far off, clusters take nothing
+# (a warp would have more stages than they take), up to 32 rows go in ranges, and more to the tensor cores.
+FAR = 40000
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d,page,rows", SHAPES)
+@pytest.mark.parametrize("mask", ["tree", None])
+def test_attention_under_a_far_bound(ctx, lens, Hq, Hkv, d, page, rows, mask):
+    import cache_harness as T
+    T.check_attention(ctx, np.random.default_rng(sum(lens) + rows + 5), lens, Hq, Hkv, d, page, rows, mask=mask, fused=mask is None, max_len=FAR)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d,page,rows", [s for s in SHAPES if s[5] > 3])
+def test_ragged_trees_under_a_far_bound(ctx, lens, Hq, Hkv, d, page, rows):
+    import cache_harness as T
+    rng = np.random.default_rng(sum(lens) + rows + 6)
+    n = rng.integers(0, rows + 1, len(lens))
+    n[-1] = rows
+    T.check_attention(ctx, rng, lens, Hq, Hkv, d, page, rows, n_nodes=n, mask="holes", max_len=FAR)
+
+
+@pytest.mark.parametrize("Hq,Hkv,rows", [(8, 8, 33), (8, 8, 32), (32, 8, 8), (32, 8, 9), (56, 8, 5), (40, 8, 64)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_many_short_sequences(ctx, Hq, Hkv, rows, d):
+    """More units than fit clusters; units of one and of two row blocks, and of none, in turn."""
+    import cache_harness as T
+    rng = np.random.default_rng(rows + d)
+    lens, n = rng.integers(0, 150, 60), rng.integers(0, rows + 1, 60)
+    lens[::7], n[::5] = 0, rows
+    T.check_attention(ctx, rng, list(lens), Hq, Hkv, d, 16, rows, n_nodes=n)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d,rows", [([8000], 32, 8, 128, 1), ([7777, 20, 6400], 6, 2, 64, 2), ([9000, 0], 4, 4, 128, 8), ([6200], 32, 2, 64, 16), ([7000], 16, 1, 128, 4)])
+def test_attention_of_long_sequences_by_large_clusters(ctx, lens, Hq, Hkv, d, rows):
+    import cache_harness as T
+    T.check_attention(ctx, np.random.default_rng(lens[0]), lens, Hq, Hkv, d, 64, rows)
+
+
+@pytest.mark.parametrize("rows", [7, 64])
+def test_scores_that_jump_under_a_far_bound(ctx, rows):
+    import cache_harness as T
+    T.check_attention(ctx, np.random.default_rng(13), [1500, 70], 8, 2, 128, 32, rows, gain=30.0, max_len=FAR)
+    T.check_attention(ctx, np.random.default_rng(14), [900], 8, 2, 64, 16, rows, gain=8.0, scale=0.7, want_lse=False, max_len=FAR)
+
+
+@pytest.mark.parametrize("rows", [1, 60])
+def test_pages_beyond_four_gigabytes_under_a_far_bound(ctx, rows):
+    import torch
+    import cache_harness as T
+    T.check_attention(ctx, np.random.default_rng(17), [300, 130], 8, 8, 128, 128, rows, first_page=(1 << 32) // (8 * 8 * 18 * 128) + 5, max_len=FAR, stream=torch.cuda.Stream())
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+def test_a_far_bound_reports_what_is_out_of_range(ctx, rows):
+    import cache_harness as T
+    from paper_2512_14069_b200 import binding as rb
+    kw = T.check_attention(ctx, np.random.default_rng(19), [300, 40], 8, 2, 64, 16, rows, n_nodes=[rows, rows], max_len=FAR)
+    first = kw["O"].clone(), kw["lse"].clone()
+    o, bound = T.held_to[1]
+    good = lambda: bool(np.all(np.abs(kw["O"][1].double().cpu().numpy() - o) <= bound))
+    rb.radar_cache_attention(ctx, **kw)
+    assert (kw["O"] == first[0]).all() and (kw["lse"] == first[1]).all()
+    for name, value in (("cache_len", [FAR + 1, 40]), ("cache_len", [-1, 40]), ("n_nodes", [rows + 1, rows]), ("n_nodes", [-1, rows])):
+        kw["O"].zero_()
+        rb.radar_cache_attention(ctx, **dict(kw, **{name: T.dev(value, torch.int32)}))
+        assert ctx.read_device_status() == -1, name
+        assert float(kw["O"][0].float().abs().max()) == 0.0 and good()
+    for page in (-1, kw["pages"].shape[0]):
+        table = kw["block_table"].clone()
+        table[0, 3] = page
+        rb.radar_cache_attention(ctx, **dict(kw, block_table=table))
+        assert ctx.read_device_status() == -1
+        assert good()
