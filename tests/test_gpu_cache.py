@@ -397,6 +397,7 @@ def test_pages_beyond_four_gigabytes_under_a_far_bound(ctx, rows):
 
 @pytest.mark.parametrize("rows", [1, 64])
 def test_a_far_bound_reports_what_is_out_of_range(ctx, rows):
+    import torch
     import cache_harness as T
     from paper_2512_14069_b200 import binding as rb
     kw = T.check_attention(ctx, np.random.default_rng(19), [300, 40], 8, 2, 64, 16, rows, n_nodes=[rows, rows], max_len=FAR)
