@@ -133,7 +133,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
         uint64_t bar_pv[2];              // ... and their product has run
         uint64_t bar_pready[2];          // ... all of them
-        uint64_t bar_mlfull, bar_mlempty;
+        uint64_t bar_mlfull, bar_mlempty, bar_epilogue;
         uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
         Segment seg[kSegRing];
         float2 ml[2][128];               // per group: (m in log2 units, l) of the rows at the end of a segment
@@ -170,6 +170,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             st.st_next = 1u << 8; st.k_tree = st.v_tree = 0;
             mbar_init(&st.bar_mlfull, 8);
             mbar_init(&st.bar_mlempty, 4);
+            mbar_init(&st.bar_epilogue, 4);
             fence_barrier_init();
         }
     } else if (warp == kMmaWarp) {
@@ -297,6 +298,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             // (in the second half, the first one's product may still be under way)
                             if (half == 1) {
                                 ok = mbar_wait_while(ok, &st.bar_pv[grp], (sc - 1) & 1);
+                                ok = __all_sync(kFull, ok);          // (lanes may leave a wait apart; what follows is for a whole warp)
                                 tc_fence_after_sync();
                             }
 #pragma unroll 1
@@ -349,6 +351,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(half == 0 ? &st.bar_pfirst[grp] : &st.bar_pready[grp]);
+                    __syncwarp();
                 }
             }
 
@@ -371,6 +374,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const bool two = TWO && s.rows > P.rb_rows;
             const bool final_rows = s.n == s.nt;                 // the whole unit
             const int slot = seg == 0 ? 0 : 1;                   // a CTA has at most a cut first and a cut last segment
+            // No warp gives back an accumulator of this segment while another reads it for the one before: behind a unit of two row blocks there
+            // may be a single tile of one, whose second accumulator is given back unread.
+            ok = mbar_wait_while(ok, &st.bar_epilogue, (seg & 1) ^ 1);
             ok = mbar_wait_lazy(ok, &st.bar_mlfull, seg & 1);
             const float2 ml0 = st.ml[0][row], ml1 = st.ml[1][row];
             __syncwarp();
@@ -461,6 +467,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.bar_ofree[blk]);
             }
+            if (lane == 0) mbar_arrive(&st.bar_epilogue);
         };
         const bool values = warp < kKeyWarp;
         const int mine = (warp - kEpilogueWarp) & (kDecoders - 1);
