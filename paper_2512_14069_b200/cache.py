@@ -1,0 +1,73 @@
+"""A 4-bit paged KV cache for the requests of a batch: the pool of all layers, block tables, lengths and the stack of free pages.
+
+`FourBitCache` owns the device buffers and issues the library's calls on the current stream; nothing returns to the host, so that a
+decoding loop over it can be captured in a CUDA graph.  It contains no arithmetic.  A request is a row of the block table:
+
+    cache.admit(new_len, K, V)          # prompts (0 for the other requests) and their rows of all layers
+    step.attention_cached(cache, layer, Q, Kt, Vt)      # or cache.attention for other rows than a step's tree
+    cache.append(step, K, V)            # behind step.accept: the root and the accepted nodes, from the tree's rows
+    cache.release(finished)             # their pages go back onto the stack
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as rb
+
+
+class FourBitCache:
+    def __init__(self, ctx: rb.Context, *, n_layers, B, Hq, Hkv, d, page_size, n_pages, max_len, max_new, rows=rb.RADAR_MAX_NODES, device="cuda:0"):
+        """Pool of n_pages pages of page_size tokens in each layer; requests of up to max_len tokens; max_new: added tokens of all
+        requests in one call; rows: query rows of a sequence, at most."""
+        self.ctx = ctx
+        self.n_layers, self.B, self.Hq, self.Hkv, self.d, self.page_size, self.max_len = n_layers, B, Hq, Hkv, d, page_size, max_len
+        dev, i32 = torch.device(device), torch.int32
+        self.pages = torch.zeros((n_layers, n_pages, rb.radar_cache_page_bytes(Hkv, d, page_size)), dtype=torch.uint8, device=dev)
+        self.block_table = torch.full((B, -(-max_len // page_size)), -1, dtype=i32, device=dev)
+        self.cache_len, self.start = torch.zeros(B, dtype=i32, device=dev), torch.zeros(B + 1, dtype=i32, device=dev)
+        self.granted = torch.zeros(B, dtype=torch.uint8, device=dev)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=dev)           # taken from the top: page 0 first
+        self.free_count = torch.full((1,), n_pages, dtype=i32, device=dev)
+        self.slots, self.src_row = torch.full((max_new,), -1, dtype=torch.int64, device=dev), torch.zeros(max_new, dtype=i32, device=dev)
+        n = rb.radar_cache_attn_workspace_bytes(ctx, B, Hq, Hkv, d, rows, max_len)
+        ws = torch.zeros(n + 255, dtype=torch.uint8, device=dev)
+        off = (-ws.data_ptr()) % 256
+        self.workspace = ws[off:off + n]
+
+    def _extend(self, new_len, extra=0, n=None, path_nodes=None, rows=0):
+        """Slots of the added tokens: n of them, or (n None) as many as there are, the rest of the buffer -1."""
+        slots, src_row = self.slots[:n], self.src_row[:n]
+        if n is None:
+            slots.fill_(-1)
+        rb.radar_cache_extend(self.ctx, page_size=self.page_size, cache_len=self.cache_len, new_len=new_len, extra=extra, block_table=self.block_table,
+                              free_pages=self.free_pages, free_count=self.free_count, slots=slots, start=self.start, granted=self.granted,
+                              path_nodes=path_nodes, rows=rows, src_row=None if path_nodes is None else src_row)
+        return slots, None if path_nodes is None else src_row
+
+    def admit(self, new_len, K, V):
+        """New tokens of the requests: new_len [B] int32 on the GPU, K and V [layers, sum of new_len, Hkv, d], the requests' rows one
+        behind the other.  Requests that the pool had no pages for are left as they are; `granted` says which."""
+        if K.shape[1] > self.slots.numel():
+            raise ValueError(f"{K.shape[1]} tokens, the cache was made for {self.slots.numel()} in a call")
+        slots, _ = self._extend(new_len, n=K.shape[1])
+        rb.radar_cache_store(self.ctx, K=K, V=V, slots=slots, pages=self.pages, page_size=self.page_size)
+
+    def append(self, step, K, V):
+        """What a step accepted: the root and step.path_nodes, from the tree's rows of all layers, [layers, B, rows, Hkv, d]."""
+        rows = K.shape[2]
+        slots, src_row = self._extend(step.accept_len, extra=1, path_nodes=step.path_nodes, rows=rows)
+        rb.radar_cache_store(self.ctx, K=K.flatten(1, 2), V=V.flatten(1, 2), slots=slots, src_row=src_row, pages=self.pages, page_size=self.page_size)
+
+    def release(self, finished):
+        """Gives up the tokens of the requests with finished[b] != 0 ([B] on the GPU)."""
+        self._extend(torch.where(finished != 0, -self.cache_len, 0).to(torch.int32))
+
+    def attention(self, layer, Q, Kt, Vt, O, lse=None, mask=None, n_nodes=None, scale=0.0):
+        """radar_cache_attention over one layer's pool: Q [B, rows, Hq, d], Kt and Vt [B, rows, Hkv, d], the rows' own keys and values."""
+        rb.radar_cache_attention(self.ctx, Q=Q, Kt=Kt, Vt=Vt, pages=self.pages[layer], page_size=self.page_size, block_table=self.block_table,
+                                 cache_len=self.cache_len, max_cache_len=self.max_len, O=O, lse=lse, mask=mask, n_nodes=n_nodes,
+                                 workspace=self.workspace, scale=scale)
+
+    def load(self, first, start, K, V):
+        """Tokens first[b] .. of each request as rows start[b] .. start[b + 1] - 1 of K and V, [layers, rows, Hkv, d]."""
+        rb.radar_cache_load(self.ctx, pages=self.pages, page_size=self.page_size, block_table=self.block_table, first=first, start=start, K=K, V=V)
