@@ -127,7 +127,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     // swizzled tiles need a 1024-byte boundary and there is no room left for alignment slack.
     struct __align__(1024) Static {
         uint64_t bar_qfull, bar_qempty, bar_kfull[RK], bar_kempty[RK], bar_vfull[RV], bar_vempty[RV];
-        uint64_t bar_stfull[RS], bar_stempty[RS];      // stages: the cache's bytes as they lie there, keys and values in turn
+        // stages: the cache's bytes as they lie there, keys and values in turn.  Whoever waits for a phase must have seen the one before it
+        // complete, or takes the one before that for it: a slot has a barrier for what it holds as keys and one for values.
+        uint64_t bar_stfull[2][RS], bar_stempty[RS];
         uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2];
         uint64_t bar_idle;               // every product issued has run
         uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
@@ -137,7 +139,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
         Segment seg[kSegRing];
         float2 ml[2][128];               // per group: (m in log2 units, l) of the rows at the end of a segment
-        uint32_t q_last, st_next, k_tree, v_tree;   // phase parity of the last Q, slot and parity of the next stage, the last tree tiles
+        uint32_t q_last, st_armed[2], k_tree, v_tree;   // phase parity of the last Q, parities of the stages' next phases (a bit a slot), the last tree tiles
         uint32_t tmem_base;
         int abort;
     };
@@ -159,7 +161,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             mbar_init(&st.bar_qempty, 1);
             for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], kDecoders); mbar_init(&st.bar_kempty[i], 1); }
             for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecoders); mbar_init(&st.bar_vempty[i], 1); }
-            for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[i], 1); mbar_init(&st.bar_stempty[i], kDecoders); }
+            for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[0][i], 1); mbar_init(&st.bar_stfull[1][i], 1); mbar_init(&st.bar_stempty[i], kDecoders); }
             for (int i = 0; i < 2; ++i) {
                 mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pv[i], 1); mbar_init(&st.bar_pready[i], 4);
                 mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
@@ -167,7 +169,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
             mbar_init(&st.bar_idle, 1);
             st.q_last = 1;
-            st.st_next = 1u << 8; st.k_tree = st.v_tree = 0;
+            st.st_armed[0] = st.st_armed[1] = st.k_tree = st.v_tree = 0;
             mbar_init(&st.bar_mlfull, 8);
             mbar_init(&st.bar_mlempty, 4);
             mbar_init(&st.bar_epilogue, 4);
@@ -479,6 +481,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         Ring<RV> out(1);
         Ring<RS> in(0);
         if (values) in.next();
+        uint32_t stage_par = 0;              // phase parities of this kind's stages, a bit a slot
         Segment s, done;
         done.n = 0;
         uint32_t seg = 0;
@@ -492,7 +495,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     tree_tile(to, values ? &tmVt : &tmKt, &tiles_full[out.slot], s, mine == 0, values ? st.v_tree : st.k_tree, out.slot | (out.par ^ 1) << 8);
                 } else {
                     const int blocks = min((s.Pb - t * kTileKeys + kBlock - 1) / kBlock, kTileBlocks);
-                    ok = mbar_wait_while(ok, &st.bar_stfull[in.slot], in.par);
+                    ok = mbar_wait_while(ok, &st.bar_stfull[values][in.slot], stage_par >> in.slot & 1);
+                    stage_par ^= 1u << in.slot;
                     const uint32_t at = smem_addr(to);
                     const unsigned char* from = sS + in.slot * SM::kStageBytes;
 #pragma unroll 1
@@ -527,6 +531,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             cut.unit.valid = 0;
             cut.tot = tot_all;
             Ring<RS> out(1);
+            uint32_t armed[2] = {0, 0};
             const int per = min(P.blocks_per_page, kTileBlocks);         // blocks of a piece
             // Where the pieces are: lane l looks up piece l of a window of 32, the window after next at a time (a lookup is a trip to L2,
             // and one on the way of every stage was what bounded the kernel).
@@ -578,9 +583,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             ok = mbar_wait_while(ok, &st.bar_stempty[out.slot], out.par);
                             ok = __all_sync(kFull, ok);
                             if (!ok) break;                              // (the ring's position stays that of the last load)
-                            if (lead) mbar_arrive_expect_tx(&st.bar_stfull[out.slot], pieces * per * SM::kPartBytes);
+                            if (lead) mbar_arrive_expect_tx(&st.bar_stfull[v][out.slot], pieces * per * SM::kPartBytes);
                             __syncwarp();
-                            if (lane < pieces) tma_load_3d(sS + out.slot * SM::kStageBytes + lane * per * pitch, &tmCache, &st.bar_stfull[out.slot], 0, v, at);
+                            if (lane < pieces) tma_load_3d(sS + out.slot * SM::kStageBytes + lane * per * pitch, &tmCache, &st.bar_stfull[v][out.slot], 0, v, at);
+                            armed[v] ^= 1u << out.slot;
                             out.next();
                         }
                     }
@@ -606,7 +612,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             }
             __syncwarp();
             write_cut_unit(P, ci, cut);
-            if (lead) st.st_next = out.slot | out.par << 8;
+            if (lead) { st.st_armed[0] = armed[0]; st.st_armed[1] = armed[1]; }
             __syncwarp();
         } else if (warp == kMmaWarp) {
             // =================================== MMA issuer ===================================
@@ -784,7 +790,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             // No load may land in shared memory that the CTA has left.  (Without an abort the roles have waited for every
             // one.)
             mbar_drain(&st.bar_qfull, st.q_last);
-            for (int i = 0; i < RS; ++i) mbar_drain(&st.bar_stfull[i], last_armed_parity(i, st.st_next & 255, st.st_next >> 8));
+            for (int i = 0; i < 2 * RS; ++i) mbar_drain(&st.bar_stfull[i % 2][i / 2], ~(st.st_armed[i % 2] >> i / 2) & 1);     // (one that never was is open)
             if (st.k_tree >> 16) mbar_drain(&st.bar_kfull[st.k_tree & 255], st.k_tree >> 8 & 1);
             if (st.v_tree >> 16) mbar_drain(&st.bar_vfull[st.v_tree & 255], st.v_tree >> 8 & 1);
             set_status(P.status, RADAR_ERR_TIMEOUT);
