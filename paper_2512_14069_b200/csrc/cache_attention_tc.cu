@@ -29,6 +29,10 @@ using namespace cache4;
 
 constexpr int kTcThreads = 576;      // 18 warps are allocated as 20: 96 registers a thread
 constexpr int kEpilogueWarp = 8, kKeyWarp = 12, kProducerWarp = 16, kMmaWarp = 17, kDecoders = 4;    // decoders of either kind
+// What a tile of one and of two row blocks and a unit beside its tiles cost here (decoding takes as long for one row block as for two).
+// us, with these and with those of the kernel over bf16 rows (2, 4, 12): 32 sequences of 16384 tokens, 32 / 8 heads, 64 and 32 rows in turn
+// 500 (515), ragged trees of 9 to 64 rows, 4096 to 32768 tokens 587 (614); 4 sequences, 40 heads, 1001 to 4096 tokens 61 (63).
+constexpr TileCosts kCosts = {5, 9, 24};
 constexpr int kStaticSmem = 3072;
 constexpr int kTileBlocks = kTileKeys / kBlock;
 static_assert(kTileBlocks == 2 * kDecoders, "two blocks of a tile a decoder");
@@ -870,8 +874,7 @@ int cache_attn_tc_launch(radar_ctx* ctx, const radar_cache_attn_args* c, cudaStr
     bool whole;
     plan_grid(ctx, c->B, c->Hq, c->Hkv, c->max_cache_len, 1, &P.n_blk, &P.n_cls, &P.ncc, &whole, c->rows);
     P.pair_rows = P.n_blk * P.rb_rows;
-    const TileCosts tc = tile_costs(P.n_cls);
-    P.cost_one = tc.one; P.cost_two = tc.two; P.unit_cost = whole ? 0 : tc.unit;
+    P.cost_one = kCosts.one; P.cost_two = kCosts.two; P.unit_cost = whole ? 0 : kCosts.unit;
     const size_t grid = (size_t)P.n_cls * P.ncc;
     if (tc_partial_bytes(grid, c->d) > c->workspace_bytes) return RADAR_ERR_WORKSPACE;
     const size_t rec = grid * 2 * kPairRows;
