@@ -21,9 +21,9 @@
 // combine kernel from partial records, two at most a block.  Where there is little to do in all, finding shares and joining them
 // is what takes the time: there a cluster of blocks takes a unit, and joins its shares through its shared memories.
 // What bounds it, long caches: decoding, on the integer pipe (seven of its instructions for eight values; it works 63 % of the time, an
-// instruction is issued in 58 % of the cycles).  32 sequences of 4096 to 32768 tokens, 32 / 8 heads, one row: 165 us, 4.1 TB/s of the
-// cache's 680 MB.  Two stages a warp, four blocks an SM: three stages or five blocks (96 registers) took 2 to 8 % longer, shifts by the
-// multiplier 10 %.
+// instruction is issued in 58 % of the cycles).  32 sequences of 4096 to 32768 tokens, 32 / 8 heads, one row: 160 us, 4.2 TB/s of the
+// cache's 680 MB.  Two stages a warp and four blocks an SM; three stages 175 us, five blocks (96 registers, spilled) 216, three blocks 160;
+// shifts by the multiplier were slower too.
 #include <algorithm>
 #include <cmath>
 

@@ -12,7 +12,7 @@
 //   warp 17          issues the products
 // What bounds the kernel is the chain of a tile: S, the softmax (a warp's 500 instructions, one in about five cycles beside the others'), P V, one
 // behind the other in each group, while the other group is in another part of it.  8 sequences of 8192 tokens, 64 / 8 heads, 64 rows: 184 us of
-// which the tensor pipe works 42 %, an instruction is issued in 39 % of the cycles; the same over bf16 rows takes 154 us.
+// which the tensor pipe works 42 %, an instruction is issued in 39 % of the cycles; the same over bf16 rows takes 152 us.
 // The decoding (twelve instructions for eight values) fits beside it: 32 rows of 32 / 8 heads take 103 us here and 106 there.  A thread takes its
 // row's scores 64 at a time and waits for each load at once, which makes room for eight decoders at 96 registers; keys and
 // values are decoded by the same small loop.
