@@ -282,77 +282,75 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             }
                             tmem_wait_st();
                         }
-                        tmem_ld32(tH, va);
-                        tmem_ld32(tH + 32, vb);
-                        tmem_wait_ld();
-                        float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {                       // three-input maxima: half the instructions
-                            mx0 = max3(mx0, __uint_as_float(va[e]), __uint_as_float(va[e + 1]));
-                            mx1 = max3(mx1, __uint_as_float(vb[e]), __uint_as_float(vb[e + 1]));
-                        }
-                        // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
-                        const float m_half = fmaxf(mx0, mx1) * P.scale_log2;
-                        const bool first = j == 0 && half == 0;
-                        float factor = 1.f;
-                        if (first) {
-                            m_run = m_half;
-                        } else if (m_half > m_run + kRescaleThreshold) {
-                            factor = ex2(m_run - m_half);           // m_run may be -inf: factor 0 clears O and l
-                            m_run = m_half;
-                        }
-                        if (!first && __any_sync(kFull, factor != 1.f)) {
-                            // (in the second half, the first one's product may still be under way)
-                            if (half == 1) {
-                                ok = mbar_wait_while(ok, &st.bar_pv[grp], (sc - 1) & 1);
-                                ok = __all_sync(kFull, ok);          // (lanes may leave a wait apart; what follows is for a whole warp)
-                                tc_fence_after_sync();
-                            }
+                        // ---- P = exp2(s * scale - m) against the maximum so far, and the half's own maximum beside it; once more where a row's
+                        // exceeds the reference by 2^8 (nearly never behind the first tile), behind a rescaling of the accumulator ----
+                        // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values.  The warp issues in
+                        // order and an exponential takes its unit 8 cycles: what else there is to do stands between two of them.)
+                        float2 ls[2];
+                        uint32_t pa[16], pb[16];
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 16) {
-                                uint32_t o[16];
-                                tmem_ld16(tO + c, o);
-                                tmem_wait_ld();
+                        for (;;) {
+                            tmem_ld32(tH, va);
+                            tmem_ld32(tH + 32, vb);
+                            tmem_wait_ld();
+                            const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
+                            const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
+                            float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+                            ls[0] = ls[1] = make_float2(0.f, 0.f);
+                            auto exponentials = [&](uint32_t (&v)[32], uint32_t (&pk)[16]) {
+                                auto scale = [&](const int p) {
+                                    float& mx = p & 1 ? mx1 : mx0;
+                                    mx = max3(mx, __uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1]));
+                                    const float2 t2 = fma2_in_order(make_float2(__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])), sc2, nm2);
+                                    v[2 * p] = __float_as_uint(t2.x);
+                                    v[2 * p + 1] = __float_as_uint(t2.y);
+                                };
+                                auto finish = [&](const int p) {
+                                    const float p0 = __uint_as_float(v[2 * p]), p1 = __uint_as_float(v[2 * p + 1]);
+                                    ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
+                                    pk[p] = bf16x2_in_order(p0, p1);
+                                };
+                                // pairs that the scaling is ahead, and that the rest is behind
+                                constexpr int kAhead = 2, kLag = 3;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                                tmem_st16(tO + c, o);
+                                for (int p = 0; p < kAhead; ++p) scale(p);
+#pragma unroll
+                                for (int p = 0; p < 16 + kLag; ++p) {
+                                    if (p < 16) v[2 * p] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p])));
+                                    if (p + kAhead < 16) scale(p + kAhead);
+                                    if (p < 16) v[2 * p + 1] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p + 1])));
+                                    if (p >= kLag) finish(p - kLag);
+                                }
+                            };
+                            exponentials(va, pa);
+                            exponentials(vb, pb);
+                            const float m_half = fmaxf(mx0, mx1) * P.scale_log2;
+                            const bool move = m_half > m_run + kRescaleThreshold;       // (m_run may be -inf)
+                            if (!__any_sync(kFull, move)) break;
+                            const float factor = move ? ex2(m_run - m_half) : 1.f;       // 0 clears O and l
+                            if (move) m_run = m_half;
+                            l_run *= factor;
+                            if (j > 0 || half > 0) {
+                                // (in the second half, the first one's product may still be under way)
+                                if (half == 1) {
+                                    ok = mbar_wait_while(ok, &st.bar_pv[grp], (sc - 1) & 1);
+                                    ok = __all_sync(kFull, ok);          // (lanes may leave a wait apart; what follows is for a whole warp)
+                                    tc_fence_after_sync();
+                                }
+#pragma unroll 1
+                                for (int c = 0; c < D; c += 16) {
+                                    uint32_t o[16];
+                                    tmem_ld16(tO + c, o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                                    tmem_st16(tO + c, o);
+                                }
                             }
                         }
-                        const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
-                        // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
-                        // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
-                        // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
-                        // two of them.
-                        float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                        const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
-                        auto exponentials = [&](uint32_t (&v)[32], const uint32_t to) {
-                            uint32_t pk[16];
-                            auto scale = [&](const int p) {
-                                const float2 t2 = fma2_in_order(make_float2(__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])), sc2, nm2);
-                                v[2 * p] = __float_as_uint(t2.x);
-                                v[2 * p + 1] = __float_as_uint(t2.y);
-                            };
-                            auto finish = [&](const int p) {
-                                const float p0 = __uint_as_float(v[2 * p]), p1 = __uint_as_float(v[2 * p + 1]);
-                                ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
-                                pk[p] = bf16x2_in_order(p0, p1);
-                            };
-                            // pairs that the scaling is ahead, and that the rest is behind
-                            constexpr int kAhead = 2, kLag = 3;
-#pragma unroll
-                            for (int p = 0; p < kAhead; ++p) scale(p);
-#pragma unroll
-                            for (int p = 0; p < 16 + kLag; ++p) {
-                                if (p < 16) v[2 * p] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p])));
-                                if (p + kAhead < 16) scale(p + kAhead);
-                                if (p < 16) v[2 * p + 1] = __float_as_uint(ex2_in_order(__uint_as_float(v[2 * p + 1])));
-                                if (p >= kLag) finish(p - kLag);
-                            }
-                            tmem_st16(to, pk);
-                        };
-                        exponentials(va, tS + half * 32);
-                        exponentials(vb, tS + half * 32 + 16);
-                        l_run = l_run * factor + ((ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
+                        tmem_st16(tS + half * 32, pa);
+                        tmem_st16(tS + half * 32 + 16, pb);
+                        l_run += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
                         tmem_wait_st();
                     }
                     tc_fence_before_sync();
