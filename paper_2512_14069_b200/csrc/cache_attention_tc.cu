@@ -137,9 +137,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         uint64_t bar_stfull[2][RS], bar_stempty[RS];
         uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2];
         uint64_t bar_idle;               // every product issued has run
-        uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
-        uint64_t bar_pv[2];              // ... and their product has run
-        uint64_t bar_pready[2];          // ... all of them
+        uint64_t bar_pready[2];          // the tile's probabilities are there
         uint64_t bar_mlfull, bar_mlempty, bar_epilogue;
         uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
         Segment seg[kSegRing];
@@ -168,7 +166,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], kDecoders); mbar_init(&st.bar_vempty[i], 1); }
             for (int i = 0; i < RS; ++i) { mbar_init(&st.bar_stfull[0][i], 1); mbar_init(&st.bar_stfull[1][i], 1); mbar_init(&st.bar_stempty[i], kDecoders); }
             for (int i = 0; i < 2; ++i) {
-                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pv[i], 1); mbar_init(&st.bar_pready[i], 4);
+                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pready[i], 4);
                 mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
             }
             for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
@@ -327,16 +325,25 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             const float m_half = fmaxf(mx0, mx1) * P.scale_log2;
                             const bool move = m_half > m_run + kRescaleThreshold;       // (m_run may be -inf)
                             if (!__any_sync(kFull, move)) break;
-                            const float factor = move ? ex2(m_run - m_half) : 1.f;       // 0 clears O and l
-                            if (move) m_run = m_half;
+                            // The reference moves by a whole number, so that the factor is a power of two and scales probabilities that
+                            // are bf16 already, those of the tile's first half, without another rounding.
+                            float factor = 1.f;
+                            if (move) {
+                                const float by = ceilf(m_half - m_run);                     // infinite: factor 0 clears O and l
+                                factor = by < 126.f ? __uint_as_float((uint32_t)(127 - (int)by) << 23) : 0.f;
+                                m_run = by < 126.f ? m_run + by : m_half;
+                            }
                             l_run *= factor;
-                            if (j > 0 || half > 0) {
-                                // (in the second half, the first one's product may still be under way)
-                                if (half == 1) {
-                                    ok = mbar_wait_while(ok, &st.bar_pv[grp], (sc - 1) & 1);
-                                    ok = __all_sync(kFull, ok);          // (lanes may leave a wait apart; what follows is for a whole warp)
-                                    tc_fence_after_sync();
-                                }
+                            if (half == 1) {
+                                const uint32_t f2 = (__float_as_uint(factor) >> 16) * 0x10001u;
+                                uint32_t first[32];
+                                tmem_ld32(tS, first);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(first[e]) : "r"(f2));
+                                tmem_st32(tS, first);
+                            }
+                            if (j > 0) {
 #pragma unroll 1
                                 for (int c = 0; c < D; c += 16) {
                                     uint32_t o[16];
@@ -353,11 +360,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         l_run += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
                         tmem_wait_st();
                     }
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(half == 0 ? &st.bar_pfirst[grp] : &st.bar_pready[grp]);
-                    __syncwarp();
                 }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.bar_pready[grp]);
+                __syncwarp();
             }
 
             // the rows' (m, l) go to the epilogue, which has taken those of the segment before
@@ -639,6 +646,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             // compiler that it is the same in every lane, so that the loops below and the descriptor arithmetic in
             // them stay on the uniform datapath (this warp's own instruction stream is what bounds the issue rate).
             auto uni = [](int v) { return __shfl_sync(kFull, v, 0); };
+            // a wait that nearly always is over when it begins
+            auto wait = [&](uint64_t* bar, const uint32_t parity) {
+                if (!__all_sync(kFull, mbar_try_wait(bar, parity))) ok = mbar_wait_while(ok, bar, parity);
+            };
             Segment s;
             for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
                 const int seg_t0 = uni(s.t0), n = uni(s.n), M = uni(s.M), Pb = uni(s.Pb), last = uni(s.nt) - 1;
@@ -648,12 +659,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 bool acc[2] = {false, false};         // accumulator holds a product of this segment
                 auto take_v = [&]() {
                     v_slot = v_next;
-                    ok = mbar_wait_while(ok, &st.bar_vfull[v_slot], v_par);
+                    wait(&st.bar_vfull[v_slot], v_par);
                     if (++v_next == RV) { v_next = 0; v_par ^= 1; }
                 };
                 auto take_k = [&]() {
                     k_slot = k_next;
-                    ok = mbar_wait_while(ok, &st.bar_kfull[k_slot], k_par);
+                    wait(&st.bar_kfull[k_slot], k_par);
                     if (++k_next == RK) { k_next = 0; k_par ^= 1; }
                 };
                 // the accumulator's first product of the segment: the epilogue of the previous one has read it
@@ -684,16 +695,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                     }
                     take_o(q);
-                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
-                    tc_fence_after_sync();
-                    // V is consumed N-major: 16 keys are 2048 B; 64-column blocks are nk * 128 B apart
-                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(nk * 128 >> 4) << 16);
-                    mma_ts_x4(ok ? elected : 0u, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
-                    mma_commit_if(ok ? elected : 0u, &st.bar_pv[q]);
                     ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
                     p_par[q] ^= 1;
                     tc_fence_after_sync();
                     const uint32_t go = ok ? elected : 0u;
+                    // V is consumed N-major: 16 keys are 2048 B; 64-column blocks are nk * 128 B apart
+                    const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(nk * 128 >> 4) << 16);
+                    mma_ts_x4(go, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
                     mma_ts_x4(go, ksteps - 4, tmem + 256 + q * 128, tmem + q * 128 + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
                     acc[q] = true;
                     if (release_v) mma_commit_if(go, &st.bar_vempty[v_slot]);
@@ -720,26 +728,23 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 // Schedule.  Two live row blocks: group s owns row block s; per tile PV0(i) S0(i+1) PV1(i) S1(i+1),
                 // both groups sharing K(i+1) and V(i).  One live row block: the groups take alternate tiles,
                 // PV(i) S(i+2) for group i & 1.  S of the first tile(s) comes from the iterations with i < 0.
-                // Steady state (all tiles involved are full prefix tiles): the same steps with nothing to decide,
-                // so that the issuing warp executes as few instructions per MMA as possible.  The waits for K and V, which are
-                // there most of the time, stand where the warp would wait for P.
+                // Steady state (behind the first tiles, and all tiles involved are full prefix tiles): the same steps with nothing to decide,
+                // so that the issuing warp executes as few instructions per MMA as possible.  (It is what the groups wait for: 32 MMAs a
+                // tile take it 2300 cycles, so everything else counts.)
                 auto full = [&](const int q, const uint32_t a0, const bool fresh, const bool release) {
-                    static_assert(kFirstKeys == 64 && kTileKeys == 128, "four steps before and behind the second wait");
+                    static_assert(kTileKeys == 128, "eight steps");
                     const uint32_t o_col = tmem + 256 + q * 128, p_col = tmem + q * 128;
-                    if (fresh) take_v();
-                    take_o(q);
+                    if (fresh) {
+                        take_v();
+                        take_k();
+                    }
                     const uint32_t b_lo = (v_lo + v_slot * (SM::kTileBytes >> 4)) | ((uint32_t)(kTileKeys * 128 >> 4) << 16);
-                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
-                    tc_fence_after_sync();
-                    mma_ts_x4(ok ? elected : 0u, o_col, p_col, b_lo, kDescHi, idesc_pv, acc[q]);
-                    mma_commit_if(ok ? elected : 0u, &st.bar_pv[q]);
-                    if (fresh) take_k();
                     const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
-                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    wait(&st.bar_pready[q], p_par[q]);
                     p_par[q] ^= 1;
-                    acc[q] = true;
                     tc_fence_after_sync();
                     const uint32_t go = ok ? elected : 0u;
+                    mma_ts_x4(go, o_col, p_col, b_lo, kDescHi, idesc_pv, true);
                     mma_ts_x4(go, o_col, p_col + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
                     if (release) mma_commit_if(go, &st.bar_vempty[v_slot]);
                     mma_ss_x4(go, p_col, a0, b0, kDescHi, idesc_s128, false);
@@ -752,7 +757,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 if (two) {
 #pragma unroll 1
                     for (int i = -1; i < n; ++i) {
-                        if (i >= 0 && i + 2 < n_full) {           // tiles i and i+1 full, and S(i+1) is not the segment's last
+                        if (i > 0 && i + 2 < n_full) {            // tiles i and i+1 full, and S(i+1) is not the segment's last
                             full(0, a_q0, true, false);
                             full(1, a_q1, false, true);
                         } else {
@@ -765,7 +770,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 } else {
 #pragma unroll 1
                     for (int i = -2; i < n; i += 2) {
-                        if (i >= 0 && i + 4 < n_full) {           // tiles i to i+3 full, S(i+3) not the last
+                        if (i > 0 && i + 4 < n_full) {            // tiles i to i+3 full, S(i+3) not the last
                             full(0, a_q0, true, true);
                             full(1, a_q0, true, true);
                         } else {
