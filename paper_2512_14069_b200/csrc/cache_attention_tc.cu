@@ -10,12 +10,12 @@
 //   warps 12-15      decoders of keys, the same; the tree's K by TMA
 //   warp 16          producer: segments, stages, Q
 //   warp 17          issues the products
-// What bounds the kernel is the chain of a tile: S, the softmax (a warp's 500 instructions, one in about five cycles beside the others'), P V, one
-// behind the other in each group, while the other group is in another part of it.  8 sequences of 8192 tokens, 64 / 8 heads, 64 rows: 184 us of
-// which the tensor pipe works 42 %, an instruction is issued in 39 % of the cycles; the same over bf16 rows takes 152 us.
-// The decoding (twelve instructions for eight values) fits beside it: 32 rows of 32 / 8 heads take 103 us here and 106 there.  A thread takes its
-// row's scores 64 at a time and waits for each load at once, which makes room for eight decoders at 96 registers; keys and
-// values are decoded by the same small loop.
+// What bounds the kernel is the warp that issues the products, with two row blocks a tile: 32 MMAs, which the tensor pipe takes at 64 to 70
+// cycles each, and waits and commits between them in which it runs dry (4500 cycles a tile); and the softmax behind it, half as
+// long.  8 sequences of 8192 tokens, 64 / 8 heads, 64 rows: 158 us; the same over bf16 rows takes 152.  The decoding (twelve instructions
+// for eight values) fits beside it: 32 rows of 32 / 8 heads, 16384 tokens, take 94 us here and 106 there.  A thread takes its row's scores
+// 64 at a time, against the maximum so far, and waits for each load at once, which makes room for eight decoders at 96 registers;
+// keys and values are decoded by the same small loop.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -31,9 +31,9 @@ using namespace cache4;
 constexpr int kTcThreads = 576;      // 18 warps are allocated as 20: 96 registers a thread
 constexpr int kEpilogueWarp = 8, kKeyWarp = 12, kProducerWarp = 16, kMmaWarp = 17, kDecoders = 4;    // decoders of either kind
 // What a tile of one and of two row blocks and a unit beside its tiles cost here (decoding takes as long for one row block as for two).
-// us, with these and with those of the kernel over bf16 rows (2, 4, 12): 32 sequences of 16384 tokens, 32 / 8 heads, 64 and 32 rows in turn
-// 500 (515), ragged trees of 9 to 64 rows, 4096 to 32768 tokens 587 (614); 4 sequences, 40 heads, 1001 to 4096 tokens 61 (63).
-constexpr TileCosts kCosts = {5, 9, 24};
+// us, with these and with 5, 9, 24: 32 sequences of 16384 tokens, 32 / 8 heads, 64 and 32 rows in turn 444 (479), ragged trees of 9 to 64
+// rows, 4096 to 32768 tokens 513 (560).
+constexpr TileCosts kCosts = {5, 8, 24};
 constexpr int kStaticSmem = 3072;
 constexpr int kTileBlocks = kTileKeys / kBlock;
 static_assert(kTileBlocks == 2 * kDecoders, "two blocks of a tile a decoder");
@@ -337,6 +337,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             if (half == 1) {
                                 const uint32_t f2 = (__float_as_uint(factor) >> 16) * 0x10001u;
                                 uint32_t first[32];
+                                tmem_wait_st();
                                 tmem_ld32(tS, first);
                                 tmem_wait_ld();
 #pragma unroll
@@ -358,9 +359,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         tmem_st16(tS + half * 32, pa);
                         tmem_st16(tS + half * 32 + 16, pb);
                         l_run += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
-                        tmem_wait_st();
                     }
                 }
+                tmem_wait_st();
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.bar_pready[grp]);
