@@ -54,9 +54,10 @@ constexpr int kMaxCluster = 16;
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 4 : 2; }
 constexpr float kMove = 8.f;         // log2 units
 // Query rows of a KV head up to which this form takes all work; above, only what is little, and cache_attention_tc.cu the rest.  8
-// sequences of 4096 to 16384 tokens, 32 / 8 heads of 128: 16 rows 44 us (there 70), 32 rows 69 (70), 48 rows 96 (72), 64 rows 123 (72); of
-// 2048 tokens: 32 rows 26 us (33), 48 rows 31 (33), 64 rows 37 (33).  Little work: 64 rows over 300 tokens 11 us (20), one
-// sequence of 1000 tokens, 256 rows 14 us (17).
+// sequences of 4096 to 16384 tokens, 32 / 8 heads of 128: 16 rows 42 us (there 65), 32 rows 68 (65), 48 rows 95 (68), 64 rows 120 (68); of
+// 2048 tokens: 32 rows 20 us (32), 48 rows 32 (33), 64 rows 37 (33).  (17 to 32 rows over long caches are up to 18 % faster there, 64 sequences
+// of 4096 to 32768 tokens 766 us (627), but the lengths are the GPU's, and the bound that the host has may be far off.)  Little work: 64
+// rows over 300 tokens 11 us (20), one sequence of 1000 tokens, 256 rows 14 us (17).
 constexpr int kTokenRows = 32;
 
 __device__ __forceinline__ float ex2(float x) {
