@@ -810,6 +810,72 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 }
 
 
+// Joins the pieces of the units that were cut: blocks (c, *) those of the unit whose first piece CTA c holds.  A warp takes a row at a time,
+// four of its pieces in flight.  What bounds it, large launches: the partial sums, written and read (8 sequences of 8192 tokens, 64 / 8 heads, 64 rows:
+// 36 MB each way, 15 of the attention's 157 us); small ones, the waves of blocks, so there are two of those and not a block for
+// each eight rows (4 sequences of 300 tokens, 40 / 40 heads, 64 rows 24 us, with 4736 blocks 26; two rows a warp spill, 30).
+template <int D>
+__global__ void __launch_bounds__(256, 6) cache_tc_combine_kernel(const TcParams P) {
+    chain_wait();
+    const radar_attn_args& a = P.a;
+    const CutUnit& cu = P.cut[blockIdx.x];
+    const int valid = cu.valid, b = cu.b, g = cu.g, slot = cu.slot, rows = cu.rows, n_pieces = cu.n_pieces;
+    const uint32_t live0 = cu.live[0];
+    if (!valid) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int E = D / 32, kPieces = 4;                   // elements of a lane; pieces in flight together
+    using Part = std::conditional_t<E == 4, float4, float2>;
+    for (int r = blockIdx.y * 8 + warp; r < rows; r += gridDim.y * 8) {
+        const int blk = r < P.rb_rows ? 0 : 1, in_blk = r - blk * P.rb_rows;       // row blocks start 128 records apart, whatever part of them is live
+        float m = -CUDART_INF_F, l = 0.f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        for (int j0 = 0; j0 < n_pieces; j0 += kPieces) {
+            const uint32_t live = (j0 < 32 ? live0 : cu.live[j0 >> 5]) >> (j0 & 31);
+            float2 ml[kPieces];
+            Part v[kPieces];
+            float m2 = m;
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                ml[j] = make_float2(-CUDART_INF_F, 0.f);
+                if (j0 + j < n_pieces && (live >> j & 1u)) {                       // (a range that holds no tile's start has no piece)
+                    const int64_t cta = (int64_t)blockIdx.x + (int64_t)(j0 + j) * P.n_cls;
+                    const int64_t rec = (cta * 2 + (j0 + j == 0 ? slot : 0)) * kPairRows + blk * 128 + in_blk;
+                    ml[j] = P.part_ml[rec];
+                    v[j] = *reinterpret_cast<const Part*>(P.part_o + rec * D + lane * E);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) m2 = fmaxf(m2, ml[j].x);
+            if (m2 == -CUDART_INF_F) continue;
+            const float old = __expf(m - m2);
+            m = m2;
+            l *= old;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= old;
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                if (ml[j].x == -CUDART_INF_F) continue;
+                const float w = __expf(ml[j].x - m);
+                l = fmaf(ml[j].y, w, l);
+                const float* x = reinterpret_cast<const float*>(&v[j]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = fmaf(x[e], w, o[e]);
+            }
+        }
+        const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
+        const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        __nv_bfloat162 w[E / 2];
+#pragma unroll
+        for (int e = 0; e < E; e += 2) w[e / 2] = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
+        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * P.nodes + node) * a.Hq + hq) * D + lane * E;
+        if (E == 4) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(w);
+        else *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(w);
+        if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * P.nodes + node] = l > 0.f ? m + logf(l) : -CUDART_INF_F;
+    }
+}
+
 // a pool as [blocks][keys or values][bytes], in numbers of eight bytes; box: that of `box_blocks` blocks
 template <int D>
 bool make_cache_map(CUtensorMap* tm, const void* pages, long long blocks, int box_blocks) {
@@ -838,7 +904,10 @@ int launch_tc(radar_ctx* ctx, const radar_cache_attn_args& c, TcParams& P, cudaS
     }
     {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_COMBINE, stream);
-        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, false, kFourBit>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
+        // two waves of blocks share out the units that can be cut
+        const int grid = P.n_cls * P.ncc, cut = (int)std::min<long long>(grid, (long long)c.B * c.Hkv * P.n_cls);
+        const int per = std::clamp((12 * ctx->sm_count + cut - 1) / cut, 1, kPairRows / 8);
+        RADAR_CUDA_CHECK(launch_chained(cache_tc_combine_kernel<D>, dim3((unsigned)grid, (unsigned)per), dim3(256), 0, stream, P));
     }
     RADAR_CUDA_CHECK(cudaGetLastError());
     return RADAR_OK;

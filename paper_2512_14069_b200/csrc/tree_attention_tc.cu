@@ -1490,7 +1490,7 @@ static int launch_tc(radar_ctx* ctx, TcParams& P, cudaStream_t stream) {
     RADAR_CUDA_CHECK(cudaGetLastError());
     {
         radar_launch_scope scope(ctx, RADAR_K_ATTN_COMBINE, stream);
-        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, FINE, kPaged>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
+        RADAR_CUDA_CHECK(launch_chained(tree_attn_tc_combine_kernel<D, FINE>, dim3((unsigned)(P.n_cls * P.ncc), kPairRows / 8), dim3(256), 0, stream, P));
     }
     RADAR_CUDA_CHECK(cudaGetLastError());
     return RADAR_OK;

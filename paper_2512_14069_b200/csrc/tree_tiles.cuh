@@ -302,11 +302,9 @@ struct __align__(16) Segment {
 // segment.  A warp merges one query row, every piece of it in flight together: the work is a chain of three trips to L2,
 // and many warps hide it better than many rows a warp do (148 cut units of 256 rows: 17.1 us event-timed with one row a
 // warp, 18.4 with two, 20.6 with four; 72 cut units of 128 rows: 10.0, 10.8, 14.7).
-// (KIND: kFourBit, or any of the others, which are alike here)
-template <int D, bool FINE, int KIND>
+template <int D, bool FINE>
 __global__ void __launch_bounds__(256) tree_attn_tc_combine_kernel(const TcParams P) {
     chain_wait();
-    const int nodes = KIND == kFourBit ? P.nodes : kMaxNodes;
     auto weight = [](float d) { return FINE ? ex2(d) : __expf(d); };      // of two pieces' maxima that differ by d
     const radar_attn_args& a = P.a;
     const CutUnit& cu = P.cut[blockIdx.x];
@@ -324,16 +322,16 @@ __global__ void __launch_bounds__(256) tree_attn_tc_combine_kernel(const TcParam
         return (cta * 2 + (j == 0 ? slot : 0)) * kPairRows + blk * 128 + in_blk;
     };
     auto store_row = [&](const float (&o)[E], float mx, float den) {
-        const float inv = KIND == kFourBit && !(den > 0.f) ? 0.f : 1.f / den;
+        const float inv = 1.f / den;
         const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
         const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.O) + layer * P.o_ls + (((int64_t)b * nodes + node) * a.Hq + hq) * D + lane * E;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.O) + layer * P.o_ls + (((int64_t)b * kMaxNodes + node) * a.Hq + hq) * D + lane * E;
         __nv_bfloat162 w[E / 2];
 #pragma unroll
         for (int q = 0; q < E; q += 2) w[q / 2] = __floats2bfloat162_rn(o[q] * inv, o[q + 1] * inv);
         if (E == 4) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(w);
         else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(w);
-        if (a.lse != nullptr && lane == 0) a.lse[layer * P.lse_ls + ((int64_t)b * a.Hq + hq) * nodes + node] = FINE ? lse_of(mx, den) : mx + logf(den);
+        if (a.lse != nullptr && lane == 0) a.lse[layer * P.lse_ls + ((int64_t)b * a.Hq + hq) * kMaxNodes + node] = FINE ? lse_of(mx, den) : mx + logf(den);
     };
     auto load_row = [&](const float* src, float (&v)[E]) {
         if (E == 4) {
