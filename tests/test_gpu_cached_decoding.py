@@ -109,3 +109,41 @@ def test_a_full_pool_grants_no_pages(ctx):
         c.admit(torch.tensor([40, 40], dtype=torch.int32, device="cuda"), torch.randn(1, 80, 2, 64, device="cuda"), torch.randn(1, 80, 2, 64, device="cuda"))
     c.release(torch.tensor([1, 0], dtype=torch.uint8, device="cuda"))
     assert int(c.free_count) == 3 and c.cache_len.tolist() == [0, 0]
+
+
+def test_a_captured_step_is_the_step(ctx):
+    """Attention and append as a CUDA graph, replayed: the same output, pages, lengths and tables as the calls issued one by one."""
+    import types
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    from paper_2512_14069_b200.cache import FourBitCache
+    B, L, Hq, Hkv, d, R = 3, 2, 8, 2, 64, rb.RADAR_MAX_NODES
+    g = torch.Generator().manual_seed(2)
+    rand = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()
+    prompt, rows, Q = (rand(L, 90, Hkv, d), rand(L, 90, Hkv, d)), (rand(L, B, R, Hkv, d), rand(L, B, R, Hkv, d)), rand(B, R, Hq, d)
+    n_nodes = torch.tensor([20, 33, 1], dtype=torch.int32, device="cuda")
+    step = types.SimpleNamespace(accept_len=torch.tensor([2, 0, 0], dtype=torch.int32, device="cuda"),
+                                 path_nodes=torch.tensor([[0, 3, 7, -1], [0, -1, -1, -1], [0, -1, -1, -1]], dtype=torch.int32, device="cuda"))
+    caches = [FourBitCache(ctx, n_layers=L, B=B, Hq=Hq, Hkv=Hkv, d=d, page_size=16, n_pages=30, max_len=160, max_new=90) for _ in range(2)]
+    O = [torch.zeros(L, B, R, Hq, d, dtype=torch.bfloat16, device="cuda") for _ in caches]
+    for c in caches:
+        c.admit(torch.tensor([40, 33, 17], dtype=torch.int32, device="cuda"), *prompt)
+
+    def run(c, out):
+        for _ in range(2):
+            for layer in range(L):
+                c.attention(layer, Q, rows[0][layer], rows[1][layer], out[layer], n_nodes=n_nodes)
+            c.append(step, *rows)
+    run(caches[0], O[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(caches[1], O[1])
+    assert caches[1].cache_len.tolist() == [40, 33, 17]
+    graph.replay()
+    torch.cuda.synchronize()
+    ctx.check_device_status()
+    assert caches[1].cache_len.tolist() == [46, 35, 19]
+    for name in ("pages", "cache_len", "block_table", "free_pages", "free_count", "granted"):
+        assert torch.equal(getattr(caches[0], name), getattr(caches[1], name)), name
+    assert torch.equal(O[0], O[1])
