@@ -514,6 +514,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     for (int k = mine; k < blocks; k += kDecoders) decode_part<D>(from + k * pitch, at + k * (kBlock * 128), share);
                     fence_proxy_async_smem();
                     ok = __all_sync(kFull, ok);
+                    __syncwarp();                            // lane 0 speaks for all lanes' reads and writes, which a vote does not order
                     if (lane == 0) {
                         mbar_arrive(&st.bar_stempty[in.slot]);
                         if (ok) mbar_arrive(&tiles_full[out.slot]);
