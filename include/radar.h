@@ -438,8 +438,9 @@ size_t radar_cache_page_bytes(int Hkv, int d, int page_size);
  * a request whose pages are not there any more (counting what all requests before it asked for) gets none, granted[b] = 0,
  * and keeps its length.  Outputs: block_table (only the entries of pages that were granted), free_pages, free_count_out,
  * cache_len_out, granted, start[0 .. B] (the running sum of the added tokens, granted or not) and slots[start[b] + j] of
- * the j-th added token, -1 where it was not granted.  With path_nodes ([B][path_stride]; entry j is the tree row of the j-th added
- * token) src_row[start[b] + j] = b * rows + path_nodes[b][j], the row that radar_cache_store takes it from.
+ * the j-th added token, -1 where it was not granted and in all entries from start[B] on.  With path_nodes ([B][path_stride];
+ * entry j is the tree row of the j-th added token) src_row[start[b] + j] = b * rows + path_nodes[b][j], the row that
+ * radar_cache_store takes it from.
  * cache_len_out may be cache_len and free_count_out free_count.  A request whose length would leave [0, max_pages * page_size],
  * or is not in it, adds nothing and records RADAR_ERR_INVALID_ARG, as do a free_count outside [0, free_capacity], a stack
  * that would overflow, a slot at or beyond slot_capacity (it is not written) and a path row outside [0, rows) (src_row -1). */

@@ -35,10 +35,8 @@ class FourBitCache:
         self.workspace = ws[off:off + n]
 
     def _extend(self, new_len, extra=0, n=None, path_nodes=None, rows=0):
-        """Slots of the added tokens: n of them, or (n None) as many as there are, the rest of the buffer -1."""
+        """Slots of the added tokens: n of them, or (n None) the whole buffer; those that no token takes are -1."""
         slots, src_row = self.slots[:n], self.src_row[:n]
-        if n is None:
-            slots.fill_(-1)
         rb.radar_cache_extend(self.ctx, page_size=self.page_size, cache_len=self.cache_len, new_len=new_len, extra=extra, block_table=self.block_table,
                               free_pages=self.free_pages, free_count=self.free_count, slots=slots, start=self.start, granted=self.granted,
                               path_nodes=path_nodes, rows=rows, src_row=None if path_nodes is None else src_row)
@@ -46,7 +44,8 @@ class FourBitCache:
 
     def admit(self, new_len, K, V):
         """New tokens of the requests: new_len [B] int32 on the GPU, K and V [layers, sum of new_len, Hkv, d], the requests' rows one
-        behind the other.  Requests that the pool had no pages for are left as they are; `granted` says which."""
+        behind the other; more rows than that are left out.  Requests that the pool had no pages for are left as they are; `granted`
+        says which."""
         if K.shape[1] > self.slots.numel():
             raise ValueError(f"{K.shape[1]} tokens, the cache was made for {self.slots.numel()} in a call")
         slots, _ = self._extend(new_len, n=K.shape[1])

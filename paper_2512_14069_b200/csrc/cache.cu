@@ -196,8 +196,10 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
             a.slots[i] = slot;
         }
     }
-    // returned pages onto the stack, new ones into the tables
+    // no slots behind the last token: whoever stores as many rows as there are slots stores nothing there
     const int step = gridDim.x * threads, me = blockIdx.x * threads + tid;
+    for (int64_t i = tokens + me; i < a.slot_capacity; i += step) a.slots[i] = -1;
+    // returned pages onto the stack, new ones into the tables
     for (int i = me; i < back_all; i += step) a.free_pages[n0 + i] = given_up(i);
     for (int i = me; i < grow_all && i < n1; i += step) {
         const int b = owner(s_grow, 0, B, i);
