@@ -442,8 +442,9 @@ size_t radar_cache_page_bytes(int Hkv, int d, int page_size);
  * entry j is the tree row of the j-th added token) src_row[start[b] + j] = b * rows + path_nodes[b][j], the row that
  * radar_cache_store takes it from.
  * cache_len_out may be cache_len and free_count_out free_count.  A request whose length would leave [0, max_pages * page_size],
- * or is not in it, adds nothing and records RADAR_ERR_INVALID_ARG, as do a free_count outside [0, free_capacity], a stack
- * that would overflow, a slot at or beyond slot_capacity (it is not written) and a path row outside [0, rows) (src_row -1). */
+ * or is not in it, is not granted (its tokens count in start like those of any other) and records RADAR_ERR_INVALID_ARG, as do a
+ * free_count outside [0, free_capacity], a stack that would overflow, a slot at or beyond slot_capacity (it is not written) and a path
+ * row outside [0, rows) (src_row -1). */
 typedef struct {
     int B, page_size, max_pages;
     const int32_t* cache_len;           /* [B] */

@@ -44,8 +44,8 @@ class FourBitCache:
 
     def admit(self, new_len, K, V):
         """New tokens of the requests: new_len [B] int32 on the GPU, K and V [layers, sum of new_len, Hkv, d], the requests' rows one
-        behind the other; more rows than that are left out.  Requests that the pool had no pages for are left as they are; `granted`
-        says which."""
+        behind the other; more rows than that are left out.  Requests that the pool had no pages for, or the table no room, are left as
+        they are; `granted` says which."""
         if K.shape[1] > self.slots.numel():
             raise ValueError(f"{K.shape[1]} tokens, the cache was made for {self.slots.numel()} in a call")
         slots, _ = self._extend(new_len, n=K.shape[1])

@@ -37,13 +37,16 @@ __device__ __forceinline__ int pages_of(const ExtendParams& P, int tokens) {
     return P.shift >= 0 ? (tokens + P.a.page_size - 1) >> P.shift : (int)((unsigned)(tokens + P.a.page_size - 1) / (unsigned)P.a.page_size);
 }
 
-struct Request { int len, n, have, want; bool ok; };
+// add: tokens that it counts in the running sum, also where it is refused (the caller's rows are laid out by new_len, whatever happens
+// to a request)
+struct Request { int len, n, add, have, want; bool ok; };
 __device__ __forceinline__ Request request(const ExtendParams& P, int b) {
     Request r;
     r.len = P.a.cache_len[b];
     const long long n = (long long)P.a.new_len[b] + P.a.extra, most = min((long long)P.a.max_pages * P.a.page_size, (long long)INT32_MAX - P.a.page_size);
     r.ok = r.len >= 0 && r.len <= most && r.len + n >= 0 && r.len + n <= most;
     r.n = r.ok ? (int)n : 0;
+    r.add = (int)max(0ll, min(n, (long long)INT32_MAX));
     r.have = r.ok ? pages_of(P, r.len) : 0;
     r.want = r.ok ? pages_of(P, r.len + r.n) : 0;
     return r;
@@ -55,7 +58,7 @@ __device__ __forceinline__ int add_clipped(int a, int b) { return (int)min((unsi
 // what a request adds to the three sums
 struct Sums {
     int v[3];                            // tokens, pages lacked, pages given up
-    __device__ __forceinline__ explicit Sums(const Request& r) : v{max(r.n, 0), max(r.want - r.have, 0), max(r.have - r.want, 0)} {}
+    __device__ __forceinline__ explicit Sums(const Request& r) : v{r.add, max(r.want - r.have, 0), max(r.have - r.want, 0)} {}
 };
 
 // Exclusive sums over the block's threads, behind `carry`, which the block's own are added to.
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
     int sum[3] = {0, 0, 0};
     for (int b0 = 0; b0 < B; b0 += threads) {
         const int b = b0 + tid;
-        Request r = {0, 0, 0, 0, true};
+        Request r = {0, 0, 0, 0, 0, true};
         if (b < B) r = request(P, b);
         if (!r.ok && first) set_status(P.status, RADAR_ERR_INVALID_ARG);
         Sums x(r);
@@ -156,8 +159,8 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
         const int at = n1 - 1 - i;
         return at < n0 ? a.free_pages[at] : given_up(at - n0);
     };
-    auto granted = [&](int b, const Request& r) { return r.want <= r.have || s_grow[b + 1] <= n1; };
-    // tokens of ungranted requests still count in `start`; slots beyond the capacity are not written
+    auto granted = [&](int b, const Request& r) { return r.ok && (r.want <= r.have || s_grow[b + 1] <= n1); };
+    // tokens of requests that are not granted still count in `start`; slots beyond the capacity are not written
     const int64_t tokens = min((int64_t)tok_all, a.slot_capacity);
     const int lane = tid & 31, warps = threads >> 5;
     constexpr int kRun = 32 * RUNS;
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
         if (b == B) break;
         const Request r = request(P, b);
         const bool on = granted(b, r);
-        a.granted[b] = r.ok && on;
+        a.granted[b] = on;
         if (P.lengths_here) a.cache_len_out[b] = on ? r.len + r.n : r.len;
     }
 }
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(kExtendThreads) cache_lengths_kernel(const Ext
     int sum[3] = {0, 0, 0};
     for (int b0 = 0; b0 < a.B; b0 += kExtendThreads) {
         const int b = b0 + threadIdx.x;
-        Request r = {0, 0, 0, 0, true};
+        Request r = {0, 0, 0, 0, 0, true};
         if (b < a.B) r = request(P, b);
         Sums x(r);
         if (b < a.B) {

@@ -22,7 +22,8 @@ def _rows(seed, L, n, Hkv, d):
 
 
 def _held(x):
-    return C.values(*C.quantise(x.double().cpu().numpy()))
+    x = x.double().cpu().numpy()
+    return C.values(*C.quantise(x)) if x.size else x
 
 
 def _load(cache, lens):
@@ -49,6 +50,43 @@ def _cache(ctx, **kw):
 
 
 # ---- admission ------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("where", [0, 1, 2])
+def test_a_prompt_that_is_too_long_takes_nobodys_rows(ctx, where):
+    """The others get their own rows, and a request admitted before keeps its own."""
+    c = _cache(ctx)
+    before = _rows(1, 2, 40, 2, 64)
+    c.admit(_i32([0, 0, 0, 40]), *before)
+    new = [20, 5]
+    new.insert(where, 100)
+    rows = _rows(2, 2, 125, 2, 64)
+    c.admit(_i32(new + [0]), *rows)
+    assert ctx.read_device_status() == -1
+    kept = [n if n < 100 else 0 for n in new] + [40]
+    assert c.cache_len.tolist() == kept and c.granted.tolist() == [int(n < 100) for n in new] + [1]
+    got = _load(c, kept)
+    ctx.check_device_status()
+    at = 0
+    for b, n in enumerate(new):
+        for x, have in zip(rows, got[b]):
+            assert np.array_equal(have, _held(x[:, at:at + kept[b]])), b
+        at += n
+    for x, have in zip(before, got[3]):
+        assert np.array_equal(have, _held(x))
+
+
+def test_refused_requests_count_their_tokens(ctx):
+    """... in the running sum, with no slots: lengths that do not fit, lengths that are none."""
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    lens, new = [3, 0, -7, 60, 16], [10, 9, 4, 5, 8]
+    t = dict(cache_len=_i32(lens), new_len=_i32(new), block_table=_i32(np.arange(20).reshape(5, 4).tolist()), free_pages=_i32(list(range(20, 40))), free_count=_i32([20]),
+             slots=torch.full((50,), 77, dtype=torch.int64, device="cuda"), start=_i32([0] * 6), granted=torch.zeros(5, dtype=torch.uint8, device="cuda"))
+    rb.radar_cache_extend(ctx, page_size=16, **t)
+    assert ctx.read_device_status() == -1
+    assert t["start"].tolist() == [0, 10, 19, 23, 28, 36] and t["granted"].tolist() == [1, 1, 0, 0, 1]
+    assert t["cache_len"].tolist() == [13, 9, -7, 60, 24]
+    s = t["slots"].tolist()
+    assert s[:10] == list(range(3, 13)) and s[10:19] == [39 * 16 + i for i in range(9)] and s[19:28] == [-1] * 9 and s[28:36] == [38 * 16 + i for i in range(8)]
 def test_rows_beyond_the_new_tokens_are_nobodys(ctx):
     """K and V of a fixed size, as a captured admission has them, hold more rows than are added."""
     c = _cache(ctx)
