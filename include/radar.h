@@ -435,16 +435,16 @@ size_t radar_cache_page_bytes(int Hkv, int d, int page_size);
  * and extra 1: the root and the accepted nodes).  n < 0: it gives up its last tokens (a finished request all of them), and
  * the pages that it no longer needs go onto the stack free_pages[0 .. free_count), request after request, in the order of its
  * table.  n > 0: the pages that it lacks come from the top of the stack, request after request, behind all that was given up;
- * a request whose pages are not there any more (counting what all requests before it asked for) gets none, granted[b] = 0,
- * and keeps its length.  Outputs: block_table (only the entries of pages that were granted), free_pages, free_count_out,
- * cache_len_out, granted, start[0 .. B] (the running sum of the added tokens, granted or not) and slots[start[b] + j] of
- * the j-th added token, -1 where it was not granted and in all entries from start[B] on.  With path_nodes ([B][path_stride];
+ * a request whose pages are not there any more (counting what all requests before it asked for), or whose tokens pass the slots'
+ * capacity, gets none, granted[b] = 0, and keeps its length.  Outputs: block_table (only the entries of pages that were
+ * granted), free_pages, free_count_out, cache_len_out, granted, start[0 .. B] (the running sum of the added tokens, granted or not)
+ * and slots[start[b] + j] of the j-th added token, -1 where it was not granted and in all entries from start[B] on.  With path_nodes ([B][path_stride];
  * entry j is the tree row of the j-th added token) src_row[start[b] + j] = b * rows + path_nodes[b][j], the row that
  * radar_cache_store takes it from.
  * cache_len_out may be cache_len and free_count_out free_count.  A request whose length would leave [0, max_pages * page_size],
  * or is not in it, is not granted (its tokens count in start like those of any other) and records RADAR_ERR_INVALID_ARG, as do a
- * free_count outside [0, free_capacity], a stack that would overflow, a slot at or beyond slot_capacity (it is not written) and a path
- * row outside [0, rows) (src_row -1). */
+ * free_count outside [0, free_capacity], a stack that would overflow, a running sum beyond slot_capacity and a path row outside
+ * [0, rows) (src_row -1). */
 typedef struct {
     int B, page_size, max_pages;
     const int32_t* cache_len;           /* [B] */

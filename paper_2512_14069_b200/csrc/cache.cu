@@ -159,7 +159,10 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
         const int at = n1 - 1 - i;
         return at < n0 ? a.free_pages[at] : given_up(at - n0);
     };
-    auto granted = [&](int b, const Request& r) { return r.ok && (r.want <= r.have || s_grow[b + 1] <= n1); };
+    // Pages and slots go to requests in order as long as there are enough: both sums only grow, so one request is the first that gets none.
+    // (A sum that ended at the largest int has no slots.)
+    const int room = (int)min(a.slot_capacity, (int64_t)INT32_MAX - 1);
+    auto granted = [&](int b, const Request& r) { return r.ok && (r.n <= 0 || (s_tok[b + 1] <= room && (r.want <= r.have || s_grow[b + 1] <= n1))); };
     // tokens of requests that are not granted still count in `start`; slots beyond the capacity are not written
     const int64_t tokens = min((int64_t)tok_all, a.slot_capacity);
     const int lane = tid & 31, warps = threads >> 5;
@@ -214,8 +217,9 @@ __global__ void __launch_bounds__(kExtendThreads) cache_extend_kernel(const Exte
     if (P.lengths_here) __syncthreads();
     for (int b = tid; b <= B; b += threads) {
         a.start[b] = s_tok[b];
-        // pages go to requests in order as long as there are enough: the largest sum that does not pass n1 is used up
-        if (P.lengths_here && s_grow[b] <= n1 && (b == B || s_grow[b + 1] > n1)) *a.free_count_out = n1 - s_grow[b];
+        // the pages of the requests before the first one that gets none are used up
+        const bool before = s_grow[b] <= n1 && s_tok[b] <= room;
+        if (P.lengths_here && before && (b == B || s_grow[b + 1] > n1 || s_tok[b + 1] > room)) *a.free_count_out = n1 - s_grow[b];
         if (b == B) break;
         const Request r = request(P, b);
         const bool on = granted(b, r);

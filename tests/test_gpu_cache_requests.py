@@ -115,3 +115,49 @@ def test_slots_behind_the_last_token_hold_none(ctx, capacity, in_place):
     ctx.check_device_status()
     s = t["slots"].cpu()
     assert bool((s[:n] >= 0).all()) and bool((s[n:] == -1).all())
+
+
+# ---- room for slots -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("B,most,capacity", [(2, 8, 6), (5, 9, 11), (300, 40, 4000), (300, 40, 4500), (300, 60, 0), (700, 33, 8000)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_tokens_without_a_slot_are_not_granted(ctx, B, most, capacity, in_place):
+    """A length counts only tokens that have a slot to be stored in: from the first request whose tokens pass the slots' capacity on,
+    requests that add tokens are not granted, take no pages and keep their lengths."""
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    rng = np.random.default_rng(B + capacity)
+    page, columns = 16, 8
+    lens = rng.integers(0, 40, B)
+    new = np.where(rng.random(B) < 0.2, -rng.integers(0, lens + 1), rng.integers(0, most, B))
+    new[0] = min(4, most)
+    table, n_pages = np.arange(B * columns).reshape(B, columns), B * columns
+    stack = np.arange(n_pages, 2 * n_pages)
+    t = dict(cache_len=_i32(lens.tolist()), new_len=_i32(new.tolist()), block_table=_i32(table.tolist()), free_pages=_i32(stack.tolist()), free_count=_i32([n_pages - 3 * B]),
+             slots=torch.full((capacity,), 9, dtype=torch.int64, device="cuda"), start=_i32([0] * (B + 1)), granted=torch.zeros(B, dtype=torch.uint8, device="cuda"))
+    if not in_place:
+        t.update(cache_len_out=_i32([0] * B), free_count_out=_i32([0]))
+    rb.radar_cache_extend(ctx, page_size=page, **t)
+    add = np.maximum(new, 0)
+    end = np.cumsum(add)
+    assert end[-1] > capacity and ctx.read_device_status() == -1
+    out = (new > 0) & (end > capacity)
+    want = C.extend(page, lens, np.where(out, 0, new), table, stack, n_pages - 3 * B)
+    got = lambda name: (t[name] if in_place or name + "_out" not in t else t[name + "_out"]).cpu().numpy()
+    assert np.array_equal(t["granted"].cpu().numpy().astype(bool), want[5] & ~out)
+    assert np.array_equal(got("cache_len"), want[3]) and got("free_count")[0] == want[2]
+    assert np.array_equal(t["block_table"].cpu().numpy(), want[0]) and np.array_equal(t["free_pages"].cpu().numpy()[:want[2]], want[1][:want[2]])
+    assert np.array_equal(t["start"].cpu().numpy(), np.concatenate([[0], end]))
+    slots = np.concatenate([[-1] * add[b] if out[b] else want[4][b] for b in range(B)])[:capacity]
+    assert np.array_equal(t["slots"].cpu().numpy(), slots)
+
+
+def test_counts_that_no_int_holds(ctx):
+    """The running sum ends at the largest int: what lies behind has no slots and is not granted."""
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    t = dict(cache_len=_i32([0, 0]), new_len=_i32([2 ** 31 - 1, 4]), block_table=_i32([[0], [1]]), free_pages=_i32(list(range(20))), free_count=_i32([20]),
+             slots=torch.full((50,), 77, dtype=torch.int64, device="cuda"), start=_i32([0] * 3), granted=torch.zeros(2, dtype=torch.uint8, device="cuda"))
+    rb.radar_cache_extend(ctx, page_size=16, extra=5, **t)
+    assert ctx.read_device_status() == -1
+    assert t["cache_len"].tolist() == [0, 0] and t["granted"].tolist() == [0, 0] and t["start"].tolist() == [0, 2 ** 31 - 1, 2 ** 31 - 1]
+    assert t["slots"].tolist() == [-1] * 50 and t["free_count"].tolist() == [20]
