@@ -18,7 +18,7 @@ from . import binding as rb
 class FourBitCache:
     def __init__(self, ctx: rb.Context, *, n_layers, B, Hq, Hkv, d, page_size, n_pages, max_len, max_new, rows=rb.RADAR_MAX_NODES, device="cuda:0"):
         """Pool of n_pages pages of page_size tokens in each layer; requests of up to max_len tokens; max_new: added tokens of all
-        requests in one call; rows: query rows of a sequence, at most."""
+        requests in one call (B * (t_max + 1) for a step's); rows: query rows of a sequence, at most."""
         self.ctx = ctx
         self.n_layers, self.B, self.Hq, self.Hkv, self.d, self.page_size, self.max_len = n_layers, B, Hq, Hkv, d, page_size, max_len
         dev, i32 = torch.device(device), torch.int32
@@ -54,6 +54,8 @@ class FourBitCache:
     def append(self, step, K, V):
         """What a step accepted: the root and step.path_nodes, from the tree's rows of all layers, [layers, B, rows, Hkv, d]."""
         rows = K.shape[2]
+        if step.path_nodes.numel() > self.slots.numel():
+            raise ValueError(f"a step may accept {step.path_nodes.numel()} tokens, the cache was made for {self.slots.numel()} in a call")
         slots, src_row = self._extend(step.accept_len, extra=1, path_nodes=step.path_nodes, rows=rows)
         rb.radar_cache_store(self.ctx, K=K.flatten(1, 2), V=V.flatten(1, 2), slots=slots, src_row=src_row, pages=self.pages, page_size=self.page_size)
 

@@ -1,4 +1,6 @@
 """Requests that a 4-bit cache has no room for, beside others that it holds; rows that are not in use; bounds of the lengths."""
+import types
+
 import numpy as np
 import pytest
 
@@ -161,3 +163,17 @@ def test_counts_that_no_int_holds(ctx):
     assert ctx.read_device_status() == -1
     assert t["cache_len"].tolist() == [0, 0] and t["granted"].tolist() == [0, 0] and t["start"].tolist() == [0, 2 ** 31 - 1, 2 ** 31 - 1]
     assert t["slots"].tolist() == [-1] * 50 and t["free_count"].tolist() == [20]
+
+
+def _step(accept, columns=4):
+    n = len(accept)
+    return types.SimpleNamespace(accept_len=_i32(accept), path_nodes=_i32([list(range(columns))] * n))
+
+
+def test_append_wants_room_for_what_a_step_may_accept(ctx):
+    c = _cache(ctx, max_new=15)
+    K, V = _rows(5, 2, 4 * 64, 2, 64)
+    c.admit(_i32([2, 3, 1, 1]), K[:, :7], V[:, :7])
+    with pytest.raises(ValueError, match="made for 15"):
+        c.append(_step([0, 0, 0, 0]), K.view(2, 4, 64, 2, 64), V.view(2, 4, 64, 2, 64))
+    assert c.cache_len.tolist() == [2, 3, 1, 1]
