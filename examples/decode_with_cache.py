@@ -71,9 +71,8 @@ class Decoder:
             s = s.masked_fill(torch.ones(n, n, device="cuda", dtype=torch.bool).triu(1), float("-inf"))
             return (s.softmax(-1) @ heads(Vt)).transpose(0, 1)[None].bfloat16()
         m.forward(tokens[None, :n], torch.arange(n, device="cuda")[None], attend)
-        new_len = torch.zeros(self.B, dtype=torch.int32, device="cuda")
-        new_len[b] = n
-        self.cache.admit(new_len, K, V)
+        which = torch.arange(self.B, device="cuda") == b
+        self.cache.admit(torch.where(which, n, 0).to(torch.int32), K, V, requests=which)
         self.root[b] = int(prompt[-1])
 
     def draft(self):
@@ -130,8 +129,7 @@ def main(requests=6, B=3, tokens=24, seed=1):
             if slot[b] is not None:
                 text[slot[b]] += new[b]
                 if len(text[slot[b]]) >= tokens:
-                    slot[b] = None
-            done[b] = slot[b] is None
+                    slot[b], done[b] = None, 1
         dec.cache.release(done.cuda())
         ctx.check_device_status()
     for i in sorted(text):

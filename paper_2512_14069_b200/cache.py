@@ -7,6 +7,8 @@ decoding loop over it can be captured in a CUDA graph.  It contains no arithmeti
     step.attention_cached(cache, layer, Q, Kt, Vt)      # or cache.attention for other rows than a step's tree
     cache.append(step, K, V)            # behind step.accept: the root and the accepted nodes, from the tree's rows
     cache.release(finished)             # their pages go back onto the stack
+
+`live` says which rows hold a request: from an admission that was granted until its release.  Only those take what a step accepted.
 """
 from __future__ import annotations
 
@@ -25,7 +27,7 @@ class FourBitCache:
         self.pages = torch.zeros((n_layers, n_pages, rb.radar_cache_page_bytes(Hkv, d, page_size)), dtype=torch.uint8, device=dev)
         self.block_table = torch.full((B, -(-max_len // page_size)), -1, dtype=i32, device=dev)
         self.cache_len, self.start = torch.zeros(B, dtype=i32, device=dev), torch.zeros(B + 1, dtype=i32, device=dev)
-        self.granted = torch.zeros(B, dtype=torch.uint8, device=dev)
+        self.granted, self.live = torch.zeros(B, dtype=torch.uint8, device=dev), torch.zeros(B, dtype=torch.bool, device=dev)
         self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=dev)           # taken from the top: page 0 first
         self.free_count = torch.full((1,), n_pages, dtype=i32, device=dev)
         self.slots, self.src_row = torch.full((max_new,), -1, dtype=torch.int64, device=dev), torch.zeros(max_new, dtype=i32, device=dev)
@@ -42,26 +44,31 @@ class FourBitCache:
                               path_nodes=path_nodes, rows=rows, src_row=None if path_nodes is None else src_row)
         return slots, None if path_nodes is None else src_row
 
-    def admit(self, new_len, K, V):
+    def admit(self, new_len, K, V, requests=None):
         """New tokens of the requests: new_len [B] int32 on the GPU, K and V [layers, sum of new_len, Hkv, d], the requests' rows one
         behind the other; more rows than that are left out.  Requests that the pool had no pages for, or the table no room, are left as
-        they are; `granted` says which."""
+        they are; `granted` says which.  requests [B] on the GPU names those that are admitted (not 0) where one of them has no
+        tokens to cache yet; without it they are those with new_len > 0."""
         if K.shape[1] > self.slots.numel():
             raise ValueError(f"{K.shape[1]} tokens, the cache was made for {self.slots.numel()} in a call")
         slots, _ = self._extend(new_len, n=K.shape[1])
         rb.radar_cache_store(self.ctx, K=K, V=V, slots=slots, pages=self.pages, page_size=self.page_size)
+        self.live |= ((new_len > 0) if requests is None else (requests != 0)) & (self.granted != 0)
 
     def append(self, step, K, V):
-        """What a step accepted: the root and step.path_nodes, from the tree's rows of all layers, [layers, B, rows, Hkv, d]."""
+        """What a step accepted: the root and step.path_nodes, from the tree's rows of all layers, [layers, B, rows, Hkv, d].  Rows that
+        hold no request take nothing; a request that the pool had no pages for keeps its length (`granted`), and takes the step again
+        when there are some."""
         rows = K.shape[2]
         if step.path_nodes.numel() > self.slots.numel():
             raise ValueError(f"a step may accept {step.path_nodes.numel()} tokens, the cache was made for {self.slots.numel()} in a call")
-        slots, src_row = self._extend(step.accept_len, extra=1, path_nodes=step.path_nodes, rows=rows)
+        slots, src_row = self._extend(torch.where(self.live, step.accept_len, -1), extra=1, path_nodes=step.path_nodes, rows=rows)
         rb.radar_cache_store(self.ctx, K=K.flatten(1, 2), V=V.flatten(1, 2), slots=slots, src_row=src_row, pages=self.pages, page_size=self.page_size)
 
     def release(self, finished):
         """Gives up the tokens of the requests with finished[b] != 0 ([B] on the GPU)."""
         self._extend(torch.where(finished != 0, -self.cache_len, 0).to(torch.int32))
+        self.live &= finished == 0
 
     def attention(self, layer, Q, Kt, Vt, O, lse=None, mask=None, n_nodes=None, scale=0.0):
         """radar_cache_attention over one layer's pool: Q [B, rows, Hq, d], Kt and Vt [B, rows, Hkv, d], the rows' own keys and values."""

@@ -177,3 +177,54 @@ def test_append_wants_room_for_what_a_step_may_accept(ctx):
     with pytest.raises(ValueError, match="made for 15"):
         c.append(_step([0, 0, 0, 0]), K.view(2, 4, 64, 2, 64), V.view(2, 4, 64, 2, 64))
     assert c.cache_len.tolist() == [2, 3, 1, 1]
+
+
+# ---- rows that hold no request ----------------------------------------------------------------------------------------------
+def test_append_leaves_out_rows_that_hold_no_request(ctx):
+    """Never admitted, refused, released: none of them grows or takes a page, and one that is admitted again does."""
+    import torch
+    c = _cache(ctx, n_pages=6)
+    K, V = _rows(6, 2, 4 * 64, 2, 64)
+    tree = K.view(2, 4, 64, 2, 64), V.view(2, 4, 64, 2, 64)
+    c.admit(_i32([20, 16, 60, 0]), K[:, :96], V[:, :96])             # two pages, one, four (refused), never
+    assert c.granted.tolist() == [1, 1, 0, 1] and int(c.free_count) == 3
+    c.append(_step([3, 1, 3, 3]), *tree)
+    ctx.check_device_status()
+    assert c.cache_len.tolist() == [24, 18, 0, 0] and int(c.free_count) == 2
+    c.release(torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda"))
+    free = int(c.free_count)
+    for _ in range(3):
+        c.append(_step([3, 0, 3, 3]), *tree)
+    ctx.check_device_status()
+    assert c.cache_len.tolist() == [0, 21, 0, 0] and int(c.free_count) == free == 4
+    c.admit(_i32([0, 0, 5, 0]), K[:, :5], V[:, :5])
+    c.append(_step([1, 1, 1, 1]), *tree)
+    ctx.check_device_status()
+    assert c.cache_len.tolist() == [0, 23, 7, 0]
+    got = _load(c, [0, 23, 7, 0])
+    want = np.concatenate([_held(K[:, :5]), _held(K[:, 2 * 64:2 * 64 + 2])], 1)
+    assert np.array_equal(got[2][0], want)
+
+
+def test_a_request_without_cached_tokens_may_be_admitted(ctx):
+    """A prompt of one token, the first step's root: nothing is cached yet, and its steps count."""
+    import torch
+    c = _cache(ctx)
+    K, V = _rows(7, 2, 4 * 64, 2, 64)
+    c.admit(_i32([0, 0, 0, 0]), K[:, :0], V[:, :0], requests=torch.tensor([0, 1, 0, 0], dtype=torch.uint8, device="cuda"))
+    c.append(_step([2, 2, 2, 2]), K.view(2, 4, 64, 2, 64), V.view(2, 4, 64, 2, 64))
+    ctx.check_device_status()
+    assert c.cache_len.tolist() == [0, 3, 0, 0]
+
+
+def test_an_idle_row_takes_no_page_from_a_live_one(ctx):
+    import torch
+    c = _cache(ctx, n_pages=3)
+    K, V = _rows(8, 2, 4 * 64, 2, 64)
+    tree = K.view(2, 4, 64, 2, 64), V.view(2, 4, 64, 2, 64)
+    c.admit(_i32([15, 31, 0, 0]), K[:, :46], V[:, :46])
+    c.release(torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda"))
+    c.append(_step([0, 0, 0, 0]), *tree)
+    c.append(_step([0, 1, 0, 0]), *tree)
+    ctx.check_device_status()
+    assert c.granted.tolist() == [1, 1, 1, 1] and c.cache_len.tolist() == [0, 34, 0, 0]
