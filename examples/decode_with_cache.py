@@ -58,7 +58,8 @@ class Decoder:
         self.root = torch.zeros(B, dtype=torch.int32, device="cuda")
 
     def admit(self, b, prompt):
-        """A prompt for request b, which must be empty.  Its last token becomes the root of the first step."""
+        """A prompt for request b, which must be empty.  Its last token becomes the root of the first step.  False: there are no pages
+        for it."""
         m, n = self.model, len(prompt) - 1
         tokens = torch.tensor(prompt, device="cuda")
         K = torch.empty(m.layers, n, m.Hkv, m.d, dtype=torch.bfloat16, device="cuda")
@@ -74,6 +75,7 @@ class Decoder:
         which = torch.arange(self.B, device="cuda") == b
         self.cache.admit(torch.where(which, n, 0).to(torch.int32), K, V, requests=which)
         self.root[b] = int(prompt[-1])
+        return bool(self.cache.granted[b])
 
     def draft(self):
         """The draft calls of a step: rows of the bigram table for the root, then for each call's frontier."""
@@ -99,43 +101,58 @@ class Decoder:
         return self.model.forward(tokens, positions, attend)
 
     def decode_step(self, check=None):
-        """One step of all requests; the tokens that it emitted, by request."""
+        """One step of all requests; the tokens that it emitted, by request.  A request that the pool has no page for emits none and keeps
+        its root: the same step again when there are pages."""
         s, c = self.step, self.cache
         self.draft()
         s.build_tree(self.root, c.cache_len)
         s.accept(self.verify(check), self.draft_logits)
         c.append(s, self.K, self.V)
-        self.root.copy_(s.next_token)
-        lens, path, nxt = s.accept_len.tolist(), s.path_tokens.tolist(), s.next_token.tolist()
-        return [path[b][1:1 + lens[b]] + [nxt[b]] for b in range(self.B)]
+        took = c.live & (c.granted != 0)
+        self.root.copy_(torch.where(took, s.next_token, self.root))
+        took, lens, path, nxt = took.tolist(), s.accept_len.tolist(), s.path_tokens.tolist(), s.next_token.tolist()
+        return [path[b][1:1 + lens[b]] + [nxt[b]] if took[b] else [] for b in range(self.B)]
 
 
-def main(requests=6, B=3, tokens=24, seed=1):
+def main(requests=6, B=3, tokens=24, seed=1, n_pages=64):
     torch.manual_seed(seed)
     ctx = rb.Context(0)
     model = Model(layers=2, Hq=8, Hkv=2, d=64, V=512, max_len=256)
-    dec = Decoder(ctx, model, B=B)
-    waiting = [(i, torch.randint(0, model.V, (int(n),)).tolist()) for i, n in enumerate(torch.randint(5, 60, (requests,)))]
-    slot, text, steps = [None] * B, {}, 0
-    while waiting or any(x is not None for x in slot):
+    dec = Decoder(ctx, model, B=B, n_pages=n_pages)
+    prompts = [torch.randint(0, model.V, (int(n),)).tolist() for n in torch.randint(5, 60, (requests,))]
+    waiting, text = list(range(requests)), [[] for _ in range(requests)]
+    slot, admitted, starved, steps = [None] * B, [], False, 0            # requests in the batch's rows; rows in the order of their admission
+    while waiting or admitted:
         for b in range(B):
-            if slot[b] is None and waiting:
-                slot[b], prompt = waiting.pop(0)
-                text[slot[b]] = []
-                dec.admit(b, prompt)
+            if slot[b] is None and waiting and not (starved and admitted):     # (pages go to those that run before new ones come in)
+                if not dec.admit(b, prompts[waiting[0]] + text[waiting[0]]):
+                    break
+                slot[b] = waiting.pop(0)
+                admitted.append(b)
+        if not admitted:
+            raise RuntimeError("too few pages for a prompt")
         new, steps = dec.decode_step(), steps + 1
+        starved = not all(new[b] for b in admitted)
         done = torch.zeros(B, dtype=torch.uint8)
+        for b in list(admitted):
+            text[slot[b]] += new[b]
+            if len(text[slot[b]]) >= tokens:
+                done[b] = 1
+        if not any(new[b] for b in admitted):                            # nobody goes on: the last one makes room, and waits
+            if len(admitted) == 1:
+                raise RuntimeError("too few pages for a request")
+            done[admitted[-1]] = 1
+            waiting.insert(0, slot[admitted[-1]])
         for b in range(B):
-            if slot[b] is not None:
-                text[slot[b]] += new[b]
-                if len(text[slot[b]]) >= tokens:
-                    slot[b], done[b] = None, 1
+            if done[b]:
+                admitted.remove(b)
+                slot[b] = None
         dec.cache.release(done.cuda())
         ctx.check_device_status()
-    for i in sorted(text):
+    for i in range(requests):
         print(i, *text[i][:tokens])
-    print(f"{sum(map(len, text.values()))} tokens in {steps} steps, {int(dec.cache.free_count)} of {dec.cache.free_pages.numel()} pages free")
-    return text, dec
+    print(f"{sum(map(len, text))} tokens in {steps} steps, {int(dec.cache.free_count)} of {dec.cache.free_pages.numel()} pages free")
+    return dict(enumerate(text)), dec
 
 
 if __name__ == "__main__":

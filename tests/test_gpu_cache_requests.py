@@ -228,3 +228,49 @@ def test_an_idle_row_takes_no_page_from_a_live_one(ctx):
     c.append(_step([0, 1, 0, 0]), *tree)
     ctx.check_device_status()
     assert c.granted.tolist() == [1, 1, 1, 1] and c.cache_len.tolist() == [0, 34, 0, 0]
+
+
+def test_a_step_that_finds_no_page_is_taken_again():
+    """The example's decoder: a request whose tokens were not granted emits none and keeps its root, until there are pages."""
+    import os
+    import sys
+    import torch
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode_with_cache as D
+    from paper_2512_14069_b200 import binding as rb
+    ctx = rb.Context(0)
+    model = D.Model(layers=2, Hq=4, Hkv=2, d=64, V=100, max_len=128, seed=4)
+    texts = []
+    for n_pages in (20, 4):
+        dec = D.Decoder(ctx, model, B=2, n_pages=n_pages, max_len=128)
+        assert dec.admit(0, list(range(17))) and dec.admit(1, list(range(30, 63)))       # one page, two
+        text = []
+        for step in range(40):
+            if step == 12:
+                dec.cache.release(torch.tensor([1, 0], dtype=torch.uint8, device="cuda"))
+            before, root = dec.cache.cache_len.tolist(), dec.root.tolist()
+            new = dec.decode_step()
+            ctx.check_device_status()
+            assert [a - b for a, b in zip(dec.cache.cache_len.tolist(), before)] == [len(e) for e in new]
+            if not new[1]:
+                assert dec.root[1] == root[1]
+            text += new[1]
+            if step >= 12:
+                assert new[0] == []
+        texts.append(text)
+        assert dec.cache.granted.tolist()[1] == (n_pages == 20 or len(text) + 32 <= 64)
+    assert len(texts[1]) < len(texts[0])
+    assert texts[1] == texts[0][:len(texts[1])]
+    ctx.close()
+
+
+def test_the_example_with_few_pages_answers_every_request():
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode_with_cache as D
+    text, dec = D.main(n_pages=8)
+    assert len(text) == 6 and all(len(t) >= 24 for t in text.values())
+    assert int(dec.cache.free_count) == 8 and dec.cache.cache_len.tolist() == [0] * dec.B
+    with pytest.raises(RuntimeError, match="pages"):
+        D.main(n_pages=1)
