@@ -19,19 +19,21 @@ from . import binding as rb
 
 class FourBitCache:
     def __init__(self, ctx: rb.Context, *, n_layers, B, Hq, Hkv, d, page_size, n_pages, max_len, max_new, rows=rb.RADAR_MAX_NODES, device="cuda:0"):
-        """Pool of n_pages pages of page_size tokens in each layer; requests of up to max_len tokens; max_new: added tokens of all
-        requests in one call (B * (t_max + 1) for a step's); rows: query rows of a sequence, at most."""
+        """Pool of n_pages pages of page_size tokens in each layer; requests of up to max_len tokens (and to the end of their last
+        page); max_new: added tokens of all requests in one call (B * (t_max + 1) for a step's); rows: query rows of a sequence, at
+        most."""
         self.ctx = ctx
-        self.n_layers, self.B, self.Hq, self.Hkv, self.d, self.page_size, self.max_len = n_layers, B, Hq, Hkv, d, page_size, max_len
+        self.n_layers, self.B, self.Hq, self.Hkv, self.d, self.page_size = n_layers, B, Hq, Hkv, d, page_size
+        self.max_len = -(-max_len // page_size) * page_size              # what the table has room for, which is what is granted
         dev, i32 = torch.device(device), torch.int32
         self.pages = torch.zeros((n_layers, n_pages, rb.radar_cache_page_bytes(Hkv, d, page_size)), dtype=torch.uint8, device=dev)
-        self.block_table = torch.full((B, -(-max_len // page_size)), -1, dtype=i32, device=dev)
+        self.block_table = torch.full((B, self.max_len // page_size), -1, dtype=i32, device=dev)
         self.cache_len, self.start = torch.zeros(B, dtype=i32, device=dev), torch.zeros(B + 1, dtype=i32, device=dev)
         self.granted, self.live = torch.zeros(B, dtype=torch.uint8, device=dev), torch.zeros(B, dtype=torch.bool, device=dev)
         self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=dev)           # taken from the top: page 0 first
         self.free_count = torch.full((1,), n_pages, dtype=i32, device=dev)
         self.slots, self.src_row = torch.full((max_new,), -1, dtype=torch.int64, device=dev), torch.zeros(max_new, dtype=i32, device=dev)
-        n = rb.radar_cache_attn_workspace_bytes(ctx, B, Hq, Hkv, d, rows, max_len)
+        n = rb.radar_cache_attn_workspace_bytes(ctx, B, Hq, Hkv, d, rows, self.max_len)
         ws = torch.zeros(n + 255, dtype=torch.uint8, device=dev)
         off = (-ws.data_ptr()) % 256
         self.workspace = ws[off:off + n]

@@ -274,3 +274,35 @@ def test_the_example_with_few_pages_answers_every_request():
     assert int(dec.cache.free_count) == 8 and dec.cache.cache_len.tolist() == [0] * dec.B
     with pytest.raises(RuntimeError, match="pages"):
         D.main(n_pages=1)
+
+
+# ---- bounds of the lengths --------------------------------------------------------------------------------------------------
+def _attend(c, ctx, rows, **kw):
+    import torch
+    g = torch.Generator().manual_seed(9)
+    Q, Kt, Vt = (torch.randn(c.B, rows, h, c.d, generator=g).bfloat16().cuda() for h in (c.Hq, c.Hkv, c.Hkv))
+    O = torch.full_like(Q, 7.0)
+    lse = torch.full((c.B, c.Hq, rows), 7.0, device="cuda")
+    ctx.reset_launch_counts()
+    c.attention(1, Q, Kt, Vt, O, lse, **kw)
+    n = {k: v[0] for k, v in ctx.kernel_stats().items()}
+    return O, lse, (Q, Kt, Vt), n["cache_attention"], n["cache_attention_combine"]
+
+
+@pytest.mark.parametrize("rows", [1, 33])
+def test_a_request_may_fill_its_last_page(ctx, rows):
+    """Capacities that are no multiple of the page size: what is granted can be attended to."""
+    c = _cache(ctx, B=1, page_size=64, max_len=100, Hq=4, n_pages=3)
+    rows_in = _rows(11, 2, 120, 2, 64)
+    c.admit(_i32([120]), *rows_in)
+    ctx.check_device_status()
+    if c.granted.tolist() == [0]:
+        return
+    O, lse, (Q, Kt, Vt), _, _ = _attend(c, ctx, rows)
+    ctx.check_device_status()
+    q, kt, vt = (x[0].double().cpu().numpy() for x in (Q, Kt, Vt))
+    k, v = (np.concatenate([_held(x)[1], t]) for x, t in zip(rows_in, (kt, vt)))
+    see = np.concatenate([np.ones((rows, 120), bool), np.tril(np.ones((rows, rows), bool))], 1)
+    o, _ = C.attention(q, k, v, see, 64 ** -0.5)
+    size, _ = C.attention(q, k, np.abs(v), see, 64 ** -0.5)
+    assert np.all(np.abs(O[0].double().cpu().numpy() - o) <= 1.2 * 2.0 ** -7 * size)
