@@ -72,10 +72,13 @@ class FourBitCache:
         self._extend(torch.where(finished != 0, -self.cache_len, 0).to(torch.int32))
         self.live &= finished == 0
 
-    def attention(self, layer, Q, Kt, Vt, O, lse=None, mask=None, n_nodes=None, scale=0.0):
-        """radar_cache_attention over one layer's pool: Q [B, rows, Hq, d], Kt and Vt [B, rows, Hkv, d], the rows' own keys and values."""
+    def attention(self, layer, Q, Kt, Vt, O, lse=None, mask=None, n_nodes=None, scale=0.0, max_cache_len=None):
+        """radar_cache_attention over one layer's pool: Q [B, rows, Hq, d], Kt and Vt [B, rows, Hkv, d], the rows' own keys and values.
+        max_cache_len: a bound of the lengths, if the caller has a nearer one than the cache's capacity; the form that takes the
+        call goes by it (one request of 2048 tokens in a cache for 32768, 32 / 8 heads of 128, one row: 14.4 us, with its length as the
+        bound 6.8; 64 rows over 300 tokens 22 and 10)."""
         rb.radar_cache_attention(self.ctx, Q=Q, Kt=Kt, Vt=Vt, pages=self.pages[layer], page_size=self.page_size, block_table=self.block_table,
-                                 cache_len=self.cache_len, max_cache_len=self.max_len, O=O, lse=lse, mask=mask, n_nodes=n_nodes,
+                                 cache_len=self.cache_len, max_cache_len=self.max_len if max_cache_len is None else max_cache_len, O=O, lse=lse, mask=mask, n_nodes=n_nodes,
                                  workspace=self.workspace, scale=scale)
 
     def load(self, first, start, K, V):

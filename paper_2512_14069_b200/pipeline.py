@@ -225,9 +225,9 @@ class SpecStep:
             mask=self.tree_mask if mask is None else mask, n_nodes=self.n_nodes if n_nodes is None else n_nodes,
             O=self.O, lse=self.lse, workspace=self.ws_attn, block_table=block_table, page_size=page_size)
 
-    def attention_cached(self, cache, layer, Q, Kt, Vt):
+    def attention_cached(self, cache, layer, Q, Kt, Vt, max_cache_len=None):
         """The tree's attention in one layer over a `cache.FourBitCache` of the step's requests."""
-        cache.attention(layer, Q, Kt, Vt, self.O, self.lse, mask=self.tree_mask, n_nodes=self.n_nodes)
+        cache.attention(layer, Q, Kt, Vt, self.O, self.lse, mask=self.tree_mask, n_nodes=self.n_nodes, max_cache_len=max_cache_len)
 
     def accept(self, target_logits, draft_logits=None, u_accept=None, u_sample=None):
         rb.radar_verify_accept(

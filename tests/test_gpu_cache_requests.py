@@ -289,6 +289,21 @@ def _attend(c, ctx, rows, **kw):
     return O, lse, (Q, Kt, Vt), n["cache_attention"], n["cache_attention_combine"]
 
 
+@pytest.mark.parametrize("rows", [1, 9, 64])
+def test_a_bound_of_the_lengths_may_be_given(ctx, rows):
+    """Which form takes a call goes by it: a short request in a cache made for long ones runs as one among short ones."""
+    c = _cache(ctx, B=1, max_len=32768, Hq=8, d=128)
+    c.admit(_i32([300]), *_rows(10, 2, 300, 2, 128))
+    O, lse, _, one, joined = _attend(c, ctx, rows)
+    O2, lse2, _, one2, joined2 = _attend(c, ctx, rows, max_cache_len=300)
+    ctx.check_device_status()
+    assert (one, joined) == (1, 1) and (one2, joined2) == (1, 0)
+    # each is off by up to 1.1 2^-7 sum p |v| <= 1.1 2^-7 max |v|; normal rows lie within 6
+    assert float((O.float() - O2.float()).abs().max()) <= 2.2 * 2.0 ** -7 * 6 and float((lse - lse2).abs().max()) <= 1e-4
+    _attend(c, ctx, rows, max_cache_len=299)
+    assert ctx.read_device_status() == -1
+
+
 @pytest.mark.parametrize("rows", [1, 33])
 def test_a_request_may_fill_its_last_page(ctx, rows):
     """Capacities that are no multiple of the page size: what is granted can be attended to."""
