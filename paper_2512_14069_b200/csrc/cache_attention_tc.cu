@@ -892,10 +892,13 @@ int launch_tc(radar_ctx* ctx, const radar_cache_attn_args& c, TcParams& P, cudaS
     using SM = Smem<D, TWO>;
     CUtensorMap tmQ, tmKt, tmVt, tmCache;
     const long long tree_rows = (long long)c.B * c.rows;
+    // Without a pool nothing is loaded through its map, which still has to lie over memory that is there: some of the tree's keys.
+    const bool pool = c.pages != nullptr && c.n_pages > 0;
+    const long long blocks = pool ? (long long)c.n_pages * c.Hkv * P.blocks_per_page : 1;
     if (!make_map(&tmQ, c.Q, D, c.Hq, tree_rows, P.G, P.nodes_per_rb, 1, 0, c.q_row_stride) ||
         !make_map(&tmKt, c.Kt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride) ||
         !make_map(&tmVt, c.Vt, D, c.Hkv, tree_rows, 1, kTreeKeys, 1, 0, c.kv_row_stride) ||
-        !make_cache_map<D>(&tmCache, c.pages, std::max<long long>(c.n_pages, 1) * c.Hkv * P.blocks_per_page, std::min(P.blocks_per_page, kTileBlocks)))
+        !make_cache_map<D>(&tmCache, pool ? c.pages : c.Kt, blocks, std::min(P.blocks_per_page, kTileBlocks)))
         return RADAR_ERR_CUDA;
     auto* const kernel = cache_attn_tc_kernel<D, TWO>;
     RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_ATTN_TC + 2 * (D == 128) + TWO, kernel, (size_t)SM::kDynamic));
