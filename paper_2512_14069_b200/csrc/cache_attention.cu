@@ -79,11 +79,14 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-// m ln 2 + ln l, m in log2 units
+// m ln 2 + ln l, m in log2 units; a row that attends to nothing (l = 0) has -inf
 __device__ __forceinline__ float lse_of(float m, float l) {
     constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
-    return fmaf(m, kHi, fmaf(m, kLo, logf(l)));
+    return l == 0.f ? -CUDART_INF_F : fmaf(m, kHi, fmaf(m, kLo, logf(l)));
 }
+// ... and 0 for O.  A score that is NaN makes l NaN, and where shares are joined a weight of 0 keeps it so, whatever their maxima
+// (which a NaN does not move): the row's O and lse are NaN however its keys were shared out.
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
 // What a warp keeps of its rows.  Thread (g, q) has rows 2q and 2q + 1 of each tile of eight.
 template <int D, int NT>
 struct State {
@@ -585,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NT)) cache_attn_kernel
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) {
                     const float2 ml = s_ml[w][r];
-                    l += ml.x == -CUDART_INF_F ? 0.f : ml.y * ex2(ml.x - m);
+                    l = fmaf(ml.y, ml.x == -CUDART_INF_F ? 0.f : ex2(ml.x - m), l);
                     const float4 x = *reinterpret_cast<const float4*>(s_o + (w * 8 * NT + r) * SP::kHalf + c4);
                     o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
                 }
@@ -593,10 +596,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NT)) cache_attn_kernel
                 const int node = row / P.G, hq = h * P.G + row - node * P.G;
                 const bool first = half == 0 && c4 == 0;
                 if (whole) {
-                    const float inv = l > 0.f ? 1.f / l : 0.f;
+                    const float inv = inverse(l);
                     *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * a.rows + node) * a.Hq + hq) * D + c) =
                         make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
-                    if (first && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = l > 0.f ? lse_of(m, l) : -CUDART_INF_F;
+                    if (first && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
                 } else {
                     const int64_t rec = ((int64_t)blockIdx.x * 2 + (cur.k0 == 0)) * (8 * NT) + r;
                     *reinterpret_cast<float4*>(P.part_o + rec * D + c) = o;
@@ -729,10 +732,10 @@ __global__ void __launch_bounds__(kThreads) cache_attn_small_kernel(const CacheA
         const int row = row0 + r;
         if (row >= R) return;
         const int node = row / P.G, hq = h * P.G + row - node * P.G;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = inverse(l);
         *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * a.rows + node) * a.Hq + hq) * D + c) =
             make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
-        if (c == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = l > 0.f ? lse_of(m, l) : -CUDART_INF_F;
+        if (c == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
     };
     for (int i = tid; i < 8 * NT * (D / 4); i += kThreads) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -803,7 +806,6 @@ __global__ void __launch_bounds__(128) cache_combine_kernel(const CacheAttnParam
         if (j <= last && (j == first || items_before(range * j, start, s.stages) < items_before(range * (j + 1), start, s.stages)))
             ml = P.part_ml[((int64_t)j * 2 + (j == first)) * (8 * NT) + r];
         const float m2 = fmaxf(m, warp_max(ml.x));
-        if (m2 == -CUDART_INF_F) continue;
         const float old = m == -CUDART_INF_F ? 0.f : ex2(m - m2), w = ml.x == -CUDART_INF_F ? 0.f : ex2(ml.x - m2);
         m = m2;
         l = l * old + warp_sum(ml.y * w);
@@ -834,11 +836,11 @@ __global__ void __launch_bounds__(128) cache_combine_kernel(const CacheAttnParam
                 for (int e = 0; e < E; ++e) o[e] = fmaf(v[k][e], wk[k], o[e]);
         }
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = inverse(l);
     uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.O) + item * D + lane * E);
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) to[e] = pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-    if (lane == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = l > 0.f ? lse_of(m, l) : -CUDART_INF_F;
+    if (lane == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
 }
 
 // Row tiles of eight in a warp, and blocks: as many as are resident, each with a stage for every warp at least.

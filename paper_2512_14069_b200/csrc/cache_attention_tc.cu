@@ -422,7 +422,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         l_out = ml0.y * w0 + ml1.y * w1;
                     }
                     const float m_safe = m_out == -CUDART_INF_F ? 0.f : m_out;
-                    const float inv = final_rows ? (l_out > 0.f ? 1.f / l_out : 0.f) : 1.f;
+                    const float inv = final_rows ? (l_out == 0.f ? 0.f : 1.f / l_out) : 1.f;        // (NaN stays NaN)
                     const int node = (pp * P.n_blk + blk) * P.nodes_per_rb + rb_node;
                     const int hq = s.g * G + row - rb_node * G;
                     const int64_t out_row = ((int64_t)s.b * P.nodes + node) * a.Hq + hq;
@@ -470,7 +470,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     if (row_live) {
                         const float m_nat = m_safe * 0.6931471805599453f;
                         if (final_rows) {
-                            if (a.lse != nullptr) a.lse[((int64_t)s.b * a.Hq + hq) * P.nodes + node] = l_out > 0.f ? m_nat + logf(l_out) : -CUDART_INF_F;
+                            if (a.lse != nullptr) a.lse[((int64_t)s.b * a.Hq + hq) * P.nodes + node] = l_out == 0.f ? -CUDART_INF_F : m_nat + logf(l_out);
                         } else {
                             P.part_ml[rec] = make_float2(m_out == -CUDART_INF_F ? m_out : m_nat, l_out);
                         }
@@ -848,7 +848,11 @@ __global__ void __launch_bounds__(256, 6) cache_tc_combine_kernel(const TcParams
             }
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) m2 = fmaxf(m2, ml[j].x);
-            if (m2 == -CUDART_INF_F) continue;
+            if (m2 == -CUDART_INF_F) {                                             // all sums are 0, or NaN from a NaN among the scores
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) l += ml[j].y;
+                continue;
+            }
             const float old = __expf(m - m2);
             m = m2;
             l *= old;
@@ -856,7 +860,10 @@ __global__ void __launch_bounds__(256, 6) cache_tc_combine_kernel(const TcParams
             for (int e = 0; e < E; ++e) o[e] *= old;
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
-                if (ml[j].x == -CUDART_INF_F) continue;
+                if (ml[j].x == -CUDART_INF_F) {
+                    l += ml[j].y;
+                    continue;
+                }
                 const float w = __expf(ml[j].x - m);
                 l = fmaf(ml[j].y, w, l);
                 const float* x = reinterpret_cast<const float*>(&v[j]);
@@ -866,14 +873,14 @@ __global__ void __launch_bounds__(256, 6) cache_tc_combine_kernel(const TcParams
         }
         const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
         const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         __nv_bfloat162 w[E / 2];
 #pragma unroll
         for (int e = 0; e < E; e += 2) w[e / 2] = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
         __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * P.nodes + node) * a.Hq + hq) * D + lane * E;
         if (E == 4) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(w);
         else *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(w);
-        if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * P.nodes + node] = l > 0.f ? m + logf(l) : -CUDART_INF_F;
+        if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * P.nodes + node] = l == 0.f ? -CUDART_INF_F : m + logf(l);
     }
 }
 

@@ -6,6 +6,7 @@ import pytest
 from oracle import cache_oracle as C
 
 pytestmark = pytest.mark.gpu
+FAR = 40000          # a bound of the lengths that leaves nothing to clusters
 
 
 @pytest.fixture(scope="module")
@@ -39,3 +40,60 @@ def test_attention_over_an_empty_pool(ctx, B, Hq, Hkv, d, rows):
         move = 2.0 ** -23 * d ** 0.5 * np.abs(q).max() * np.abs(k).max()
         assert np.all(np.abs(O[b].double().cpu().numpy() - o) <= (1.1 * 2.0 ** -7 + 2 * move) * size)
         assert np.all(np.abs(lse[b].double().cpu().numpy() - l) <= 2.0 ** -20 + move + 2.0 ** -23 * np.abs(l))
+
+
+# ---- infinities and NaN ---------------------------------------------------------------------------------------------------------
+FORMS = [([300, 20], 1, None), ([300, 20], 12, None), ([300, 20], 64, None), ([9000, 100], 1, FAR), ([9000, 100], 7, FAR), ([9000, 100], 64, FAR), ([100, 30], 64, FAR)]
+
+
+def _run(ctx, kw, **changed):
+    from paper_2512_14069_b200 import binding as rb
+    kw["O"].fill_(7.0), kw["lse"].fill_(7.0)
+    rb.radar_cache_attention(ctx, **dict(kw, **changed))
+    ctx.check_device_status()
+    return kw["O"].double().cpu().numpy(), kw["lse"].double().cpu().numpy()
+
+
+@pytest.mark.parametrize("lens,rows,max_len", FORMS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_row_of_nan_is_nan_and_the_others_are_not(ctx, lens, rows, max_len, d):
+    """However its keys are shared out: O and lse of that row and head, and no others."""
+    import cache_harness as T
+    kw = T.check_attention(ctx, np.random.default_rng(41), lens, 8, 2, d, 16, rows, max_len=max_len)
+    lse0 = kw["lse"].double().cpu().numpy()
+    Q = kw["Q"].clone()
+    Q[0, rows - 1, 5, 3] = float("nan")
+    O, lse = _run(ctx, kw, Q=Q)
+    assert np.isnan(O[0, rows - 1, 5]).all() and np.isnan(lse[0, 5, rows - 1])
+    hit = np.zeros(O.shape[:3], bool)
+    hit[0, rows - 1, 5] = True
+    for b in range(2):
+        o, bound = T.held_to[b]
+        assert np.all((np.abs(O[b] - o) <= bound)[~hit[b]])
+    at = ~hit.transpose(0, 2, 1)
+    assert np.all(np.abs(lse - lse0)[at] <= 2e-4)            # twice 2^-20 + 2^-23 d max|q| max|k| / sqrt(d) + 2^-23 |lse|, with |q| < 6, |k| < 8, |lse| < 100
+
+
+@pytest.mark.parametrize("lens,rows,max_len", FORMS)
+def test_keys_that_are_infinite(ctx, lens, rows, max_len):
+    """A score of +inf leaves a row without a value, one of -inf takes the key from it, as in the definition."""
+    import torch
+    import cache_harness as T
+    kw = T.check_attention(ctx, np.random.default_rng(43), lens, 8, 2, 128, 16, rows, max_len=max_len)
+    Kt = kw["Kt"].clone()
+    Kt[0, 0, 1, 9] = float("inf")                            # of the root, which all rows see
+    O, lse = _run(ctx, kw, Kt=Kt)
+    q = kw["Q"][0].double().cpu().numpy()
+    see = np.ones(rows, bool)
+    plus = see[:, None] & (q[:, :, 9] > 0) & (np.arange(8) >= 4)[None]
+    assert plus.any() and np.array_equal(np.isnan(O[0]).all(-1), plus) and np.array_equal(np.isnan(O[0]).any(-1), plus)
+    assert not np.isfinite(lse[0].T[plus]).any() and np.isfinite(lse[0].T[~plus]).all()
+    # the others: as if the key were hidden from them
+    hidden = kw["mask"].clone()
+    hidden[0] &= ~1
+    O2, lse2 = _run(ctx, kw, mask=hidden)
+    minus = see[:, None] & (q[:, :, 9] < 0) & (np.arange(8) >= 4)[None]
+    most = 2 * 1.1 * 2.0 ** -7 * 8                           # of two results, |v| < 8
+    assert np.all(np.abs(O[0] - O2[0])[minus] <= most)
+    o, bound = T.held_to[0]
+    assert np.all((np.abs(O[0] - o) <= bound)[~plus & ~minus])
