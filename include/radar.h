@@ -510,7 +510,9 @@ int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* args, void* st
  * tokens); q_row_stride and kv_row_stride: elements between consecutive rows of Q, and of Kt and Vt (rows of a fused projection
  * are read in place; the rows of a sequence follow those of the one before), O is contiguous.  Row i < n_nodes[b] attends to the
  * prefix [0, cache_len[b]) and to the tree rows t < n_nodes[b] with bit t of mask[b][i] set (mask NULL: t <= i, a chain).
- * Rows i >= n_nodes[b] of O and lse are left untouched; a row that attends to nothing gets 0, and lse -inf.
+ * Rows i >= n_nodes[b] of O and lse are left untouched; a row that attends to nothing gets 0, and lse -inf.  Keys that a row does not
+ * attend to may hold anything; values of the rows t < n_nodes[b] have to be finite, as a probability of 0 times infinity or NaN is
+ * NaN (in that channel, for all rows of the sequence and KV head).
  * lse (optional) [B][Hq][rows].  scale <= 0 selects 1/sqrt(d).  Products are accumulated in fp32; the probabilities enter P V as
  * bf16.  max_cache_len (host) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes is out of range
  * records RADAR_ERR_INVALID_ARG and is skipped; a page outside the pool records it too and is read as page 0.

@@ -1,5 +1,7 @@
 """Values and shapes at the edge of what the 4-bit cache's attention takes: empty pools, scales from end to end, infinities and NaN in
 Q, K and V, many sequences, layouts whose strides differ where they count for nothing."""
+import functools
+
 import numpy as np
 import pytest
 
@@ -42,6 +44,31 @@ def test_attention_over_an_empty_pool(ctx, B, Hq, Hkv, d, rows):
         assert np.all(np.abs(lse[b].double().cpu().numpy() - l) <= 2.0 ** -20 + move + 2.0 ** -23 * np.abs(l))
 
 
+# ---- scales -----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [1, 7, 64])
+@pytest.mark.parametrize("max_len", [None, FAR])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_from_the_smallest_to_the_largest(ctx, monkeypatch, rows, max_len, d):
+    """Scale bytes 0 to 255 (values from 2^-20 to 30720) side by side, and pools of one end alone."""
+    import cache_harness as T
+    whole = T.random_pool
+    for i, (lo, hi, gain) in enumerate(((0, 256, 2.0 ** -8), (0, 1, 1.0), (255, 256, 2.0 ** -12))):
+        monkeypatch.setattr(T, "random_pool", functools.partial(whole, lo=lo, hi=hi))
+        T.check_attention(ctx, np.random.default_rng(31 + i), [700, 33], 8, 2, d, 32, rows, max_len=max_len, gain=gain)
+
+
+# ---- many sequences -----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("B,Hq,Hkv,d,rows", [(97, 8, 2, 64, 1), (133, 4, 1, 128, 8), (130, 8, 2, 64, 20), (161, 8, 8, 128, 50)])
+@pytest.mark.parametrize("max_len", [None, FAR])
+def test_attention_of_more_sequences_than_a_warp_has_lanes(ctx, B, Hq, Hkv, d, rows, max_len):
+    import cache_harness as T
+    rng = np.random.default_rng(B)
+    lens, n = rng.integers(0, 90, B), rng.integers(0, rows + 1, B)
+    lens[::5], n[::6], lens[-1] = 0, 0, 600
+    n[-1] = rows
+    T.check_attention(ctx, rng, list(lens), Hq, Hkv, d, 16, rows, n_nodes=n, max_len=max_len)
+
+
 # ---- infinities and NaN ---------------------------------------------------------------------------------------------------------
 FORMS = [([300, 20], 1, None), ([300, 20], 12, None), ([300, 20], 64, None), ([9000, 100], 1, FAR), ([9000, 100], 7, FAR), ([9000, 100], 64, FAR), ([100, 30], 64, FAR)]
 
@@ -74,6 +101,24 @@ def test_a_row_of_nan_is_nan_and_the_others_are_not(ctx, lens, rows, max_len, d)
     assert np.all(np.abs(lse - lse0)[at] <= 2e-4)            # twice 2^-20 + 2^-23 d max|q| max|k| / sqrt(d) + 2^-23 |lse|, with |q| < 6, |k| < 8, |lse| < 100
 
 
+@pytest.mark.parametrize("lens,rows,max_len", [f for f in FORMS if f[1] > 1])
+@pytest.mark.parametrize("value", ["nan", "inf", "-inf"])
+def test_a_key_that_no_row_sees_is_not_there(ctx, lens, rows, max_len, value):
+    """Whatever it is: the same bits as with zeros in its place."""
+    import torch
+    import cache_harness as T
+    kw = T.check_attention(ctx, np.random.default_rng(42), lens, 8, 2, 128, 16, rows, max_len=max_len)
+    t = rows - 3
+    mask = kw["mask"] & ~(1 << t)
+    Kt = kw["Kt"].clone()
+    Kt[:, t] = 0.0
+    want = _run(ctx, kw, mask=mask, Kt=Kt)
+    Kt[:, t] = float(value)
+    got = _run(ctx, kw, mask=mask, Kt=Kt)
+    assert np.isfinite(want[0]).all()
+    assert np.array_equal(want[0], got[0]) and np.array_equal(want[1], got[1])
+
+
 @pytest.mark.parametrize("lens,rows,max_len", FORMS)
 def test_keys_that_are_infinite(ctx, lens, rows, max_len):
     """A score of +inf leaves a row without a value, one of -inf takes the key from it, as in the definition."""
@@ -97,3 +142,21 @@ def test_keys_that_are_infinite(ctx, lens, rows, max_len):
     assert np.all(np.abs(O[0] - O2[0])[minus] <= most)
     o, bound = T.held_to[0]
     assert np.all((np.abs(O[0] - o) <= bound)[~plus & ~minus])
+
+
+@pytest.mark.parametrize("lens,rows,max_len", FORMS)
+def test_a_value_of_nan_reaches_its_head_and_no_other(ctx, lens, rows, max_len):
+    """A probability of zero does not hide it: V of a live node has to be finite.  Other KV heads and sequences do not see it."""
+    import cache_harness as T
+    kw = T.check_attention(ctx, np.random.default_rng(44), lens, 8, 2, 64, 16, rows, max_len=max_len)
+    Vt = kw["Vt"].clone()
+    Vt[0, rows - 1, 1, 7] = float("nan")
+    O, lse = _run(ctx, kw, Vt=Vt)
+    o, bound = T.held_to[0]
+    assert np.isnan(O[0, rows - 1, 4:, 7]).all()
+    hit = np.zeros(O.shape[1:], bool)
+    hit[:, 4:, 7] = True
+    assert np.all((np.abs(O[0] - o) <= bound)[~hit])
+    o, bound = T.held_to[1]
+    assert np.all(np.abs(O[1] - o) <= bound)
+    assert np.isfinite(lse).all()
