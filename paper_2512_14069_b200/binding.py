@@ -602,9 +602,9 @@ def radar_cache_extend(ctx: Context, *, page_size, cache_len, new_len, block_tab
 
 
 def radar_cache_store(ctx: Context, *, K, V, slots, pages, page_size, src_row=None, stream=None):
-    """Rows of K and V ([rows, Hkv, d], or [layers, rows, Hkv, d] for all layers at once; float32 or bfloat16, any strides between
-    rows and layers) into the slots of `pages` (uint8, [n_pages, page bytes] or with a leading layer dimension).  Token i is row
-    src_row[i], or row i."""
+    """Rows of K and V ([rows, Hkv, d], or [layers, rows, Hkv, d] for all layers at once; float32 or bfloat16; between rows and
+    layers any strides that K and V share) into the slots of `pages` (uint8, [n_pages, page bytes] or with a leading layer
+    dimension).  Token i is row src_row[i], or row i."""
     _cache_store(ctx, stream, K, V, slots, pages, page_size, src_row)
 
 

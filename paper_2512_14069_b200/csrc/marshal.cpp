@@ -215,6 +215,12 @@ void* strided_rows(const at::Tensor& t, int64_t dims, const char* name) {
     }
     return t.data_ptr();
 }
+// (tensors of one shape; the stride of a dimension of one element leads nowhere)
+bool same_strides(const at::Tensor& x, const at::Tensor& y) {
+    for (int64_t i = 0; i < x.dim(); ++i)
+        if (x.size(i) > 1 && x.stride(i) != y.stride(i)) return false;
+    return true;
+}
 int dtype_code(const at::Tensor& t) {
     if (t.scalar_type() == at::kFloat) return RADAR_F32;
     if (t.scalar_type() == at::kBFloat16) return RADAR_BF16;
@@ -300,7 +306,7 @@ PyObject* cache_store(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return cache_call(args, n, 9, [](PyObject* const* v) {
         radar_cache_store_args a = {};
         const at::Tensor &K = *tensor(v[0], "K"), &V = *tensor(v[1], "V"), *slots, *src;
-        need((K.dim() == 3 || K.dim() == 4) && K.sizes() == V.sizes() && K.scalar_type() == V.scalar_type() && K.strides() == V.strides(),
+        need((K.dim() == 3 || K.dim() == 4) && K.sizes() == V.sizes() && K.scalar_type() == V.scalar_type() && same_strides(K, V),
              "K and V must share shape, dtype and strides");
         const bool layers = K.dim() == 4;
         const int64_t rows = K.size(-3), Hkv = K.size(-2), d = K.size(-1);
@@ -317,7 +323,7 @@ PyObject* cache_store(PyObject*, PyObject* const* args, Py_ssize_t n) {
         a.n_tokens = slots->numel();
         a.n_rows = rows;
         a.row_stride = rows > 1 ? K.stride(-3) : Hkv * d;
-        a.row_layer_stride = layers ? K.stride(0) : 0;
+        a.row_layer_stride = a.n_layers > 1 ? K.stride(0) : 0;
         need((src == nullptr ? rows : src->numel()) >= a.n_tokens, "fewer rows (or entries of src_row) than slots");
         const Pool p = pool(v[3], a.page_size, Hkv, d, a.n_layers);
         a.pages = p.p; a.n_pages = p.n_pages; a.page_layer_stride = p.layer_bytes;
@@ -367,7 +373,7 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const int64_t B = Q.size(0), rows = Q.size(1), Hq = Q.size(2), Hkv = Kt.size(2), d = Q.size(3);
         need(B <= INT_MAX && rows <= INT_MAX && Hq <= INT_MAX && d <= INT_MAX, "Q: too large");
         a.O = packed(v[8], "O", at::kBFloat16, false, &O);
-        need(Kt.sizes() == Vt.sizes() && Kt.size(0) == B && Kt.size(1) == rows && Kt.size(3) == d && O->sizes() == Q.sizes() && Kt.strides() == Vt.strides(),
+        need(Kt.sizes() == Vt.sizes() && Kt.size(0) == B && Kt.size(1) == rows && Kt.size(3) == d && O->sizes() == Q.sizes() && same_strides(Kt, Vt),
              "Q, O, Kt and Vt disagree in shape or strides");
         need(B == 1 || rows == 1 || (Q.stride(0) == rows * Q.stride(1) && Kt.stride(0) == rows * Kt.stride(1)),
              "Q, Kt, Vt: the rows of a sequence must follow those of the one before");

@@ -160,3 +160,28 @@ def test_a_value_of_nan_reaches_its_head_and_no_other(ctx, lens, rows, max_len):
     o, bound = T.held_to[1]
     assert np.all(np.abs(O[1] - o) <= bound)
     assert np.isfinite(lse).all()
+
+
+# ---- layouts ----------------------------------------------------------------------------------------------------------------------
+def test_strides_of_dimensions_of_one_element_do_not_matter(ctx):
+    """Keys as [B, heads, rows, d] with one row, values as [B, rows, heads, d]: alike in memory."""
+    import torch
+    import cache_harness as T
+    from paper_2512_14069_b200 import binding as rb
+    kw = T.check_attention(ctx, np.random.default_rng(51), [100, 7, 40], 8, 2, 64, 16, 1)
+    first = kw["O"].clone()
+    Kt = torch.empty_strided(kw["Kt"].shape, (2 * 64, 64, 64, 1), dtype=torch.bfloat16, device="cuda").copy_(kw["Kt"])
+    assert Kt.stride() != kw["Vt"].stride()
+    kw["O"].zero_()
+    rb.radar_cache_attention(ctx, **dict(kw, Kt=Kt))
+    ctx.check_device_status()
+    assert torch.equal(kw["O"], first)
+    K = torch.randn(1, 5, 3, 64, device="cuda")
+    V = torch.empty_strided(K.shape, (7, 192, 64, 1), device="cuda").copy_(torch.randn_like(K))      # one layer
+    pool = torch.zeros(1, 1, 3 * 18 * 64, dtype=torch.uint8, device="cuda")
+    rb.radar_cache_store(ctx, K=K, V=V, slots=torch.arange(5, device="cuda"), pages=pool, page_size=16)
+    K2, V2 = torch.zeros_like(K), torch.zeros(1, 5, 3, 64, device="cuda")
+    rb.radar_cache_load(ctx, pages=pool, page_size=16, block_table=T.dev([[0]], torch.int32), first=T.dev([0], torch.int32), start=T.dev([0, 5], torch.int32), K=K2, V=V2)
+    ctx.check_device_status()
+    for x, y in ((K, K2), (V, V2)):
+        assert np.array_equal(y.double().cpu().numpy(), C.values(*C.quantise(x.double().cpu().numpy())))
