@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NT)) cache_attn_kernel
             out[c] = 0;
             if (i + lane < far_n && (blk + c) * kBlock < far.len) {
                 const int index = P.page_shift_blocks >= 0 ? (blk + c) >> P.page_shift_blocks : (blk + c) / P.blocks_per_page;
-                int page = __ldg(a.block_table + (int64_t)far.b * a.max_pages + index);
+                int page = a.block_table[(int64_t)far.b * a.max_pages + index];
                 if (page < 0 || page >= a.n_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
                 out[c] = (page * a.Hkv + far.h) * P.blocks_per_page + blk + c - index * P.blocks_per_page;
             }

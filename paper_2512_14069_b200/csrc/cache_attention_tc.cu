@@ -552,7 +552,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 const int blk = key0 / kBlock + lane * per;
                 if (blk * kBlock >= key_end) return 0;
                 const int index = P.page_shift_blocks >= 0 ? blk >> P.page_shift_blocks : blk / P.blocks_per_page;
-                int page = __ldg(a.block_table + (long long)b * a.max_pages + index);
+                int page = a.block_table[(long long)b * a.max_pages + index];
                 if (page < 0 || page >= P.n_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
                 return (page * a.Hkv + g) * P.blocks_per_page + blk - index * P.blocks_per_page;
             };

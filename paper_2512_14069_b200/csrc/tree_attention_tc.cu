@@ -483,7 +483,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                             n_ld = (min(kTileKeys, Pb - t * kTileKeys) + per - 1) >> box_shift;
                             if (lane < n_ld) {
                                 const int index = first_page(t) + lane;
-                                int page = __ldg(a.block_table + (long long)b * a.max_pages + index);
+                                int page = a.block_table[(long long)b * a.max_pages + index];
                                 if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
                                 page_row = page * a.page_size + (tiles_per_page > 1 ? (t - index * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
                             }
@@ -956,7 +956,7 @@ tree_attn_tc_fine_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                         __syncwarp();
                         if (const int p = lane; p < n_ld) {
                             const int key = key0 + p * per;
-                            long long page = __ldg(a.block_table + (long long)b * a.max_pages + key / ps);
+                            long long page = a.block_table[(long long)b * a.max_pages + key / ps];
                             if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
                             const int row = (int)(page * ps + key % ps);
                             for (int h = 0; h < H; ++h)
