@@ -60,11 +60,6 @@ constexpr float kMove = 8.f;         // log2 units
 // rows over 300 tokens 11 us (20), one sequence of 1000 tokens, 256 rows 14 us (17).
 constexpr int kTokenRows = 32;
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -79,14 +74,10 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-// m ln 2 + ln l, m in log2 units; a row that attends to nothing (l = 0) has -inf
-__device__ __forceinline__ float lse_of(float m, float l) {
-    constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
-    return l == 0.f ? -CUDART_INF_F : fmaf(m, kHi, fmaf(m, kLo, logf(l)));
-}
-// ... and 0 for O.  A score that is NaN makes l NaN, and where shares are joined a weight of 0 keeps it so, whatever their maxima
+// A row that attends to nothing (l = 0) has 0 in O and lse = -inf.  A score that is NaN makes l NaN, and where shares are joined a weight of 0 keeps it so, whatever their maxima
 // (which a NaN does not move): the row's O and lse are NaN however its keys were shared out.
 __device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -CUDART_INF_F : lse_of(m, l); }
 // What a warp keeps of its rows.  Thread (g, q) has rows 2q and 2q + 1 of each tile of eight.
 template <int D, int NT>
 struct State {
@@ -599,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NT)) cache_attn_kernel
                     const float inv = inverse(l);
                     *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * a.rows + node) * a.Hq + hq) * D + c) =
                         make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
-                    if (first && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
+                    if (first && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = row_lse(m, l);
                 } else {
                     const int64_t rec = ((int64_t)blockIdx.x * 2 + (cur.k0 == 0)) * (8 * NT) + r;
                     *reinterpret_cast<float4*>(P.part_o + rec * D + c) = o;
@@ -735,7 +726,7 @@ __global__ void __launch_bounds__(kThreads) cache_attn_small_kernel(const CacheA
         const float inv = inverse(l);
         *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.O) + (((int64_t)b * a.rows + node) * a.Hq + hq) * D + c) =
             make_uint2(pack(o.x * inv, o.y * inv), pack(o.z * inv, o.w * inv));
-        if (c == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
+        if (c == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = row_lse(m, l);
     };
     for (int i = tid; i < 8 * NT * (D / 4); i += kThreads) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -840,7 +831,7 @@ __global__ void __launch_bounds__(128) cache_combine_kernel(const CacheAttnParam
     uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.O) + item * D + lane * E);
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) to[e] = pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-    if (lane == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = lse_of(m, l);
+    if (lane == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.Hq + hq) * a.rows + node] = row_lse(m, l);
 }
 
 // Row tiles of eight in a warp, and blocks: as many as are resident, each with a stage for every warp at least.
@@ -889,7 +880,7 @@ int launch(radar_ctx* ctx, const CacheAttnParams& P, cudaStream_t stream) {
         RADAR_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, P));
         return RADAR_OK;
     }
-    RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_ATTN + 4 * (D == 128) + NT - 1, cache_attn_kernel<D, NT>, (size_t)SP::kDynamic));
+    RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CACHE_ATTN + 2 * (D == 128) + NT - 1, cache_attn_kernel<D, NT>, (size_t)SP::kDynamic));
     {
         radar_launch_scope scope(ctx, RADAR_K_CACHE_ATTN, stream);
         RADAR_CUDA_CHECK(launch_chained(cache_attn_kernel<D, NT>, dim3((unsigned)P.blocks), dim3(kThreads), (size_t)SP::kDynamic, stream, P));
@@ -939,7 +930,6 @@ extern "C" int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args
     P.page_shift_blocks = -1;
     for (int s = 0; s < 28; ++s)
         if (P.blocks_per_page == 1 << s) P.page_shift_blocks = s;
-    P.page_bytes = page_bytes(a->Hkv, a->d, a->page_size);
     P.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)a->d)) * 1.4426950408889634f;
     P.status = ctx->d_status;
     const int64_t n = records(ctx, p.nt);

@@ -9,7 +9,6 @@ struct CacheAttnParams {
     int G;
     int blocks, cluster;                         // of the launch; of a unit, in the form for little work
     int blocks_per_page, page_shift_blocks;      // log2 of it, -1: no power of two
-    int64_t page_bytes;
     float scale_log2;
     // [blocks][2][8 or 16 rows]: a block's share of the unit that its range begins in, and of the one that it ends in
     float2* part_ml;                             // (maximum in log2 units, sum)

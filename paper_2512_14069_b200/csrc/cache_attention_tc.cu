@@ -949,9 +949,7 @@ int cache_attn_tc_launch(radar_ctx* ctx, const radar_cache_attn_args* c, cudaStr
     P.status = ctx->d_status;
     P.n_layers = 1;
     P.nodes = c->rows;
-    P.pages = reinterpret_cast<const unsigned char*>(c->pages);
     P.n_pages = c->n_pages;
-    P.page_bytes = page_bytes(c->Hkv, c->d, c->page_size);
     P.blocks_per_page = c->page_size / kBlock;
     P.page_shift_blocks = -1;
     for (int s = 0; s < 28; ++s)

@@ -48,8 +48,8 @@ enum radar_smem_slot {
     RADAR_SMEM_ACCLEN = RADAR_SMEM_WALK + 4,        // the same
     RADAR_SMEM_ATTN_FMA = RADAR_SMEM_ACCLEN + 4,        // + 4 * (bf16) + 2 * (d == 128) + (clusters)
     RADAR_SMEM_ATTN_TC = RADAR_SMEM_ATTN_FMA + 8,   // + 8 * fine + 4 * (d == 128) + 2 * two + paged
-    RADAR_SMEM_CACHE_ATTN = RADAR_SMEM_ATTN_TC + 16,   // + 4 * (d == 128) + row tiles of eight - 1
-    RADAR_SMEM_CACHE_EXTEND = RADAR_SMEM_CACHE_ATTN + 8,   // + (several blocks)
+    RADAR_SMEM_CACHE_ATTN = RADAR_SMEM_ATTN_TC + 16,   // + 2 * (d == 128) + row tiles of eight - 1
+    RADAR_SMEM_CACHE_EXTEND = RADAR_SMEM_CACHE_ATTN + 4,   // + (several blocks)
     RADAR_SMEM_CACHE_ATTN_TC = RADAR_SMEM_CACHE_EXTEND + 2,   // + 2 * (d == 128) + two
     RADAR_SMEM_CACHE_SMALL = RADAR_SMEM_CACHE_ATTN_TC + 4,    // + 2 * (d == 128) + row tiles of eight - 1
     RADAR_SMEM_COUNT = RADAR_SMEM_CACHE_SMALL + 4
@@ -171,6 +171,18 @@ __device__ __forceinline__ void set_status(int* status, int code) { atomicCAS(st
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// 2^x
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// m ln 2 + ln l, m in log2 units
+__device__ __forceinline__ float lse_of(float m, float l) {
+    constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
+    return fmaf(m, kHi, fmaf(m, kLo, logf(l)));
+}
 
 // (value desc, index asc) ordering: true if a precedes b
 __device__ __forceinline__ bool precedes(float va, int ia, float vb, int ib) {

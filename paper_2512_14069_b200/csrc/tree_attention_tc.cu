@@ -51,6 +51,9 @@ static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block sha
 constexpr int kStaticSmem = 3072;    // barriers and exchange arrays: with the tiles exactly the 227 KB a block may have
 constexpr long long kLatencyWork = 9 << 15;   // sequences x query heads x keys x head dimension: tree_attn_tc_supported
 
+template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 template <int D, bool TWO>
 struct Smem {
     static constexpr int kHalves = D / 64;
@@ -1426,6 +1429,120 @@ tree_attn_tc_fine_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         }
         tmem_dealloc(tmem, 512);
     }
+}
+
+// Merges the pieces of the units that were cut across CTAs.  Blocks (c, *): CTA c of the attention kernel holds the first
+// piece of a cut unit (or the blocks exit); the following CTAs of the same class hold the rest, each as its first
+// segment.  A warp merges one query row, every piece of it in flight together: the work is a chain of three trips to L2,
+// and many warps hide it better than many rows a warp do (148 cut units of 256 rows: 17.1 us event-timed with one row a
+// warp, 18.4 with two, 20.6 with four; 72 cut units of 128 rows: 10.0, 10.8, 14.7).
+template <int D, bool FINE>
+__global__ void __launch_bounds__(256) tree_attn_tc_combine_kernel(const TcParams P) {
+    chain_wait();
+    auto weight = [](float d) { return FINE ? ex2(d) : __expf(d); };      // of two pieces' maxima that differ by d
+    const radar_attn_args& a = P.a;
+    const CutUnit& cu = P.cut[blockIdx.x];
+    const int valid = cu.valid, b = cu.b, g = cu.g, layer = cu.layer, slot = cu.slot, rows = cu.rows, n_pieces = cu.n_pieces;
+    const uint32_t live0 = cu.live[0];
+    if (!valid) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = blockIdx.y * 8 + warp;
+    if (r >= rows) return;                                   // rows of a unit are live from 0 up
+    constexpr int E = D / 32;                                // output elements per lane
+    // the row's record in piece j's partials (row blocks start 128 records apart, whatever part of them is live)
+    const int blk = r < P.rb_rows ? 0 : 1, in_blk = r - blk * P.rb_rows;
+    auto rec_of = [&](int j) {
+        const int64_t cta = (int64_t)blockIdx.x + (int64_t)j * P.n_cls;
+        return (cta * 2 + (j == 0 ? slot : 0)) * kPairRows + blk * 128 + in_blk;
+    };
+    auto store_row = [&](const float (&o)[E], float mx, float den) {
+        const float inv = 1.f / den;
+        const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
+        const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.O) + layer * P.o_ls + (((int64_t)b * kMaxNodes + node) * a.Hq + hq) * D + lane * E;
+        __nv_bfloat162 w[E / 2];
+#pragma unroll
+        for (int q = 0; q < E; q += 2) w[q / 2] = __floats2bfloat162_rn(o[q] * inv, o[q + 1] * inv);
+        if (E == 4) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(w);
+        else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(w);
+        if (a.lse != nullptr && lane == 0) a.lse[layer * P.lse_ls + ((int64_t)b * a.Hq + hq) * kMaxNodes + node] = FINE ? lse_of(mx, den) : mx + logf(den);
+    };
+    auto load_row = [&](const float* src, float (&v)[E]) {
+        if (E == 4) {
+            const float4 t = *reinterpret_cast<const float4*>(src);
+            v[0] = t.x; v[1] = t.y; v[E - 2] = t.z; v[E - 1] = t.w;
+        } else {
+            const float2 t = *reinterpret_cast<const float2*>(src);
+            v[0] = t.x; v[1] = t.y;
+        }
+    };
+
+    if (n_pieces <= 4) {
+        // ---- the usual case: a unit spread over a few CTAs.  (A CTA whose range holds no tile start has no piece.) ----
+        float2 ml[4];
+        float v[4][E], o[E];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool on = ((live0 >> j) & 1u) && j < n_pieces;
+            const int64_t rec = rec_of(on ? j : 0);
+            ml[j] = P.part_ml[rec];
+            load_row(P.part_o + rec * D + lane * E, v[j]);
+            if (!on) ml[j] = make_float2(-CUDART_INF_F, 0.f);
+        }
+        const float mx = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+        float den = 0.f;
+#pragma unroll
+        for (int q = 0; q < E; ++q) o[q] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (ml[j].x == -CUDART_INF_F) continue;
+            const float w = weight(ml[j].x - mx);
+            den = fmaf(ml[j].y, w, den);
+#pragma unroll
+            for (int q = 0; q < E; ++q) o[q] = fmaf(v[j][q], w, o[q]);
+        }
+        store_row(o, mx, den);
+        return;
+    }
+
+    // ---- a unit spread over many CTAs (few units, long prefixes): lane j holds piece j's (m, l) ----
+    float den = 0.f, mx = -CUDART_INF_F, o[E];
+#pragma unroll
+    for (int q = 0; q < E; ++q) o[q] = 0.f;
+    for (int j0 = 0; j0 < n_pieces; j0 += 32) {
+        const int jl = j0 + lane;
+        const uint32_t live = cu.live[j0 >> 5];
+        float2 ml = make_float2(-CUDART_INF_F, 0.f);
+        if (jl < n_pieces && ((live >> lane) & 1u)) ml = P.part_ml[rec_of(jl)];
+        const float mnew = fmaxf(mx, warp_max(ml.x));
+        if (mnew == -CUDART_INF_F) continue;
+        const float rescale = weight(mx - mnew);             // 0 on the first live batch
+        den *= rescale;
+#pragma unroll
+        for (int q = 0; q < E; ++q) o[q] *= rescale;
+        mx = mnew;
+        const float wl = ml.x == -CUDART_INF_F ? 0.f : weight(ml.x - mx);
+        den += warp_sum(ml.y * wl);
+        const int nb = min(32, n_pieces - j0);
+        for (int u0 = 0; u0 < nb; u0 += 4) {
+            float v[4][E], w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                w[u] = u0 + u < nb ? __shfl_sync(kFull, wl, u0 + u) : 0.f;
+                if (w[u] != 0.f) {
+                    load_row(P.part_o + rec_of(j0 + u0 + u) * D + lane * E, v[u]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < E; ++q) v[u][q] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int q = 0; q < E; ++q) o[q] = fmaf(v[u][q], w[u], o[q]);
+        }
+    }
+    store_row(o, mx, den);
 }
 
 }  // namespace

@@ -1,6 +1,6 @@
 // The tile space of the tensor-core attention kernels, shared by the bf16 caches (tree_attention_tc.cu) and the 4-bit cache
 // (cache_attention_tc.cu): units of (layer, sequence, KV head, row-block pair), their tiles laid end to end and cut into equal
-// ranges, the pieces' records and their merge, tensor maps and grid.
+// ranges, the pieces' records, tensor maps and grid.
 #pragma once
 #include <cuda.h>
 
@@ -16,7 +16,6 @@ using namespace tc05;
 
 // how the prefix is held: what the tile space has to look up
 enum CacheKind { kContiguous = 0, kPaged = 1, kFourBit = 2 };
-
 
 constexpr int kTileKeys = 128;       // keys per prefix tile
 constexpr int kFirstKeys = 64;       // keys of a tile whose products start before the rest of its probabilities is there
@@ -64,8 +63,7 @@ struct TcParams {
     int* status;
     // the 4-bit cache
     int nodes;           // tree rows of a sequence in Q, O, lse, mask and the tree's K and V (RADAR_MAX_NODES elsewhere)
-    const unsigned char* pages;
-    long long n_pages, page_bytes;
+    long long n_pages;
     int blocks_per_page, page_shift_blocks;      // blocks of 16 tokens of a page, log2 of it or -1
 };
 
@@ -81,12 +79,7 @@ __device__ __forceinline__ void st_global_32b(void* p, const uint32_t (&w)[8]) {
                  "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                  : "memory");
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// the same and the other steps of a probability, kept in the order in which they are written
+// 2^x and the other steps of a probability, kept in the order in which they are written
 __device__ __forceinline__ float ex2_in_order(float x) {
     float y;
     asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -109,13 +102,6 @@ __device__ __forceinline__ uint32_t bf16x2_in_order(float lo, float hi) {
     uint32_t d;
     asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
-}
-template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// m ln 2 + ln l, m in log2 units
-__device__ __forceinline__ float lse_of(float m, float l) {
-    constexpr float kHi = 0.693147182f, kLo = (float)(0.6931471805599453 - (double)kHi);
-    return fmaf(m, kHi, fmaf(m, kLo, logf(l)));
 }
 
 // ---- the tile space of one class (unit index pp within a KV head) ---------------------------------
@@ -296,120 +282,6 @@ struct __align__(16) Segment {
     int b, g, layer;
     int pad[3];
 };
-
-// Merges the pieces of the units that were cut across CTAs.  Blocks (c, *): CTA c of the attention kernel holds the first
-// piece of a cut unit (or the blocks exit); the following CTAs of the same class hold the rest, each as its first
-// segment.  A warp merges one query row, every piece of it in flight together: the work is a chain of three trips to L2,
-// and many warps hide it better than many rows a warp do (148 cut units of 256 rows: 17.1 us event-timed with one row a
-// warp, 18.4 with two, 20.6 with four; 72 cut units of 128 rows: 10.0, 10.8, 14.7).
-template <int D, bool FINE>
-__global__ void __launch_bounds__(256) tree_attn_tc_combine_kernel(const TcParams P) {
-    chain_wait();
-    auto weight = [](float d) { return FINE ? ex2(d) : __expf(d); };      // of two pieces' maxima that differ by d
-    const radar_attn_args& a = P.a;
-    const CutUnit& cu = P.cut[blockIdx.x];
-    const int valid = cu.valid, b = cu.b, g = cu.g, layer = cu.layer, slot = cu.slot, rows = cu.rows, n_pieces = cu.n_pieces;
-    const uint32_t live0 = cu.live[0];
-    if (!valid) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int r = blockIdx.y * 8 + warp;
-    if (r >= rows) return;                                   // rows of a unit are live from 0 up
-    constexpr int E = D / 32;                                // output elements per lane
-    // the row's record in piece j's partials (row blocks start 128 records apart, whatever part of them is live)
-    const int blk = r < P.rb_rows ? 0 : 1, in_blk = r - blk * P.rb_rows;
-    auto rec_of = [&](int j) {
-        const int64_t cta = (int64_t)blockIdx.x + (int64_t)j * P.n_cls;
-        return (cta * 2 + (j == 0 ? slot : 0)) * kPairRows + blk * 128 + in_blk;
-    };
-    auto store_row = [&](const float (&o)[E], float mx, float den) {
-        const float inv = 1.f / den;
-        const int rb_node = (int)(((uint32_t)in_blk * P.g_magic) >> 16);
-        const int node = ((blockIdx.x % P.n_cls) * P.n_blk + blk) * P.nodes_per_rb + rb_node, hq = g * P.G + in_blk - rb_node * P.G;
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.O) + layer * P.o_ls + (((int64_t)b * kMaxNodes + node) * a.Hq + hq) * D + lane * E;
-        __nv_bfloat162 w[E / 2];
-#pragma unroll
-        for (int q = 0; q < E; q += 2) w[q / 2] = __floats2bfloat162_rn(o[q] * inv, o[q + 1] * inv);
-        if (E == 4) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(w);
-        else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(w);
-        if (a.lse != nullptr && lane == 0) a.lse[layer * P.lse_ls + ((int64_t)b * a.Hq + hq) * kMaxNodes + node] = FINE ? lse_of(mx, den) : mx + logf(den);
-    };
-    auto load_row = [&](const float* src, float (&v)[E]) {
-        if (E == 4) {
-            const float4 t = *reinterpret_cast<const float4*>(src);
-            v[0] = t.x; v[1] = t.y; v[E - 2] = t.z; v[E - 1] = t.w;
-        } else {
-            const float2 t = *reinterpret_cast<const float2*>(src);
-            v[0] = t.x; v[1] = t.y;
-        }
-    };
-
-    if (n_pieces <= 4) {
-        // ---- the usual case: a unit spread over a few CTAs.  (A CTA whose range holds no tile start has no piece.) ----
-        float2 ml[4];
-        float v[4][E], o[E];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool on = ((live0 >> j) & 1u) && j < n_pieces;
-            const int64_t rec = rec_of(on ? j : 0);
-            ml[j] = P.part_ml[rec];
-            load_row(P.part_o + rec * D + lane * E, v[j]);
-            if (!on) ml[j] = make_float2(-CUDART_INF_F, 0.f);
-        }
-        const float mx = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
-        float den = 0.f;
-#pragma unroll
-        for (int q = 0; q < E; ++q) o[q] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (ml[j].x == -CUDART_INF_F) continue;
-            const float w = weight(ml[j].x - mx);
-            den = fmaf(ml[j].y, w, den);
-#pragma unroll
-            for (int q = 0; q < E; ++q) o[q] = fmaf(v[j][q], w, o[q]);
-        }
-        store_row(o, mx, den);
-        return;
-    }
-
-    // ---- a unit spread over many CTAs (few units, long prefixes): lane j holds piece j's (m, l) ----
-    float den = 0.f, mx = -CUDART_INF_F, o[E];
-#pragma unroll
-    for (int q = 0; q < E; ++q) o[q] = 0.f;
-    for (int j0 = 0; j0 < n_pieces; j0 += 32) {
-        const int jl = j0 + lane;
-        const uint32_t live = cu.live[j0 >> 5];
-        float2 ml = make_float2(-CUDART_INF_F, 0.f);
-        if (jl < n_pieces && ((live >> lane) & 1u)) ml = P.part_ml[rec_of(jl)];
-        const float mnew = fmaxf(mx, warp_max(ml.x));
-        if (mnew == -CUDART_INF_F) continue;
-        const float rescale = weight(mx - mnew);             // 0 on the first live batch
-        den *= rescale;
-#pragma unroll
-        for (int q = 0; q < E; ++q) o[q] *= rescale;
-        mx = mnew;
-        const float wl = ml.x == -CUDART_INF_F ? 0.f : weight(ml.x - mx);
-        den += warp_sum(ml.y * wl);
-        const int nb = min(32, n_pieces - j0);
-        for (int u0 = 0; u0 < nb; u0 += 4) {
-            float v[4][E], w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                w[u] = u0 + u < nb ? __shfl_sync(kFull, wl, u0 + u) : 0.f;
-                if (w[u] != 0.f) {
-                    load_row(P.part_o + rec_of(j0 + u0 + u) * D + lane * E, v[u]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < E; ++q) v[u][q] = 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int q = 0; q < E; ++q) o[q] = fmaf(v[u][q], w[u], o[q]);
-        }
-    }
-    store_row(o, mx, den);
-}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
