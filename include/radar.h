@@ -514,8 +514,8 @@ int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* args, void* st
  * attend to may hold anything; values of the rows t < n_nodes[b] have to be finite, as a probability of 0 times infinity or NaN is
  * NaN (in that channel, for all rows of the sequence and KV head).
  * lse (optional) [B][Hq][rows].  scale <= 0 selects 1/sqrt(d).  Products are accumulated in fp32; the probabilities enter P V as
- * bf16.  max_cache_len (host) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes is out of range
- * records RADAR_ERR_INVALID_ARG and is skipped; a page outside the pool records it too and is read as page 0.
+ * bf16.  max_cache_len (host, at most 2^31 - 2^14 - 1) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes
+ * is out of range records RADAR_ERR_INVALID_ARG and is skipped; a page outside the pool records it too and is read as page 0.
  * Q, Kt, Vt, O, pages and the row strides times two: 16 bytes; the workspace 256.
  * Hq a multiple of Hkv, at most 128 query heads to a KV head.  The workspace's size is enough for any fewer sequences and any
  * shorter max_cache_len. */

@@ -59,6 +59,9 @@ constexpr float kMove = 8.f;         // log2 units
 // of 4096 to 32768 tokens 766 us (627), but the lengths are the GPU's, and the bound that the host has may be far off.)  Little work: 64
 // rows over 300 tokens 11 us (20), one sequence of 1000 tokens, 256 rows 14 us (17).
 constexpr int kTokenRows = 32;
+// The longest bound: keys are counted in int, and pages are looked up as far as 2 x 4096 keys ahead of a position (two windows of 32 pieces
+// of at most a tile), rounded up to tiles.
+constexpr int kMaxLen = INT32_MAX - (1 << 14);
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -909,7 +912,7 @@ extern "C" int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args
         a->n_pages < 0)
         return RADAR_ERR_INVALID_ARG;
     if ((a->d != 64 && a->d != 128) || a->dtype != RADAR_BF16 || a->Hq / a->Hkv > 128) return RADAR_ERR_UNSUPPORTED;
-    if (!page_size_ok(a->page_size) || a->max_pages <= 0 || (int64_t)a->max_pages * a->page_size < a->max_cache_len) return RADAR_ERR_INVALID_ARG;
+    if (!page_size_ok(a->page_size) || a->max_pages <= 0 || (int64_t)a->max_pages * a->page_size < a->max_cache_len || a->max_cache_len > kMaxLen) return RADAR_ERR_INVALID_ARG;
     if (!a->Q || !a->Kt || !a->Vt || !a->O || !a->cache_len || !a->block_table || !a->workspace || (a->max_cache_len > 0 && (!a->pages || a->n_pages == 0)))
         return RADAR_ERR_INVALID_ARG;
     if (a->q_row_stride < (int64_t)a->Hq * a->d || a->kv_row_stride < (int64_t)a->Hkv * a->d || a->q_row_stride % 8 != 0 || a->kv_row_stride % 8 != 0)

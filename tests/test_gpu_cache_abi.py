@@ -117,3 +117,14 @@ def test_refusals_of_the_library(ctx):
         assert getattr(rb.lib(), "radar_cache_" + name)(None, ctypes.byref(args[name]), None) == invalid
     ctx.check_device_status()
     assert float(s["O"].float().abs().max()) == 0.0 and s["cache_len"].tolist() == [0, 0, 0]
+
+
+def test_lengths_that_an_int_cannot_look_ahead_of_are_refused(ctx):
+    """A bound near 2^31 (a table of many pages that share one): lookups run ahead of the keys, beyond what an int counts."""
+    from paper_2512_14069_b200 import binding as rb
+    a = _structs(ctx, _inputs(3))["attention"]
+    a.max_pages = 2 ** 31 // 16
+    for bound in (2 ** 31 - 1, 2 ** 31 - 2 ** 14):
+        a.max_cache_len = bound
+        assert _call(ctx, "attention", a) == -1
+    ctx.check_device_status()
