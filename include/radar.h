@@ -490,7 +490,8 @@ int radar_cache_store(radar_ctx* ctx, const radar_cache_store_args* args, void* 
 /* radar_cache_load - cached tokens as rows: of request b the tokens first[b] .. first[b] + start[b + 1] - start[b] - 1 become the
  * rows start[b] .. of K and V ([n_layers][n_rows][Hkv][d], contiguous rows; RADAR_BF16 holds the values exactly).  start is
  * non-decreasing, start[0] = 0.  Rows at or beyond n_rows, tokens outside [0, max_pages * page_size) and pages outside
- * the pool record RADAR_ERR_INVALID_ARG and are skipped. */
+ * the pool record RADAR_ERR_INVALID_ARG and are skipped.  The lengths are the caller's to keep to: a token beyond its request's
+ * comes back as what the page in the table holds, which may be another request's by now. */
 typedef struct {
     int n_layers, B, Hkv, d, page_size, max_pages;
     int dtype;                          /* RADAR_F32 or RADAR_BF16: K and V */
@@ -505,16 +506,17 @@ typedef struct {
 
 int radar_cache_load(radar_ctx* ctx, const radar_cache_load_args* args, void* stream);
 
-/* radar_cache_attention - tree-masked attention of one layer over the 4-bit cache, GQA; what radar_tree_attention does over the
- * rows that radar_cache_load would give.  Q and O [B][rows][Hq][d], Kt and Vt [B][rows][Hkv][d] in bf16, 1 <= rows <= 64 (1: single
- * tokens); q_row_stride and kv_row_stride: elements between consecutive rows of Q, and of Kt and Vt (rows of a fused projection
- * are read in place; the rows of a sequence follow those of the one before), O is contiguous.  Row i < n_nodes[b] attends to the
+/* radar_cache_attention - tree-masked attention of one layer over the 4-bit cache, GQA: that of radar_tree_attention over the rows that
+ * radar_cache_load would give, but that the probabilities enter P V as bf16 for every ratio of heads.  Q and O [B][rows][Hq][d], Kt
+ * and Vt [B][rows][Hkv][d] in bf16, 1 <= rows <= 64 (1: single tokens); q_row_stride and kv_row_stride: elements between consecutive
+ * rows of Q, and of Kt and Vt (rows of a fused projection are read in place; the rows of a sequence follow those of the one before),
+ * O is contiguous.  Row i < n_nodes[b] attends to the
  * prefix [0, cache_len[b]) and to the tree rows t < n_nodes[b] with bit t of mask[b][i] set (mask NULL: t <= i, a chain).
  * Rows i >= n_nodes[b] of O and lse are left untouched; a row that attends to nothing gets 0, and lse -inf.  Keys that a row does not
  * attend to may hold anything; values of the rows t < n_nodes[b] have to be finite, as a probability of 0 times infinity or NaN is
  * NaN (in that channel, for all rows of the sequence and KV head).
- * lse (optional) [B][Hq][rows].  scale <= 0 selects 1/sqrt(d).  Products are accumulated in fp32; the probabilities enter P V as
- * bf16.  max_cache_len (host, at most 2^31 - 2^14 - 1) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes
+ * lse (optional) [B][Hq][rows].  scale <= 0 selects 1/sqrt(d).  Products are accumulated in fp32.
+ * max_cache_len (host, at most 2^31 - 2^14 - 1) bounds cache_len and sizes the launch.  A sequence whose cache_len or n_nodes
  * is out of range records RADAR_ERR_INVALID_ARG and is skipped; a page outside the pool records it too and is read as page 0.
  * Q, Kt, Vt, O, pages and the row strides times two: 16 bytes; the workspace 256.
  * Hq a multiple of Hkv, at most 128 query heads to a KV head.  The workspace's size is enough for any fewer sequences and any

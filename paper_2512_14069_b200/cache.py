@@ -82,5 +82,6 @@ class FourBitCache:
                                  workspace=self.workspace, scale=scale)
 
     def load(self, first, start, K, V):
-        """Tokens first[b] .. of each request as rows start[b] .. start[b + 1] - 1 of K and V, [layers, rows, Hkv, d]."""
+        """Tokens first[b] .. of each request as rows start[b] .. start[b + 1] - 1 of K and V, [layers, rows, Hkv, d]; those below
+        cache_len[b] are the request's."""
         rb.radar_cache_load(self.ctx, pages=self.pages, page_size=self.page_size, block_table=self.block_table, first=first, start=start, K=K, V=V)

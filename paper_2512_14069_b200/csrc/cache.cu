@@ -15,8 +15,8 @@ using namespace cache4;
 // request in the sums.  The stack as it is after the returns is never read back: an index at or beyond the old count is the
 // returned page of some request, looked up in its table.  So no block waits for another one.  What may overwrite the inputs
 // (lengths, free count) is written behind all reads: by the only block, or by a second kernel where there are several.
-// What bounds it is the chain of loads, sums, searches and loads behind one another, not their number: 3.0 us for one request, 3.6 for 32
-// that grow by 1 to 9 tokens, 10.1 for 512 admitted with 17 to 4096 tokens (a million slots; a launch that does nothing takes
+// What bounds it is the chain of loads, sums, searches and loads behind one another, not their number: 2.8 us for one request, 3.4 for 32
+// that grow by 1 to 9 tokens, 10.9 for 512 admitted with 17 to 4096 tokens (a million slots; a launch that does nothing takes
 // 2.2).  The three sums run side by side in 32 bits and each value is loaded once; with three sums of 64 bits behind one another, and four
 // consecutive slots a thread, it was 5.7, 7.7 and 14.6 us.
 constexpr int kExtendThreads = 1024;

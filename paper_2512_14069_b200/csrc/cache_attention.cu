@@ -20,8 +20,9 @@
 // merged in shared memory at its end, while the next segment's copies are under way.  Units that were cut are joined by the
 // combine kernel from partial records, two at most a block.  Where there is little to do in all, finding shares and joining them
 // is what takes the time: there a cluster of blocks takes a unit, and joins its shares through its shared memories.
-// What bounds it, long caches: decoding, on the integer pipe (seven of its instructions for eight values; it works 63 % of the time, an
-// instruction is issued in 58 % of the cycles).  32 sequences of 4096 to 32768 tokens, 32 / 8 heads, one row: 160 us, 4.2 TB/s of the
+// What bounds it, long caches: the warps' own chains of loads, decoding, products and votes.  No unit is full: an instruction is issued
+// in 58 % of the cycles, the integer pipe, the busiest (seven of its instructions for eight values), works 63 % of the time; 16 warps an SM do not
+// cover one another's waits, and there are no registers for more.  32 sequences of 4096 to 32768 tokens, 32 / 8 heads, one row: 160 us, 4.2 TB/s of the
 // cache's 680 MB.  Two stages a warp and four blocks an SM; three stages 175 us, five blocks (96 registers, spilled) 216, three blocks 160;
 // shifts by the multiplier were slower too.
 #include <algorithm>
@@ -199,7 +200,9 @@ __device__ __forceinline__ void cached_values(State<D, NT>& st, const uint32_t (
     }
 }
 
-// Scores to probabilities: moves the reference maximum where it has to.  s are raw scores (-inf: masked).
+// Scores to probabilities: moves the reference maximum where it has to.  s are raw scores (-inf: masked).  They are rounded to bf16 for
+// the product with values that are bf16 already; their sum is taken in fp32 before that.  It costs as much as O's own rounding (O is off by
+// 0.0023 of its size, 0.0017 with fp32 probabilities), and a second bf16 part would double the products of P V.
 template <int D, int NT, int NB>
 __device__ __forceinline__ void probabilities(State<D, NT>& st, float (&s)[NB][NT][4], uint32_t (&p)[NB][NT][2], float scale_log2) {
     bool move = false;

@@ -10,11 +10,13 @@
 //   warps 12-15      decoders of keys, the same; the tree's K by TMA
 //   warp 16          producer: segments, stages, Q
 //   warp 17          issues the products
-// What bounds the kernel is the warp that issues the products, with two row blocks a tile: 32 MMAs, which the tensor pipe takes at 64 to 70
+// What bounds the kernel with two row blocks a tile is the warp that issues the products: 32 MMAs, which the tensor pipe takes at 64 to 70
 // cycles each, and waits and commits between them in which it runs dry (4500 cycles a tile); and the softmax behind it, half as
-// long.  8 sequences of 8192 tokens, 64 / 8 heads, 64 rows: 158 us; the same over bf16 rows takes 152.  The decoding (twelve instructions
-// for eight values) fits beside it: 32 rows of 32 / 8 heads, 16384 tokens, take 94 us here and 106 there.  A thread takes its row's scores
-// 64 at a time, against the maximum so far, and waits for each load at once, which makes room for eight decoders at 96 registers;
+// long.  8 sequences of 8192 tokens, 64 / 8 heads, 64 rows: 158 us; the same over bf16 rows takes 152.  With one row block a tile takes
+// about 3000 cycles (8 sequences of 16384 tokens, 32 / 8 heads, 32 rows: 94 us, where the cache's bytes take 23), with 64 live rows
+// as with 128, and its 16 MMAs some 1070 of them: neither products nor softmax.  What is left is the decoding (twelve instructions for eight
+// values, a decoder's two blocks one after the other); its part has not been measured by itself.  A thread takes its row's scores 64
+// at a time, against the maximum so far, and waits for each load at once, which makes room for eight decoders at 96 registers;
 // keys and values are decoded by the same small loop.
 #include <algorithm>
 #include <cmath>
@@ -282,6 +284,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                         // ---- P = exp2(s * scale - m) against the maximum so far, and the half's own maximum beside it; once more where a row's
                         // exceeds the reference by 2^8 (nearly never behind the first tile), behind a rescaling of the accumulator ----
+                        // Probabilities are rounded to bf16 for the product, and their sum is taken before that: each is off by up to 2^-8 of
+                        // itself, like O by its own rounding.  (A second bf16 part would double the P V products, which bound the kernel.)
                         // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values.  The warp issues in
                         // order and an exponential takes its unit 8 cycles: what else there is to do stands between two of them.)
                         float2 ls[2];

@@ -337,7 +337,8 @@ void plan_grid(const radar_ctx* ctx, int B, int Hq, int Hkv, int max_prefix_len,
     // All units of one sequence are alike, so where they are no more than the CTAs of a class a grid can be chosen in
     // which every CTA has one piece of one unit and pays for one segment (fill and epilogue, what tile_costs books per
     // unit) and not for two.  Not where that leaves so many CTAs unused that the pieces get longer than what it saves.
-    // (Attention + combine, d = 128: 40 / 40 heads, 2048 tokens 22.9 -> 19.6 us; 16 / 16 heads, 1000 tokens 14.8 -> 13.6.)
+    // (Attention + combine, d = 128: 40 / 40 heads, 2048 tokens 22.9 -> 19.6 us; 16 / 16 heads, 1000 tokens 14.8 -> 13.6.  Measured over
+    // bf16 rows, with that kernel's weights; the 4-bit cache's, which weighs its tiles otherwise, is planned by the same.)
     const long long units = (long long)layers * Hkv, tiles = unit_tiles / (B * units);
     *whole = false;
     if (B == 1 && units <= per) {
