@@ -546,6 +546,110 @@ size_t radar_cache_attn_workspace_bytes(const radar_ctx* ctx, int B, int Hq, int
 int radar_cache_attention(radar_ctx* ctx, const radar_cache_attn_args* args, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Rows with positions, and the paged cache of whole numbers of bytes: radar_rotate, radar_paged_store, radar_chunk_attention.
+ * (The paper's verification pass takes rotated queries and keys and a prefix cache for granted.  These bring rows to their positions,
+ * keep the bf16 / fp32 cache that radar_tree_attention reads with a block table, and let prompts attend over it.)
+ *
+ * Rotation.  Pair p < n_pairs of a head's first 2 n_pairs channels, (p, p + n_pairs) or with `neighbours` (2 p, 2 p + 1), is turned by the
+ * angle pos * inv_freq[p]: (x, y) -> (x cos - y sin, y cos + x sin); the channels behind them stay as they are.  The position of row i
+ * is pos[axis * pos_stride + i] with axis = pair_axis[p] (NULL: 0), one of n_axes: one for text, two for the height and width
+ * of image patches, three for time, height and width.  The angle is reduced in fp64, so that it is right for every 32-bit position; products and sums are fp32,
+ * the result is rounded once.  A pair_axis outside [0, n_axes) records RADAR_ERR_INVALID_ARG and counts as axis 0. */
+typedef struct {
+    const int32_t* pos;                 /* [n_axes][pos_stride], >= n_rows (n_tokens) of each; NULL: no rotation */
+    int64_t pos_stride;
+    int n_axes;
+    int n_pairs;
+    const float* inv_freq;              /* [n_pairs] */
+    const uint8_t* pair_axis;           /* [n_pairs] or NULL */
+    int neighbours;
+} radar_rotation;
+
+/* radar_rotate - rows of Q and K (either may be NULL, its heads 0) turned by their positions; with `inverse` by the negative angles, which
+ * is the gradient of the rotation (its transpose) and takes rows back to where they were.  Row i of Q: Hq heads of d channels at
+ * i * q_row_stride (elements; parts of a fused projection are read in place).  An output may be its own input (same address and
+ * stride); otherwise it must not overlap one.
+ * Limits: 1 <= d <= 1024, 1 <= n_pairs <= d / 2, n_rows < 2^31.  Rows of any alignment are taken; 16 bytes at a time where all addresses and
+ * strides are multiples of 16 bytes and d and n_pairs of 16 bytes' elements, one element at a time elsewhere. */
+typedef struct {
+    int Hq, Hkv, d;
+    int dtype;                          /* RADAR_F32 or RADAR_BF16 */
+    int64_t n_rows;
+    const void *Q, *K;
+    int64_t q_row_stride, k_row_stride;
+    void *Q_out, *K_out;
+    int64_t q_out_row_stride, k_out_row_stride;
+    radar_rotation rotation;
+    int inverse;
+} radar_rotate_args;
+
+int radar_rotate(radar_ctx* ctx, const radar_rotate_args* args, void* stream);
+
+/* radar_paged_store - rows of K and V into their slots of a paged cache, K turned by its positions on the way, and the queries beside them;
+ * all layers in one call.  Token i < n_tokens of layer l is row src_row[i] (i without src_row) of Q, K and V; its position is pos[i].  K and V go to
+ * cache row slots[i] of Kc and Vc, [cache_rows][Hkv][d] as radar_tree_attention and radar_chunk_attention read them (slot = page *
+ * page_size + row in the page: what radar_cache_extend gives); the turned queries to row i of Q_out.  rotation.pos NULL: rows as they are
+ * (what a step accepted: its keys were turned before the verification).  A slot below 0 is skipped (a token that was not granted; its query is
+ * turned all the same); one at or beyond cache_rows, or a row outside [0, n_rows), records RADAR_ERR_INVALID_ARG and is skipped.
+ * No two tokens of a call may have one slot.  K and V share strides.  Q may be NULL with Hq 0; Q_out may be Q where there is no src_row
+ * (same address and strides).  d, alignment and positions as in radar_rotate; row and layer strides in elements. */
+typedef struct {
+    int n_layers, Hq, Hkv, d;
+    int dtype;                          /* RADAR_F32 or RADAR_BF16: all of Q, K, V and the cache */
+    int64_t n_tokens, n_rows, cache_rows;
+    const void *Q, *K, *V;
+    int64_t q_row_stride, kv_row_stride, q_layer_stride, kv_layer_stride;
+    const int64_t* slots;               /* [n_tokens] */
+    const int32_t* src_row;             /* [n_tokens] or NULL */
+    radar_rotation rotation;
+    void* Q_out;
+    int64_t q_out_row_stride, q_out_layer_stride;
+    void *Kc, *Vc;
+    int64_t cache_layer_stride;
+} radar_paged_store_args;
+
+int radar_paged_store(radar_ctx* ctx, const radar_paged_store_args* args, void* stream);
+
+/* radar_chunk_attention - attention of chunks of new tokens over the paged cache that already holds them, one layer, GQA.
+ * Request b has the rows q_start[b] .. q_start[b + 1] - 1 of Q, n of them, and cache_len[b] tokens in the cache, of which its rows are the last
+ * n: row i < n attends to tokens 0 .. cache_len[b] - n + i (a whole prompt, a chunk of one, or with n = 1 a single token; requests of all
+ * kinds may stand in one call, n = 0 among them).  Rows that see nothing (more rows than cached tokens) get 0, and lse -inf.
+ * Q [n_rows][Hq][d] with q_row_stride elements between rows, O [n_rows][Hq][d] contiguous, lse (optional) [n_rows][Hq] receives log sum exp(scale *
+ * q.k).  Rows before q_start[0] or from q_start[B] on are left untouched.  Kc, Vc [cache_rows][Hkv][d]: token j of request b is row
+ * block_table[b * max_pages + j / page_size] * page_size + j % page_size; page_size 16, 32, 64 or a multiple of 128.
+ * max_new and max_cache_len (host) bound the rows and the cached tokens of every request and size the launch.  A request that is out of these bounds, or whose
+ * rows are outside [0, n_rows) or not in order, records RADAR_ERR_INVALID_ARG and is skipped; a page outside the cache records it too and is read
+ * as page 0.  Requests must not share rows.  scale <= 0 selects 1/sqrt(d).
+ * Values of the tokens that any row of a request sees have to be finite (a probability of 0 times infinity or NaN is NaN); keys that a row does
+ * not attend to may hold anything, and so may the cache behind a request's last token.
+ * RADAR_BF16: products on the tensor cores, probabilities enter P V as bf16, sums in fp32.  RADAR_F32: fp32 throughout.
+ * Limits: d in {64, 128}; Hq a multiple of Hkv, at most 128 query heads to a KV head; B <= 65535; n_rows, cache_rows < 2^31; max_cache_len at most 2^31 -
+ * 2^14 - 1.  Q, Kc, Vc and O: 16 bytes, as are the row stride times the element size; the workspace: 256.  The workspace's size is enough for fewer requests, shorter ones
+ * and fewer rows; calls that may overlap need one each. */
+typedef struct {
+    int B, Hq, Hkv, d;
+    int dtype;                          /* RADAR_F32 or RADAR_BF16 */
+    int64_t n_rows;
+    const void* Q;
+    int64_t q_row_stride;
+    const int32_t* q_start;             /* [B + 1] */
+    const void *Kc, *Vc;
+    int64_t cache_rows;
+    int page_size, max_pages;
+    const int32_t* block_table;         /* [B][max_pages] */
+    const int32_t* cache_len;           /* [B] */
+    int max_new, max_cache_len;         /* host values */
+    float scale;
+    void* O;
+    float* lse;                         /* or NULL */
+    void* workspace;
+    size_t workspace_bytes;
+} radar_chunk_attn_args;
+
+size_t radar_chunk_attn_workspace_bytes(const radar_ctx* ctx, int B, int Hq, int Hkv, int d, int dtype, int max_new, int max_cache_len);
+int radar_chunk_attention(radar_ctx* ctx, const radar_chunk_attn_args* args, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * radar_policy_train_step - one REINFORCE step of the prediction model on a batch of data points {S, D}.
  * (Sec. 4.2: the MDP of Eq. 3-9 and the loss of Eq. 10; Sec. 4.3: the data point x = {S, D}, the acceptance
  * length drawn from d_T; App. "Implementation Details": the network, learning rate 1e-4, batches of 256.  The

@@ -130,6 +130,36 @@ class CacheAttnArgs(ctypes.Structure):
     ]
 
 
+class Rotation(ctypes.Structure):
+    _fields_ = [("pos", _vp), ("pos_stride", _c_i64), ("n_axes", _c_int), ("n_pairs", _c_int), ("inv_freq", _vp), ("pair_axis", _vp), ("neighbours", _c_int)]
+
+
+class RotateArgs(ctypes.Structure):
+    _fields_ = [
+        ("Hq", _c_int), ("Hkv", _c_int), ("d", _c_int), ("dtype", _c_int), ("n_rows", _c_i64), ("Q", _vp), ("K", _vp), ("q_row_stride", _c_i64),
+        ("k_row_stride", _c_i64), ("Q_out", _vp), ("K_out", _vp), ("q_out_row_stride", _c_i64), ("k_out_row_stride", _c_i64),
+        ("rotation", Rotation), ("inverse", _c_int),
+    ]
+
+
+class PagedStoreArgs(ctypes.Structure):
+    _fields_ = [
+        ("n_layers", _c_int), ("Hq", _c_int), ("Hkv", _c_int), ("d", _c_int), ("dtype", _c_int), ("n_tokens", _c_i64), ("n_rows", _c_i64),
+        ("cache_rows", _c_i64), ("Q", _vp), ("K", _vp), ("V", _vp), ("q_row_stride", _c_i64), ("kv_row_stride", _c_i64),
+        ("q_layer_stride", _c_i64), ("kv_layer_stride", _c_i64), ("slots", _vp), ("src_row", _vp), ("rotation", Rotation), ("Q_out", _vp),
+        ("q_out_row_stride", _c_i64), ("q_out_layer_stride", _c_i64), ("Kc", _vp), ("Vc", _vp), ("cache_layer_stride", _c_i64),
+    ]
+
+
+class ChunkAttnArgs(ctypes.Structure):
+    _fields_ = [
+        ("B", _c_int), ("Hq", _c_int), ("Hkv", _c_int), ("d", _c_int), ("dtype", _c_int), ("n_rows", _c_i64), ("Q", _vp),
+        ("q_row_stride", _c_i64), ("q_start", _vp), ("Kc", _vp), ("Vc", _vp), ("cache_rows", _c_i64), ("page_size", _c_int),
+        ("max_pages", _c_int), ("block_table", _vp), ("cache_len", _vp), ("max_new", _c_int), ("max_cache_len", _c_int), ("scale", _c_f),
+        ("O", _vp), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _sz),
+    ]
+
+
 class TrainArgs(ctypes.Structure):
     _fields_ = [
         ("n", _c_int), ("k", _c_int), ("t_max", _c_int),
@@ -213,6 +243,14 @@ def lib() -> ctypes.CDLL:
         L.radar_cache_attn_workspace_bytes.argtypes = [_vp, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int]
         L.radar_cache_attention.restype = _c_int
         L.radar_cache_attention.argtypes = [_vp, ctypes.POINTER(CacheAttnArgs), _vp]
+        L.radar_rotate.restype = _c_int
+        L.radar_rotate.argtypes = [_vp, ctypes.POINTER(RotateArgs), _vp]
+        L.radar_paged_store.restype = _c_int
+        L.radar_paged_store.argtypes = [_vp, ctypes.POINTER(PagedStoreArgs), _vp]
+        L.radar_chunk_attn_workspace_bytes.restype = _sz
+        L.radar_chunk_attn_workspace_bytes.argtypes = [_vp] + [_c_int] * 7
+        L.radar_chunk_attention.restype = _c_int
+        L.radar_chunk_attention.argtypes = [_vp, ctypes.POINTER(ChunkAttnArgs), _vp]
         L.radar_profile_begin.restype = _c_int
         L.radar_profile_begin.argtypes = [_vp, _c_int]
         L.radar_profile_end.restype = _c_int
@@ -620,6 +658,49 @@ def radar_cache_attention(ctx: Context, *, Q, Kt, Vt, pages, page_size, block_ta
     they are: equal strides between all rows), pages [n_pages, page bytes] uint8, block_table [B, max_pages], cache_len [B]
     int32, mask [B, rows] int64 or None (a chain), n_nodes [B] int32 or None (all rows); O [B, rows, Hq, d], lse [B, Hq, rows]."""
     _cache_attention(ctx, stream, Q, Kt, Vt, pages, page_size, block_table, cache_len, max_cache_len, O, workspace, mask, n_nodes, lse, scale)
+
+
+# ---- rows with positions and the paged cache ----------------------------------------------------------------------------
+def radar_chunk_attn_workspace_bytes(ctx: Context, B, Hq, Hkv, d, dtype, max_new, max_cache_len) -> int:
+    return int(lib().radar_chunk_attn_workspace_bytes(ctx.handle, B, Hq, Hkv, d, dtype, max_new, max_cache_len))
+
+
+class _PagedCall(_CacheCall):
+    """... and checks that all its tensors are on the current device, which is the context's."""
+
+    def __call__(self, ctx, stream, *args):
+        device = torch._C._cuda_getDevice()
+        if device != ctx.device:
+            raise ValueError("%s: the current device is %d, the context's %d" % (self.name, device, ctx.device))
+        super().__call__(ctx, stream, device, *args)
+
+
+_rotate, _paged_store, _chunk_attention = (_PagedCall("radar_" + n) for n in ("rotate", "paged_store", "chunk_attention"))
+
+
+def radar_rotate(ctx: Context, *, pos, inv_freq, Q=None, Q_out=None, K=None, K_out=None, pair_axis=None, neighbours=False, inverse=False, stream=None):
+    """Rows of Q [rows, Hq, d] and K [rows, Hkv, d] (either or both; float32 or bfloat16; any stride between rows) turned by their
+    positions into Q_out and K_out, which may be Q and K.  pos [rows] or [axes, rows] int32; inv_freq [pairs] float32; pair_axis
+    [pairs] uint8, the axis of each pair; neighbours: a pair is channels (2 p, 2 p + 1) and not (p, p + pairs); inverse: the
+    negative angles, which is the rotation's gradient."""
+    _rotate(ctx, stream, Q, Q_out, K, K_out, pos, inv_freq, pair_axis, neighbours, inverse)
+
+
+def radar_paged_store(ctx: Context, *, K, V, slots, Kc, Vc, src_row=None, Q=None, Q_out=None, pos=None, inv_freq=None, pair_axis=None, neighbours=False, stream=None):
+    """Rows of K and V ([rows, Hkv, d], or [layers, rows, Hkv, d] for all layers at once; float32 or bfloat16; any strides between
+    rows and layers that K and V share) into the slots of Kc and Vc ([cache rows, Hkv, d], or with a leading layer dimension), and
+    rows of Q into Q_out.  With pos [tokens] or [axes, tokens] the keys and queries are turned on the way, as in
+    radar_rotate.  Token i is row src_row[i], or row i."""
+    _paged_store(ctx, stream, K, V, slots, src_row, Kc, Vc, Q, Q_out, pos, inv_freq, pair_axis, neighbours)
+
+
+def radar_chunk_attention(ctx: Context, *, Q, q_start, Kc, Vc, page_size, block_table, cache_len, max_new, max_cache_len, O, workspace, lse=None, scale=0.0,
+                          stream=None):
+    """One layer's attention of new tokens over the paged cache that holds them.  Q [rows, Hq, d] (float32 or bfloat16; any stride
+    between rows), request b's rows q_start[b] .. q_start[b + 1] (q_start [B + 1] int32), its last tokens of cache_len[b] (int32);
+    Kc, Vc [cache rows, Hkv, d], block_table [B, max_pages] int32; O [rows, Hq, d], lse [rows, Hq].  max_new and max_cache_len bound
+    the rows and the cached tokens of a request."""
+    _chunk_attention(ctx, stream, Q, q_start, Kc, Vc, page_size, block_table, cache_len, max_new, max_cache_len, O, workspace, lse, scale)
 
 
 def radar_policy_param_count(k: int) -> int:

@@ -108,6 +108,10 @@ extern "C" const char* radar_kernel_name(int id) {
         case RADAR_K_CACHE_LOAD: return "cache_load";
         case RADAR_K_CACHE_ATTN: return "cache_attention";
         case RADAR_K_CACHE_COMBINE: return "cache_attention_combine";
+        case RADAR_K_ROTATE: return "rotate";
+        case RADAR_K_PAGED_STORE: return "paged_store";
+        case RADAR_K_CHUNK_ATTN: return "chunk_attention";
+        case RADAR_K_CHUNK_COMBINE: return "chunk_attention_combine";
         default: return "?";
     }
 }

@@ -1,0 +1,698 @@
+// Attention of chunks of new tokens over the paged bf16 cache on the 5th-generation tensor cores (tcgen05 + tensor memory), K/V tiles
+// staged by TMA.  The machine is that of the tree attention (tree_attention_tc.cu); its units and masks are not.
+//
+// A head group is a KV head's, a row block up to 128 rows (the MMA M dimension), a unit a pair of row blocks, a tile 128 keys; one CTA per SM.
+//
+// Inside the CTA (16 warps; the registers are shared out by warpgroup):
+//   warp 12    TMA producer: works out the CTA's segments (unit, tile range) for itself and, through a ring in shared memory, for the others;
+//              per segment the Q rows, then K and V tiles into two rings (128-byte swizzle), page by page.
+//   warp 13    MMA issuer: S = Q K^T into one of two tensor-memory score buffers, and O (+)= P V with P read back from
+//              tensor memory (bf16, overlaying S) and V consumed N-major straight from the row-major tile.
+//   warps 0-3 / 4-7  softmax groups 0 / 1, one thread per query row.  Unit with two live row blocks: group s owns row block s and sees
+//              every tile, so each K/V tile is loaded once for 256 query rows.  Unit with one: the groups take alternate
+//              tiles with separate (m, l, O) and are merged at the end.  Either way one group's softmax overlaps the other's MMAs.
+//   warps 8-11 epilogue: a finished accumulator to O or to the partials, while the others are in the next segment.
+//   warps 14, 15 only fill up the producer's warpgroup.
+// Every mbarrier wait is bounded; a wait that runs out sets RADAR_ERR_TIMEOUT on the device status word, the CTA drains, frees its
+// tensor memory and returns.
+#include <algorithm>
+#include <cmath>
+
+#include "attn_tiles.cuh"
+#include "chunk_attention.cuh"
+
+namespace radar {
+namespace {
+
+constexpr int kChunkThreads = 512;
+constexpr int kEpilogueWarp = 8, kProducerWarp = 12, kMmaWarp = 13;
+// Registers a thread: 128 at launch, then shared out by warpgroup (two of softmax; what they take the other two give).
+constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
+static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
+constexpr int kStaticSmem = 3072;    // barriers and exchange arrays: with the tiles exactly the 227 KB a block may have
+
+template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+template <int D>
+struct Smem {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kQBlock = 128 * D * 2;
+    static constexpr int kQBytes = 2 * kQBlock;
+    static constexpr int kTileBytes = kTileKeys * D * 2;
+    static constexpr int kRingK = 3, kRingV = 2;
+    static constexpr int kDynamic = kQBytes + (kRingK + kRingV) * kTileBytes;     // starts on a 1024-byte boundary behind the static block
+};
+
+struct Costs {
+    static constexpr int kTile = kTileKeys, kOne = 3, kTwo = 5, kUnit = 15 * kTileKeys;
+};
+
+// What the other warps know of a segment.
+struct __align__(16) Segment {
+    int n;                               // tiles; 0: there is no further segment
+    int t0, nt;                          // first tile, tiles of the unit
+    int seen, keys, rows, row0, g;       // of the unit (keys: 0 where its last token sees none)
+};
+
+template <int D>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const ChunkParams P) {
+    chain_trigger();                     // every warp waits for the predecessor where its role begins; the barrier,
+                                         // tensor-memory and descriptor set-up needs nothing from global memory
+    using SM = Smem<D>;
+    constexpr int H = SM::kHalves, RK = SM::kRingK, RV = SM::kRingV;
+    const radar_chunk_attn_args& a = P.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = P.G;
+
+    // Static block first (padded to a multiple of 1024 bytes and aligned to it), the tiles behind it: the
+    // swizzled tiles need a 1024-byte boundary and there is no room left for alignment slack.
+    struct Shared {
+        uint64_t bar_qfull, bar_qempty, bar_kfull[RK], bar_kempty[RK], bar_vfull[RV], bar_vempty[RV];
+        uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2], bar_mlfull, bar_mlempty;
+        uint64_t bar_idle;               // every product issued has run
+        uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
+        uint64_t bar_pready[2];          // ... all of them
+        uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
+        uint32_t q_last, k_next, v_next; // the producer's: phase parity of the last Q, slot and parity of the next K and V
+        uint32_t tmem_base;
+        int abort;
+        Segment seg[kSegRing];
+        ChunkPieces cut;                 // the producer's
+        float2 ml[2][128];               // per group: (m in log2 units, l) of the rows at the end of a segment
+    };
+    static_assert(sizeof(Shared) <= kStaticSmem, "static shared-memory block");
+    struct __align__(1024) Static {
+        Shared s;
+        unsigned char pad[kStaticSmem - sizeof(Shared)];
+    };
+    static_assert(sizeof(Static) == kStaticSmem, "static shared-memory block");
+    __shared__ Static block;
+    Shared& st = block.s;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* sQ = smem_raw;
+    unsigned char* sK = sQ + SM::kQBytes;
+    unsigned char* sV = sK + RK * SM::kTileBytes;
+
+    // ---- set-up ----
+    if (warp == 0) {
+        if (lane == 0) {
+            st.abort = 0;
+            mbar_init(&st.bar_qfull, 1);
+            mbar_init(&st.bar_qempty, 1);
+            for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], 1); mbar_init(&st.bar_kempty[i], 1); }
+            for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], 1); mbar_init(&st.bar_vempty[i], 1); }
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
+                mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
+            }
+            for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
+            mbar_init(&st.bar_idle, 1);
+            st.q_last = 1;
+            mbar_init(&st.bar_mlfull, 8);
+            mbar_init(&st.bar_mlempty, 4);
+            fence_barrier_init();
+        }
+    } else if (warp == kMmaWarp) {
+        tmem_alloc(&st.tmem_base, 512);
+        tmem_relinquish();
+        if (lane == 0) { tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    // All of tensor memory is this CTA's, so its addresses are constants (the producer checks): S/P buffers in columns 0 and
+    // 128, O accumulators in 256 and 384.
+    constexpr uint32_t tmem = 0;
+    bool ok = true;                         // no wait of this thread has run out
+    // Each role starts with chain_sync(): the bounds of the waits behind it are for this kernel's own work.
+    // the producer's next segment; false behind the last one
+    auto take_segment = [&](uint32_t seg, Segment& s) {
+        ok = mbar_wait_while(ok, &st.bar_segfull[seg % kSegRing], (seg / kSegRing) & 1);
+        ok = __all_sync(kFull, ok);
+        s = st.seg[seg % kSegRing];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&st.bar_segempty[seg % kSegRing]);
+        return ok && s.n > 0;
+    };
+
+    if (warp < kEpilogueWarp) {
+        regs_inc<kSoftmaxRegs>();
+        chain_sync();
+        // =================================== softmax groups ===================================
+        // One thread per query row, which holds the tile's 128 scores in registers.
+        const int grp = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;                 // row of the block == tensor-memory lane
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + grp * 128 + lane_addr;
+        const uint32_t tO = tmem + 256 + grp * 128 + lane_addr;
+        const int rb_token = (int)(((uint32_t)row * P.g_magic) >> 16);       // row / G
+        uint32_t sc = 0;                         // S tiles this group has waited for
+        Segment s;
+        for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+            const bool two = s.rows > P.rb_rows;
+            const int blk = two ? grp : 0;                       // row block within the unit
+            const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
+            // A warp none of whose 32 rows is live does no arithmetic (the products of its rows are never read):
+            // it only keeps the barriers going.
+            const bool warp_live = row - lane < rows_here;
+            const int lim = s.seen + blk * P.tokens_per_rb + rb_token;       // keys that this row sees (more than there are for rows that are not live)
+            const int lim_warp = s.seen + blk * P.tokens_per_rb + (int)(((uint32_t)(row - lane) * P.g_magic) >> 16);    // ... and the warp's first one
+            const int n_my = two ? s.n : (s.n - grp + 1) >> 1;
+            float m_run = -CUDART_INF_F, l_run = 0.f;
+
+#pragma unroll 1
+            for (int j = 0; j < n_my; ++j) {
+                const int t = s.t0 + (two ? j : 2 * j + grp);
+                ok = mbar_wait_while(ok, &st.bar_sfull[grp], sc & 1);
+                ok = __all_sync(kFull, ok);                      // warp-uniform: guards .aligned ops
+                ++sc;
+                tc_fence_after_sync();
+                if (ok && warp_live) {
+                    uint32_t sv[4][32];
+                    if (lim_warp < (t + 1) * kTileKeys) {
+                        // Keys that the row does not see become -inf in tensor memory, 32 at a time: the last tile or two of a unit need
+                        // it, and an unrolled path for them would be fetched into the instruction cache anew each time.
+                        const int valid = lim - t * kTileKeys;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const int in = valid - c * 32;
+                            const uint32_t al = in >= 32 ? 0xffffffffu : (in <= 0 ? 0u : ((1u << in) - 1u));
+                            tmem_ld32(tS + c * 32, sv[0]);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((al >> e) & 1u)) sv[0][e] = 0xff800000u;     // -inf
+                            tmem_st32(tS + c * 32, sv[0]);
+                        }
+                        tmem_wait_st();
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sv[c]);
+                    tmem_wait_ld();
+                    float mxa[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        mxa[c] = __uint_as_float(sv[c][0]);
+#pragma unroll
+                        for (int e = 1; e < 31; e += 2)                     // three-input maxima: half the instructions
+                            mxa[c] = max3(mxa[c], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
+                        mxa[c] = fmaxf(mxa[c], __uint_as_float(sv[c][31]));
+                    }
+                    const float mx = fmaxf(max3(mxa[0], mxa[1], mxa[2]), mxa[3]);
+                    // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
+                    const float m_tile = mx * P.scale_log2;
+                    float factor = 1.f;
+                    if (j == 0) {
+                        m_run = m_tile;
+                    } else if (m_tile > m_run + kRescaleThreshold) {
+                        factor = ex2(m_run - m_tile);           // m_run may be -inf: factor 0 clears O and l
+                        m_run = m_tile;
+                    }
+                    const float m_use = m_run == -CUDART_INF_F ? 0.f : m_run;
+                    if (j > 0 && __any_sync(kFull, factor != 1.f)) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st16(tO + c, o);
+                        }
+                    }
+                    // ---- P = exp2(s * scale - m), row sum, bf16 pairs back to tensor memory ----
+                    // (the scaling and the row sum work on pairs: one packed fp32x2 instruction per two values)
+                    // The warp issues in order and an exponential takes its unit 8 cycles: what else there is to do stands between
+                    // two of them.
+                    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const float2 sc2 = make_float2(P.scale_log2, P.scale_log2), nm2 = make_float2(-m_use, -m_use);
+                    uint32_t pk[16];
+                    auto scale = [&](const int p) {
+                        uint32_t &x = sv[p >> 4][2 * (p & 15)], &y = sv[p >> 4][2 * (p & 15) + 1];
+                        const float2 s2 = make_float2(__uint_as_float(x), __uint_as_float(y));
+                        const float2 t2 = fma2_in_order(s2, sc2, nm2);
+                        x = __float_as_uint(t2.x);
+                        y = __float_as_uint(t2.y);
+                    };
+                    auto finish = [&](const int p) {
+                        const float p0 = __uint_as_float(sv[p >> 4][2 * (p & 15)]), p1 = __uint_as_float(sv[p >> 4][2 * (p & 15) + 1]);
+                        ls[p & 1] = add2_in_order(ls[p & 1], make_float2(p0, p1));
+                        pk[p & 15] = bf16x2_in_order(p0, p1);
+                        if ((p & 15) == 15) tmem_st16(tS + (p >> 4) * 16, pk);
+                    };
+                    // pairs that the scaling is ahead, that the rest is behind, and that the first stores are given to land in
+                    constexpr int kAhead = 2, kLag = 4, kLanding = 4;
+#pragma unroll
+                    for (int p = 0; p < kAhead; ++p) scale(p);
+#pragma unroll
+                    for (int p = 0; p < 64 + kLag; ++p) {
+                        if (p < 64) sv[p >> 4][2 * (p & 15)] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15)])));
+                        if (p + kAhead < 64) scale(p + kAhead);
+                        if (p < 64) sv[p >> 4][2 * (p & 15) + 1] = __float_as_uint(ex2_in_order(__uint_as_float(sv[p >> 4][2 * (p & 15) + 1])));
+                        if (p >= kLag) finish(p - kLag);
+                        if (p == kFirstKeys / 2 - 1 + kLag + kLanding) {
+                            tmem_wait_st();
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&st.bar_pfirst[grp]);
+                        }
+                    }
+                    l_run = l_run * factor + ((ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
+                    tmem_wait_st();
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (!(ok && warp_live)) mbar_arrive(&st.bar_pfirst[grp]);
+                    mbar_arrive(&st.bar_pready[grp]);
+                }
+            }
+
+            // the rows' (m, l) go to the epilogue, which has taken those of the segment before
+            ok = mbar_wait_while(ok, &st.bar_mlempty, (seg & 1) ^ 1);
+            st.ml[grp][row] = make_float2(m_run, l_run);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&st.bar_mlfull);
+        }
+    } else if (warp < kProducerWarp) {
+        regs_dec<kEpilogueRegs>();
+        chain_sync();
+        // =================================== epilogue ===================================
+        // One thread per tensor-memory lane takes the finished accumulators to O (or to the partials) while the softmax
+        // groups and the tensor cores are already in the next segment; each accumulator is handed back as soon as it is read.
+        const int row = (warp - kEpilogueWarp) * 32 + lane;
+        const uint32_t tO = tmem + 256 + ((uint32_t)((warp - kEpilogueWarp) * 32) << 16);
+        const int rb_token = (int)(((uint32_t)row * P.g_magic) >> 16);       // row / G
+        uint32_t oc[2] = {0, 0};             // accumulators waited for
+        Segment s;
+        for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+            const bool two = s.rows > P.rb_rows;
+            const bool final_rows = s.n == s.nt;                 // the whole unit
+            const int slot = seg == 0 ? 0 : 1;                   // a CTA has at most a cut first and a cut last segment
+            ok = mbar_wait_lazy(ok, &st.bar_mlfull, seg & 1);
+            const float2 ml0 = st.ml[0][row], ml1 = st.ml[1][row];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&st.bar_mlempty);
+#pragma unroll 1
+            for (int blk = 0; blk < 2; ++blk) {
+                // two live row blocks: accumulator blk is row block blk; one: both belong to it, merged in the first trip
+                if (blk == 1 && !two) {
+                    if (lane == 0) mbar_arrive(&st.bar_ofree[1]);
+                    break;
+                }
+                ok = mbar_wait_while(ok, &st.bar_odone[blk], oc[blk] & 1);
+                ++oc[blk];
+                const bool merge = !two && s.n > 1;
+                if (merge) {
+                    ok = mbar_wait_while(ok, &st.bar_odone[1], oc[1] & 1);
+                    ++oc[1];
+                }
+                ok = __all_sync(kFull, ok);
+                tc_fence_after_sync();
+                const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
+                const bool row_live = row < rows_here;
+                if (ok && row - lane < rows_here) {
+                    float m_out = blk == 0 ? ml0.x : ml1.x, l_out = blk == 0 ? ml0.y : ml1.y, w0 = 1.f, w1 = 0.f;
+                    if (merge) {
+                        m_out = fmaxf(ml0.x, ml1.x);
+                        const float ms = m_out == -CUDART_INF_F ? 0.f : m_out;
+                        w0 = ex2(ml0.x - ms);                        // exp2(-inf) = 0
+                        w1 = ex2(ml1.x - ms);
+                        l_out = ml0.y * w0 + ml1.y * w1;
+                    }
+                    // a row that saw no key of these tiles (l = 0): O is 0, whatever its accumulator holds
+                    const bool empty = l_out == 0.f;
+                    const float inv = final_rows ? 1.f / l_out : 1.f;
+                    const int token = blk * P.tokens_per_rb + rb_token;
+                    const int hq = s.g * G + row - rb_token * G;
+                    const int64_t out_row = (int64_t)(s.row0 + token) * a.Hq + hq;
+                    const int64_t rec = ((int64_t)blockIdx.x * 2 + slot) * kPairRows + blk * 128 + row;
+                    __nv_bfloat16* dst_o = reinterpret_cast<__nv_bfloat16*>(a.O) + out_row * D;
+                    float* dst_p = P.part_o + rec * D;                  // 128-byte aligned (workspace carve)
+                    const bool wide = (reinterpret_cast<uintptr_t>(dst_o) & 31) == 0;
+#pragma unroll 1
+                    for (int col = 0; col < D; col += 16) {
+                        uint32_t o[16], o2[16];
+                        tmem_ld16(tO + blk * 128 + col, o);
+                        if (merge) tmem_ld16(tO + 128 + col, o2);
+                        tmem_wait_ld();
+                        float v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(o[e]) * w0;
+                        if (merge) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = fmaf(__uint_as_float(o2[e]), w1, v[e]);
+                        }
+                        if (row_live) {
+                            uint32_t w[8];
+                            if (final_rows) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const __nv_bfloat162 t2 = __floats2bfloat162_rn(empty ? 0.f : v[2 * e] * inv, empty ? 0.f : v[2 * e + 1] * inv);
+                                    w[e] = *reinterpret_cast<const uint32_t*>(&t2);
+                                }
+                                if (wide) {
+                                    st_global_32b(dst_o + col, w);
+                                } else {
+                                    *reinterpret_cast<uint4*>(dst_o + col) = make_uint4(w[0], w[1], w[2], w[3]);
+                                    *reinterpret_cast<uint4*>(dst_o + col + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[q * 8 + e]);
+                                    st_global_32b(dst_p + col + q * 8, w);
+                                }
+                            }
+                        }
+                    }
+                    if (row_live) {
+                        if (!final_rows) P.part_ml[rec] = make_float2(empty ? -CUDART_INF_F : m_out, l_out);
+                        else if (a.lse != nullptr) a.lse[out_row] = empty ? -CUDART_INF_F : lse_of(m_out, l_out);
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.bar_ofree[blk]);
+            }
+        }
+    } else {
+        regs_dec<kIssueRegs>();
+        chain_sync();                            // every global access of the CTA comes behind one
+        if (warp == kProducerWarp) {
+            // =================================== TMA producer ===================================
+            // The whole warp walks the loop; lane p looks up and fetches page p of a tile (up to eight boxes per tile), the
+            // leading lane does the waits, the byte counts and Q.
+            const bool lead = lane == 0;
+            const bool usable = (smem_u32(smem_raw) & 1023u) == 0 && st.tmem_base == 0;     // (else the tiles would not sit on their swizzle boundary)
+            if (!usable && lead) set_status(P.status, RADAR_ERR_CUDA);
+            ChunkPieces& cut = st.cut;
+            long long tot;
+            Walk<Costs> cur = first_segment<Costs>(P, blockIdx.x, tot);
+            if (!usable) cur.t0 = cur.t1 = 0;
+            __syncwarp();
+            if (lead) { cut.unit.valid = 0; cut.tot = tot; }
+            uint32_t k_slot = 0, k_par = 1, v_slot = 0, v_par = 1;   // ring slot to fill next and the phase that frees it
+            const int n_cache_pages = (int)(a.cache_rows / a.page_size);                       // (cache_rows: below 2^31)
+            const int box_shift = __ffs(min(a.page_size, kTileKeys)) - 1, tiles_per_page = max(a.page_size / kTileKeys, 1);
+            auto first_page = [&](int t) { return tiles_per_page > 1 ? t / tiles_per_page : t << (7 - box_shift); };     // of tile t
+            // asks for the lines of the block table that tiles [t0, t1) of a request are looked up in
+            auto fetch_pages = [&](int b, int t0, int t1) {
+                const int last = min(first_page(t1), a.max_pages - 1);
+                for (int i = first_page(t0) + lane * 32; i <= last; i += 32 * 32)
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(a.block_table + (long long)b * a.max_pages + i));
+            };
+            for (uint32_t seg = 0;; ++seg) {
+                const bool on = cur.valid();
+                const int b = cur.b, g = cur.g, n = cur.t1 - cur.t0, t0 = cur.t0, row0 = cur.u.row0;
+                const int keys = min(cur.u.keys, max(cur.u.seen + cur.u.tokens - 1, 0));
+                const bool two = cur.u.rows > P.rb_rows;
+                if (lead) {
+                    ok = mbar_wait_while(ok, &st.bar_segempty[seg % kSegRing], ((seg / kSegRing) & 1) ^ 1);
+                    Segment s;                       // (behind a wait that ran out the others are sent home)
+                    s.n = on && ok ? n : 0; s.t0 = t0; s.nt = cur.u.nt; s.seen = cur.u.seen; s.keys = keys; s.rows = cur.u.rows; s.row0 = row0; s.g = g;
+                    st.seg[seg % kSegRing] = s;
+                    mbar_arrive(&st.bar_segfull[seg % kSegRing]);
+                }
+                if (!on) break;
+                if (lead && t0 == 0 && n < cur.u.nt) {               // necessarily the last segment of this CTA
+                    cut.unit.valid = 1; cut.unit.row0 = row0; cut.unit.g = g; cut.unit.slot = seg == 0 ? 0 : 1; cut.unit.rows = cur.u.rows;
+                    cut.nt = cur.u.nt; cut.w = cur.u.w; cut.size_keys = cur.u.keys; cut.u0 = cur.U;
+                }
+                cur.next(P);
+                // Order: the first K tile(s), Q (behind them, for its slot is free only after the last S of the segment before; the
+                // CTA's first segment finds it free), then V(i), K(i + la), the order in which the MMA warp consumes them.
+                const int la = two ? 1 : 2;
+#pragma unroll 1
+                for (int j = -2 * la; j < 2 * n; ++j) {              // even: V(j / 2), odd: K(j / 2 + la)
+                    const bool is_k = (j & 1) != 0;
+                    const int i = (j >> 1) + (is_k ? la : 0);
+                    if (i >= 0 && i < n) {
+                        const int t = t0 + i;
+                        // one box per page (or per tile when a page holds whole tiles); only pages that hold keys which the unit sees are
+                        // fetched, what stays stale in the slot is masked / never read.  The pages are looked up while the
+                        // slot is not free yet.
+                        const int per = min(a.page_size, kTileKeys);
+                        const int n_ld = (min(kTileKeys, keys - t * kTileKeys) + per - 1) >> box_shift;
+                        int page_row = 0;
+                        if (lane < n_ld) {
+                            const int index = first_page(t) + lane;
+                            int page = a.block_table[(long long)b * a.max_pages + index];
+                            if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
+                            page_row = page * a.page_size + (tiles_per_page > 1 ? (t - index * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
+                        }
+                        const uint32_t slot = is_k ? k_slot : v_slot;
+                        uint64_t* full = is_k ? &st.bar_kfull[slot] : &st.bar_vfull[slot];
+                        unsigned char* dst = (is_k ? sK : sV) + slot * SM::kTileBytes;
+                        if (lead) ok = mbar_wait_while(ok, is_k ? &st.bar_kempty[slot] : &st.bar_vempty[slot], is_k ? k_par : v_par);
+                        ok = __shfl_sync(kFull, ok, 0);
+                        if (!ok) break;                              // (the ring's position stays that of the last load)
+                        if (is_k) { if (++k_slot == RK) { k_slot = 0; k_par ^= 1; } }
+                        else if (++v_slot == RV) { v_slot = 0; v_par ^= 1; }
+                        if (lead) mbar_arrive_expect_tx(full, n_ld * per * D * 2);
+                        __syncwarp();
+                        if (lane < n_ld)
+                            for (int h = 0; h < H; ++h)
+                                tma_load_3d(dst + h * (kTileKeys * 128) + lane * per * 128, is_k ? &tmK : &tmV, full, h * 64, g, page_row);
+                    }
+                    if (j == (seg == 0 ? -2 * la : -1) && lead) {
+                        ok = mbar_wait_while(ok, &st.bar_qempty, (seg & 1) ^ 1);
+                        const int blocks = two ? 2 : 1;
+                        if (ok) {
+                            st.q_last = seg & 1;
+                            mbar_arrive_expect_tx(&st.bar_qfull, blocks * P.rb_rows * D * 2);   // rows past rb_rows stay stale: never read back
+                            for (int q = 0; q < blocks; ++q)
+                                for (int h = 0; h < H; ++h)
+                                    tma_load_3d(sQ + q * SM::kQBlock + h * (128 * 128), &tmQ, &st.bar_qfull, h * 64, g * G, row0 + q * P.tokens_per_rb);
+                        }
+                    }
+                    if (j == 0 && cur.valid()) fetch_pages(cur.b, cur.t0, cur.t1);
+                }
+            }
+            __syncwarp();
+            write_cut<Costs>(P, blockIdx.x, cut);
+            if (lead) { st.k_next = k_slot | k_par << 8; st.v_next = v_slot | v_par << 8; }
+            __syncwarp();
+        } else if (warp == kMmaWarp) {
+            // =================================== MMA issuer ===================================
+            // The warp runs converged: every lane waits on the barriers and executes the same straight-line issue
+            // sequences with warp-uniform descriptor words, and the elected lane issues the instructions and the
+            // commits (predicated, no branch around them).  No control flow depends on a wait's outcome: after a wait that ran out the
+            // predicate is off and the loops run dry.
+            constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTileKeys, false, false);
+            constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, false, true);
+            // high word of every shared-memory descriptor (stride between 8-row groups 1024 B, version, swizzle)
+            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            constexpr uint32_t kHalfTile = kTileKeys * 128 >> 4;     // between the 64-column blocks of a tile
+            const uint32_t q_lo = ((smem_u32(sQ) & 0x3ffff) >> 4) | (1u << 16);
+            const uint32_t k_lo = ((smem_u32(sK) & 0x3ffff) >> 4) | (1u << 16);
+            const uint32_t v_lo = ((smem_u32(sV) & 0x3ffff) >> 4) | (kHalfTile << 16);     // N-major: 64-column blocks are a half tile apart
+            const uint32_t elected = elect_one();
+            uint32_t k_next = 0, k_par = 0, v_next = 0, v_par = 0;   // ring slot to take next and its phase parity
+            uint32_t p_par[2] = {0, 0};              // phase parity of the next P tile per group
+            // The segment's shape comes from memory; passing it through a broadcast from lane 0 tells the
+            // compiler that it is the same in every lane.
+            auto uni = [](int v) { return __shfl_sync(kFull, v, 0); };
+            Segment s;
+            for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+                const int seg_t0 = uni(s.t0), n = uni(s.n), keys = uni(s.keys);
+                const bool two = uni(s.rows) > P.rb_rows;
+                ok = mbar_wait_while(ok, &st.bar_qfull, seg & 1);
+                uint32_t k_slot = 0, v_slot = 0;      // ring slots of the K and V tiles in use
+                bool acc[2] = {false, false};         // accumulator holds a product of this segment
+                auto take_v = [&]() {
+                    v_slot = v_next;
+                    ok = mbar_wait_while(ok, &st.bar_vfull[v_slot], v_par);
+                    if (++v_next == RV) { v_next = 0; v_par ^= 1; }
+                };
+                auto take_k = [&]() {
+                    k_slot = k_next;
+                    ok = mbar_wait_while(ok, &st.bar_kfull[k_slot], k_par);
+                    if (++k_next == RK) { k_next = 0; k_par ^= 1; }
+                };
+                // the accumulator's first product of the segment: the epilogue of the previous one has read it
+                auto take_o = [&](const int q) {
+                    if (!acc[q]) ok = mbar_wait_while(ok, &st.bar_ofree[q], (seg & 1) ^ 1);
+                };
+
+                // ---- O[q] (+)= P[q] V for tile i (q is a literal at every call site) ----
+                auto pv = [&](const int q, const int i, const bool fresh_v, const bool release_v) {
+                    const int valid = min(kTileKeys, keys - (seg_t0 + i) * kTileKeys);
+                    const int ksteps = (valid + 15) >> 4;
+                    if (fresh_v) {
+                        take_v();
+                        if (valid < ksteps * 16) {
+                            // rows past the last key meet P = 0; they must not hold NaN/Inf bit patterns
+                            unsigned char* vtile = sV + v_slot * SM::kTileBytes;
+                            const int nrows = ksteps * 16 - valid;
+#pragma unroll 1
+                            for (int e = lane; e < nrows * 8 * H; e += 32) {
+                                const int h = e / (nrows * 8), rem = e % (nrows * 8);
+                                const int r = valid + rem / 8, c = rem % 8;
+                                *reinterpret_cast<uint4*>(vtile + h * (kTileKeys * 128) + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                    }
+                    take_o(q);
+                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    p_par[q] ^= 1;
+                    tc_fence_after_sync();
+                    const uint32_t go = ok ? elected : 0u;
+                    const uint32_t b_lo = v_lo + v_slot * (SM::kTileBytes >> 4);
+                    mma_ts_x4(go, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
+                    mma_ts_x4(go, ksteps - 4, tmem + 256 + q * 128, tmem + q * 128 + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
+                    acc[q] = true;
+                    if (release_v) mma_commit_if(go, &st.bar_vempty[v_slot]);
+                    if (two ? i == n - 1 : i + 2 >= n) mma_commit_if(go, &st.bar_odone[q]);
+                };
+                // ---- S[q] = Q K^T for tile si.  Nothing in tensor memory changes hands here: K arrives through the
+                // async proxy, and the buffer was last read by this thread's own P V, which runs first. ----
+                auto qk = [&](const int q, const int si, const bool fresh_k, const bool release_k) {
+                    if (fresh_k) take_k();
+                    const uint32_t go = ok ? elected : 0u;
+                    const uint32_t a0 = q_lo + (two ? q : 0) * (SM::kQBlock >> 4);
+                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
+                    mma_ss_x4(go, tmem + q * 128, a0, b0, kDescHi, idesc_s, false);
+                    if (D == 128) mma_ss_x4(go, tmem + q * 128, a0 + kHalfTile, b0 + kHalfTile, kDescHi, idesc_s, true);   // second 64-column block
+                    if (release_k) mma_commit_if(go, &st.bar_kempty[k_slot]);
+                    mma_commit_if(go, &st.bar_sfull[q]);
+                    // the last S of the segment: Q may be overwritten once it has run
+                    if (si == n - 1 && release_k) mma_commit_if(go, &st.bar_qempty);
+                };
+                // Schedule.  Two live row blocks: group s owns row block s; per tile PV0(i) S0(i+1) PV1(i) S1(i+1),
+                // both groups sharing K(i+1) and V(i).  One live row block: the groups take alternate tiles,
+                // PV(i) S(i+2) for group i & 1.  S of the first tile(s) comes from the iterations with i < 0.
+                // Steady state (all tiles involved are full): the same steps with nothing to decide,
+                // so that the issuing warp executes as few instructions per MMA as possible.  The waits for K and V, which are
+                // there most of the time, stand where the warp would wait for P.
+                auto full = [&](const int q, const uint32_t a0, const bool fresh, const bool release) {
+                    static_assert(kFirstKeys == 64 && kTileKeys == 128, "four steps before and behind the second wait");
+                    const uint32_t o_col = tmem + 256 + q * 128, p_col = tmem + q * 128;
+                    if (fresh) take_v();
+                    take_o(q);
+                    const uint32_t b_lo = v_lo + v_slot * (SM::kTileBytes >> 4);
+                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
+                    tc_fence_after_sync();
+                    mma_ts_x4(ok ? elected : 0u, o_col, p_col, b_lo, kDescHi, idesc_pv, acc[q]);
+                    if (fresh) take_k();
+                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
+                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    p_par[q] ^= 1;
+                    acc[q] = true;
+                    tc_fence_after_sync();
+                    const uint32_t go = ok ? elected : 0u;
+                    mma_ts_x4(go, o_col, p_col + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
+                    if (release) mma_commit_if(go, &st.bar_vempty[v_slot]);
+                    mma_ss_x4(go, p_col, a0, b0, kDescHi, idesc_s, false);
+                    if (D == 128) mma_ss_x4(go, p_col, a0 + kHalfTile, b0 + kHalfTile, kDescHi, idesc_s, true);
+                    mma_commit_if(go, &st.bar_sfull[q]);
+                    if (release) mma_commit_if(go, &st.bar_kempty[k_slot]);
+                };
+                const uint32_t a_q0 = q_lo, a_q1 = q_lo + (SM::kQBlock >> 4);
+                const int n_full = min(n, keys / kTileKeys - seg_t0);   // tiles [0, n_full) of the segment are full
+                if (two) {
+#pragma unroll 1
+                    for (int i = -1; i < n; ++i) {
+                        if (i >= 0 && i + 2 < n_full) {           // tiles i and i+1 full, and S(i+1) is not the segment's last
+                            full(0, a_q0, true, false);
+                            full(1, a_q1, false, true);
+                        } else {
+                            if (i >= 0) pv(0, i, true, false);
+                            if (i + 1 < n) qk(0, i + 1, true, false);
+                            if (i >= 0) pv(1, i, false, true);
+                            if (i + 1 < n) qk(1, i + 1, false, true);
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = -2; i < n; i += 2) {
+                        if (i >= 0 && i + 4 < n_full) {           // tiles i to i+3 full, S(i+3) not the last
+                            full(0, a_q0, true, true);
+                            full(1, a_q0, true, true);
+                        } else {
+                            if (i >= 0) pv(0, i, true, true);
+                            if (i + 2 < n) qk(0, i + 2, true, true);
+                            if (i >= 0 && i + 1 < n) pv(1, i + 1, true, true);
+                            if (i + 3 < n) qk(1, i + 3, true, true);
+                        }
+                    }
+                }
+            }
+            // no product may read shared memory or write tensor memory that the CTA has given back
+            mma_commit_if(elected, &st.bar_idle);
+            ok &= mbar_drain(&st.bar_idle, 0);
+            __syncwarp();
+        }
+    }
+
+    // ---- teardown ----
+    if (!ok) st.abort = 1;
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        if (lane == 0 && st.abort) {
+            // No load may land in shared memory that the CTA has left.  (Without an abort the roles have waited for every one.)
+            const uint32_t k = st.k_next, v = st.v_next;
+            mbar_drain(&st.bar_qfull, st.q_last);
+            for (int i = 0; i < RK; ++i) mbar_drain(&st.bar_kfull[i], last_armed_parity(i, k & 255, k >> 8));
+            for (int i = 0; i < RV; ++i) mbar_drain(&st.bar_vfull[i], last_armed_parity(i, v & 255, v >> 8));
+            set_status(P.status, RADAR_ERR_TIMEOUT);
+        }
+        __syncwarp();
+        tmem_dealloc(st.tmem_base, 512);
+    }
+}
+
+// [rows][heads][d] bf16, row_stride elements between rows; box = (64 elements, box_heads, box_rows), 128-byte swizzle, zero fill
+bool make_map(CUtensorMap* tm, const void* base, int d, int heads, long long rows, long long row_stride, int box_heads, int box_rows) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)rows};
+    cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)row_stride * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int most_ctas(const radar_ctx* ctx) { return std::min(ctx->sm_count, kMaxCtas); }
+
+template <int D>
+int launch_d(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream) {
+    const radar_chunk_attn_args& a = P.a;
+    CUtensorMap tmQ, tmK, tmV;
+    const int box = std::min(a.page_size, kTileKeys);          // rows of a box
+    if (!make_map(&tmQ, a.Q, D, a.Hq, a.n_rows, a.q_row_stride, P.G, P.tokens_per_rb) ||
+        !make_map(&tmK, a.Kc, D, a.Hkv, a.cache_rows, (long long)a.Hkv * D, 1, box) ||
+        !make_map(&tmV, a.Vc, D, a.Hkv, a.cache_rows, (long long)a.Hkv * D, 1, box))
+        return RADAR_ERR_CUDA;
+    RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CHUNK_TC + (D == 128), chunk_attn_tc_kernel<D>, (size_t)Smem<D>::kDynamic));
+    {
+        radar_launch_scope scope(ctx, RADAR_K_CHUNK_ATTN, stream);
+        RADAR_CUDA_CHECK(launch_chained(chunk_attn_tc_kernel<D>, dim3((unsigned)P.n_cta), dim3(kChunkThreads), (size_t)Smem<D>::kDynamic, stream, tmQ, tmK, tmV, P));
+    }
+    return chunk_combine<__nv_bfloat16, D>(ctx, P, stream);
+}
+
+}  // namespace
+
+bool chunk_tc_supported(const radar_chunk_attn_args* a) { return a->dtype == RADAR_BF16 && encode_fn() != nullptr; }
+
+size_t chunk_tc_workspace_bytes(const radar_ctx* ctx, int d) { return chunk_partial_bytes((size_t)most_ctas(ctx), kPairRows, d); }
+
+int chunk_tc_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream_t stream) {
+    ChunkParams P = chunk_params(ctx, *a, a->Hq / a->Hkv, 128, 2);
+    // one CTA per SM, but at least two tiles per CTA when every request is as large as the bounds
+    const long long units = (long long)a->B * a->Hkv * ((a->max_new + P.unit_tokens - 1) / P.unit_tokens);
+    const long long tiles = units * std::max(1, (a->max_cache_len + kTileKeys - 1) / kTileKeys);
+    P.n_cta = (int)std::max<long long>(1, std::min<long long>(most_ctas(ctx), (tiles + 1) / 2));
+    chunk_carve(P);
+    return a->d == 128 ? launch_d<128>(ctx, P, stream) : launch_d<64>(ctx, P, stream);
+}
+
+}  // namespace radar

@@ -33,6 +33,10 @@ enum radar_kernel_id {
     RADAR_K_CACHE_LOAD,
     RADAR_K_CACHE_ATTN,
     RADAR_K_CACHE_COMBINE,
+    RADAR_K_ROTATE,             // rows turned by their positions
+    RADAR_K_PAGED_STORE,        // paged cache: rows in, keys turned on the way
+    RADAR_K_CHUNK_ATTN,         // attention of new tokens over the paged cache
+    RADAR_K_CHUNK_COMBINE,
     RADAR_K_COUNT
 };
 
@@ -52,7 +56,9 @@ enum radar_smem_slot {
     RADAR_SMEM_CACHE_EXTEND = RADAR_SMEM_CACHE_ATTN + 4,   // + (several blocks)
     RADAR_SMEM_CACHE_ATTN_TC = RADAR_SMEM_CACHE_EXTEND + 2,   // + 2 * (d == 128) + two
     RADAR_SMEM_CACHE_SMALL = RADAR_SMEM_CACHE_ATTN_TC + 4,    // + 2 * (d == 128) + row tiles of eight - 1
-    RADAR_SMEM_COUNT = RADAR_SMEM_CACHE_SMALL + 4
+    RADAR_SMEM_CHUNK_TC = RADAR_SMEM_CACHE_SMALL + 4,         // + (d == 128)
+    RADAR_SMEM_CHUNK_FMA = RADAR_SMEM_CHUNK_TC + 2,           // + (d == 128)
+    RADAR_SMEM_COUNT = RADAR_SMEM_CHUNK_FMA + 2
 };
 
 struct radar_ctx {

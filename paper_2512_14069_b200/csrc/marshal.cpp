@@ -408,8 +408,164 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// ---- rows with positions and the paged cache: as above, behind the number of the current device, which every tensor has to be on --------
+thread_local int current_device = -1;
+void here(const at::Tensor* t, const char* name) {
+    if (t != nullptr && t->device().index() != current_device) { PyErr_Format(PyExc_ValueError, "%s: not on the current device", name); throw Bad(); }
+}
+const at::Tensor* rows_of(PyObject* v, const char* name, int64_t min_dim, int64_t max_dim) {
+    const at::Tensor* t = tensor(v, name, true);
+    if (t == nullptr) return nullptr;
+    here(t, name);
+    if (t->dim() < min_dim || t->dim() > max_dim) { PyErr_Format(PyExc_ValueError, "%s: a tensor of another number of dimensions", name); throw Bad(); }
+    strided_rows(*t, t->dim(), name);
+    for (int64_t i = 0; i < t->dim(); ++i) need(t->size(i) <= INT_MAX, "rows, heads or channels: more than an int counts");
+    return t;
+}
+template <typename T>
+T* packed_here(PyObject* v, const char* name, at::ScalarType dtype, bool optional = false, const at::Tensor** out = nullptr) {
+    const at::Tensor* t;
+    T* p = packed<T>(v, name, dtype, optional, &t);
+    here(t, name);
+    if (out != nullptr) *out = t;
+    return p;
+}
+int64_t row_stride(const at::Tensor& t) { return t.size(-3) > 1 ? t.stride(-3) : t.size(-2) * t.size(-1); }
+int64_t layer_stride(const at::Tensor& t) { return t.dim() == 4 && t.size(0) > 1 ? t.stride(0) : 0; }
+
+// pos, inv_freq, pair_axis, neighbours
+void rotation(PyObject* const* v, int64_t n, radar_rotation& r) {
+    const at::Tensor *pos, *freq, *axis;
+    r.pos = packed_here<int32_t>(v[0], "pos", at::kInt, true, &pos);
+    if (pos == nullptr) return;
+    need(pos->dim() == 1 || pos->dim() == 2, "pos: expected [rows] or [axes, rows]");
+    need(pos->size(-1) >= n, "pos: fewer positions than rows");
+    r.pos_stride = pos->size(-1);
+    r.n_axes = pos->dim() == 2 ? static_cast<int>(pos->size(0)) : 1;
+    r.inv_freq = packed_here<float>(v[1], "inv_freq", at::kFloat, false, &freq);
+    need(freq->numel() <= INT_MAX, "inv_freq: too large");
+    r.n_pairs = static_cast<int>(freq->numel());
+    r.pair_axis = packed_here<uint8_t>(v[2], "pair_axis", at::kByte, true, &axis);
+    need(axis == nullptr || axis->numel() == freq->numel(), "pair_axis and inv_freq disagree");
+    const int on = PyObject_IsTrue(v[3]);
+    if (on < 0) throw Bad();
+    r.neighbours = on;
+}
+int set_device(PyObject* v) { return current_device = small(v, "device"); }
+
+// device, Q, Q_out, K, K_out, pos, inv_freq, pair_axis, neighbours, inverse
+PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return cache_call(args, n, 13, [](PyObject* const* v) {
+        radar_rotate_args a = {};
+        set_device(v[0]);
+        const at::Tensor *Q = rows_of(v[1], "Q", 3, 3), *Qo = rows_of(v[2], "Q_out", 3, 3), *K = rows_of(v[3], "K", 3, 3), *Ko = rows_of(v[4], "K_out", 3, 3);
+        const at::Tensor* X = Q != nullptr ? Q : K;
+        need(X != nullptr, "Q or K: expected a tensor");
+        need((Q == nullptr) == (Qo == nullptr) && (K == nullptr) == (Ko == nullptr), "Q_out and K_out: one for each of Q and K");
+        for (const at::Tensor* t : {Q, Qo, K, Ko})
+            need(t == nullptr || (t->scalar_type() == X->scalar_type() && t->size(0) == X->size(0) && t->size(2) == X->size(2)), "Q, K and their outputs disagree in rows, d or dtype");
+        need((Q == nullptr || Q->sizes() == Qo->sizes()) && (K == nullptr || K->sizes() == Ko->sizes()), "Q_out and K_out: the shapes of Q and K");
+        a.dtype = dtype_code(*X);
+        a.n_rows = X->size(0);
+        a.d = static_cast<int>(X->size(2));
+        if (Q != nullptr) { a.Hq = static_cast<int>(Q->size(1)); a.Q = Q->data_ptr(); a.Q_out = Qo->data_ptr(); a.q_row_stride = row_stride(*Q); a.q_out_row_stride = row_stride(*Qo); }
+        if (K != nullptr) { a.Hkv = static_cast<int>(K->size(1)); a.K = K->data_ptr(); a.K_out = Ko->data_ptr(); a.k_row_stride = row_stride(*K); a.k_out_row_stride = row_stride(*Ko); }
+        rotation(v + 5, a.n_rows, a.rotation);
+        need(a.rotation.pos != nullptr, "pos: expected a tensor");
+        const int on = PyObject_IsTrue(v[9]);
+        if (on < 0) throw Bad();
+        a.inverse = on;
+        return a;
+    });
+}
+
+// device, K, V, slots, src_row, Kc, Vc, Q, Q_out, pos, inv_freq, pair_axis, neighbours
+PyObject* paged_store(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return cache_call(args, n, 16, [](PyObject* const* v) {
+        radar_paged_store_args a = {};
+        set_device(v[0]);
+        const at::Tensor *K = rows_of(v[1], "K", 3, 4), *V = rows_of(v[2], "V", 3, 4), *slots, *src, *Kc, *Vc;
+        need(K != nullptr && V != nullptr, "K, V: expected tensors");
+        need(K->sizes() == V->sizes() && K->scalar_type() == V->scalar_type() && same_strides(*K, *V), "K and V must share shape, dtype and strides");
+        const bool layers = K->dim() == 4;
+        a.n_layers = layers ? static_cast<int>(K->size(0)) : 1;
+        a.Hkv = static_cast<int>(K->size(-2));
+        a.d = static_cast<int>(K->size(-1));
+        a.dtype = dtype_code(*K);
+        a.n_rows = K->size(-3);
+        a.K = K->data_ptr(); a.V = V->data_ptr();
+        a.kv_row_stride = row_stride(*K); a.kv_layer_stride = layer_stride(*K);
+        a.slots = packed_here<int64_t>(v[3], "slots", at::kLong, false, &slots);
+        a.src_row = packed_here<int32_t>(v[4], "src_row", at::kInt, true, &src);
+        a.n_tokens = slots->numel();
+        need((src == nullptr ? a.n_rows : src->numel()) >= a.n_tokens, "fewer rows (or entries of src_row) than slots");
+        a.Kc = packed_here<void>(v[5], "Kc", K->scalar_type(), false, &Kc);
+        a.Vc = packed_here<void>(v[6], "Vc", K->scalar_type(), false, &Vc);
+        const int64_t row = static_cast<int64_t>(a.Hkv) * a.d, layer = a.n_layers > 0 ? Kc->numel() / a.n_layers : 0;
+        need(Kc->dim() >= 3 && Kc->sizes() == Vc->sizes() && Kc->size(-1) == a.d && Kc->size(-2) == a.Hkv && (!layers || (Kc->dim() >= 4 && Kc->size(0) == a.n_layers)),
+             "Kc, Vc: expected [cache rows, Hkv, d] (the rows in as many dimensions as there are), behind the layers' dimension if K has one");
+        a.cache_rows = row > 0 ? layer / row : 0;
+        a.cache_layer_stride = a.n_layers > 1 ? layer : 0;
+        const at::Tensor *Q = rows_of(v[7], "Q", 3, 4), *Qo = rows_of(v[8], "Q_out", 3, 4);
+        need((Q == nullptr) == (Qo == nullptr), "Q_out: one for Q, and none without");
+        if (Q != nullptr) {
+            need(Q->dim() == K->dim() && Qo->dim() == K->dim() && Q->scalar_type() == K->scalar_type() && Qo->scalar_type() == K->scalar_type() && Q->size(-3) == a.n_rows &&
+                     Q->size(-1) == a.d && Qo->size(-1) == a.d && Qo->size(-2) == Q->size(-2) && Qo->size(-3) >= a.n_tokens && (!layers || (Q->size(0) == a.n_layers && Qo->size(0) == a.n_layers)),
+                 "Q and Q_out disagree with K in layers, rows, d or dtype");
+            a.Hq = static_cast<int>(Q->size(-2));
+            a.Q = Q->data_ptr(); a.Q_out = Qo->data_ptr();
+            a.q_row_stride = row_stride(*Q); a.q_layer_stride = layer_stride(*Q);
+            a.q_out_row_stride = row_stride(*Qo); a.q_out_layer_stride = layer_stride(*Qo);
+        }
+        rotation(v + 9, a.n_tokens, a.rotation);
+        return a;
+    });
+}
+
+// device, Q, q_start, Kc, Vc, page_size, block_table, cache_len, max_new, max_cache_len, O, workspace, lse, scale
+PyObject* chunk_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return cache_call(args, n, 17, [](PyObject* const* v) {
+        radar_chunk_attn_args a = {};
+        set_device(v[0]);
+        const at::Tensor *Q = rows_of(v[1], "Q", 3, 3), *start, *Kc, *Vc, *table, *len, *O, *lse, *ws;
+        need(Q != nullptr, "Q: expected a tensor");
+        a.dtype = dtype_code(*Q);
+        a.Hq = static_cast<int>(Q->size(1));
+        a.d = static_cast<int>(Q->size(2));
+        a.n_rows = Q->size(0);
+        a.Q = Q->data_ptr();
+        a.q_row_stride = row_stride(*Q);
+        a.q_start = packed_here<int32_t>(v[2], "q_start", at::kInt, false, &start);
+        a.Kc = packed_here<void>(v[3], "Kc", Q->scalar_type(), false, &Kc);
+        a.Vc = packed_here<void>(v[4], "Vc", Q->scalar_type(), false, &Vc);
+        need(Kc->dim() >= 3 && Kc->sizes() == Vc->sizes() && Kc->size(-1) == a.d && Kc->size(-2) > 0 && Kc->size(-2) <= INT_MAX && a.d > 0,
+             "Kc, Vc: expected [cache rows, Hkv, d] (the rows in as many dimensions as there are) with the d of Q");
+        a.Hkv = static_cast<int>(Kc->size(-2));
+        a.cache_rows = Kc->numel() / (Kc->size(-2) * a.d);
+        a.page_size = small(v[5], "page_size");
+        a.block_table = packed_here<int32_t>(v[6], "block_table", at::kInt, false, &table);
+        a.cache_len = packed_here<int32_t>(v[7], "cache_len", at::kInt, false, &len);
+        a.max_new = small(v[8], "max_new");
+        a.max_cache_len = small(v[9], "max_cache_len");
+        a.O = packed_here<void>(v[10], "O", Q->scalar_type(), false, &O);
+        a.workspace = packed_here<void>(v[11], "workspace", at::kByte, false, &ws);
+        a.workspace_bytes = static_cast<size_t>(ws->numel());
+        a.lse = packed_here<float>(v[12], "lse", at::kFloat, true, &lse);
+        const double scale = PyFloat_AsDouble(v[13]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Bad();
+        a.scale = static_cast<float>(scale);
+        const int64_t B = len->numel();
+        need(B <= INT_MAX && start->numel() == B + 1 && table->dim() == 2 && table->size(0) == B && table->size(1) <= INT_MAX, "q_start [B + 1], block_table [B, max_pages] and cache_len [B] disagree about B");
+        need(O->sizes() == Q->sizes() && (lse == nullptr || (lse->dim() == 2 && lse->size(0) == a.n_rows && lse->size(1) == a.Hq)), "O and lse [rows, Hq]: the shape of Q");
+        a.B = static_cast<int>(B);
+        a.max_pages = static_cast<int>(table->size(1));
+        return a;
+    });
+}
+
 #define RADAR_FASTCALL(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef cache_methods[] = {RADAR_FASTCALL(cache_extend), RADAR_FASTCALL(cache_store), RADAR_FASTCALL(cache_load), RADAR_FASTCALL(cache_attention), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef cache_methods[] = {RADAR_FASTCALL(cache_extend), RADAR_FASTCALL(cache_store), RADAR_FASTCALL(cache_load), RADAR_FASTCALL(cache_attention),
+                               RADAR_FASTCALL(rotate), RADAR_FASTCALL(paged_store), RADAR_FASTCALL(chunk_attention), {nullptr, nullptr, 0, nullptr}};
 
 PyType_Slot filler_slots[] = {{Py_tp_new, reinterpret_cast<void*>(filler_new)},
                               {Py_tp_call, reinterpret_cast<void*>(filler_call)},

@@ -2,26 +2,17 @@
 // (cache_attention_tc.cu): units of (layer, sequence, KV head, row-block pair), their tiles laid end to end and cut into equal
 // ranges, the pieces' records, tensor maps and grid.
 #pragma once
-#include <cuda.h>
-
 #include <algorithm>
 
-#include "common.cuh"
-#include "tc05.cuh"
+#include "attn_tiles.cuh"
 
 namespace radar {
 namespace {
 
-using namespace tc05;
-
 // how the prefix is held: what the tile space has to look up
 enum CacheKind { kContiguous = 0, kPaged = 1, kFourBit = 2 };
 
-constexpr int kTileKeys = 128;       // keys per prefix tile
-constexpr int kFirstKeys = 64;       // keys of a tile whose products start before the rest of its probabilities is there
 constexpr int kTreeKeys = 64;        // keys of the tree tile (RADAR_MAX_NODES)
-constexpr int kPairRows = 256;       // query rows of a row-block pair (and the stride of partial records)
-constexpr float kRescaleThreshold = 8.f;   // in log2 units: P stays below 2^8
 
 // Written by every CTA of the attention kernel, read by the combine kernel: the pieces are worked out by the producer warp
 // behind its last load, where nothing waits for it, and not by every warp of the combine (two 64-bit divisions a piece).
@@ -66,43 +57,6 @@ struct TcParams {
     long long n_pages;
     int blocks_per_page, page_shift_blocks;      // blocks of 16 tokens of a page, log2 of it or -1
 };
-
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float y;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-    return y;
-}
-// one 32-byte store: a whole sector per lane (the epilogue's lanes write to different rows, so every store
-// instruction is split into one transaction per lane; with 16-byte stores each of them filled half a sector)
-__device__ __forceinline__ void st_global_32b(void* p, const uint32_t (&w)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
-// 2^x and the other steps of a probability, kept in the order in which they are written
-__device__ __forceinline__ float ex2_in_order(float x) {
-    float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float2 fma2_in_order(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm volatile("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-                 "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-                 : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 add2_in_order(float2 a, float2 b) {
-    float2 d;
-    asm volatile("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-                 : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ uint32_t bf16x2_in_order(float lo, float hi) {
-    uint32_t d;
-    asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
 
 // ---- the tile space of one class (unit index pp within a KV head) ---------------------------------
 // Positions are in cost units: a tile of a unit with two live row blocks (four MMAs) weighs cost_two, a tile of
@@ -275,27 +229,12 @@ __device__ __forceinline__ void write_cut_unit(const TcParams& P, int ci, const 
 }
 
 // What the other warps know of a segment.
-constexpr int kSegRing = 4;
 struct __align__(16) Segment {
     int n;                               // tiles; 0: there is no further segment
     int t0, nt, Pb, M, rows;             // first tile, tiles of the unit, prefix length, tree rows, live query rows
     int b, g, layer;
     int pad[3];
 };
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = []() -> EncodeTiledFn {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess) return nullptr;
-        return q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
-    }();
-    return fn;
-}
 
 // [layers][rows][heads][d] bf16 tensor (layer_stride elements between layers), box = (64 elements, box_heads,
 // box_rows, one layer), 128-byte swizzle, zero fill
