@@ -471,7 +471,7 @@ PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (Q != nullptr) { a.Hq = static_cast<int>(Q->size(1)); a.Q = Q->data_ptr(); a.Q_out = Qo->data_ptr(); a.q_row_stride = row_stride(*Q); a.q_out_row_stride = row_stride(*Qo); }
         if (K != nullptr) { a.Hkv = static_cast<int>(K->size(1)); a.K = K->data_ptr(); a.K_out = Ko->data_ptr(); a.k_row_stride = row_stride(*K); a.k_out_row_stride = row_stride(*Ko); }
         rotation(v + 5, a.n_rows, a.rotation);
-        need(a.rotation.pos != nullptr, "pos: expected a tensor");
+        need(v[5] != Py_None, "pos: expected a tensor");
         const int on = PyObject_IsTrue(v[9]);
         if (on < 0) throw Bad();
         a.inverse = on;

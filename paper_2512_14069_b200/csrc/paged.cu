@@ -12,7 +12,7 @@ namespace radar {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxRows = 4;              // rows of a block
+constexpr int kRows = 4;                 // rows of a block, where there are many
 constexpr int kMaxPairs = 512;
 
 struct PagedParams {
@@ -21,7 +21,7 @@ struct PagedParams {
     void* out[3];
     int64_t in_row[3], out_row[3], in_layer[3], out_layer[3];      // strides, elements
     int heads[3];
-    int d, rows;                         // channels of a head, rows of a block (at most kMaxRows)
+    int d;                               // channels of a head
     int turn_items, rest_items, copy_items;   // of a head: of its pairs, of the channels behind them, of a head that is not turned
     int rest_units, copy_units;          // ... the last two in units (an item is two of them, the last one perhaps one)
     int64_t n_tokens, n_rows, cache_rows;
@@ -68,98 +68,113 @@ __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
     return make_float2(c, s * sign);
 }
 
-// A block takes P.rows rows of one layer, its threads first the rows' angles, one each, into shared memory, then the items: two units of
-// a head that are turned together (or copied).  The first item is loaded ahead of the barrier.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 6) paged_rows_kernel(const PagedParams P) {
-    __shared__ __align__(16) float s_cos[kMaxRows * kMaxPairs], s_sin[kMaxRows * kMaxPairs];
+// A block takes up to R rows of one layer: its threads first load their items of all of these rows (two units of a head that are turned together, or
+// copied), then take the rows' angles, one each, into shared memory, then turn and store.  A thread's items stand at the same place in every row,
+// so where they lie is worked out once.
+template <typename T, int V, int R>
+__global__ void __launch_bounds__(kThreads, 4) paged_rows_kernel(const PagedParams P) {
+    extern __shared__ __align__(16) float s_angles[];
     chain_wait();
     const int pairs = P.r.n_pairs, layer = blockIdx.y;
-    const int64_t first = (int64_t)blockIdx.x * P.rows;
-    const int n = (int)min((int64_t)P.rows, P.n_tokens - first);
+    float *s_cos = s_angles, *s_sin = s_angles + R * pairs;
+    const int64_t first = (int64_t)blockIdx.x * R;
+    const int n = (int)min((int64_t)R, P.n_tokens - first);
     const int turned = P.turn_items + P.rest_items;              // items of a head that is turned
     const int q_items = P.heads[0] * turned, qk_items = q_items + P.heads[1] * turned, row_items = qk_items + P.heads[2] * P.copy_items;
-    const int total = n * row_items, step = gridDim.z * kThreads;
+    const int step = gridDim.z * blockDim.x;
 
-    struct Item {
-        const T *a, *b;                  // b NULL: one unit
-        T *to_a, *to_b;
-        int row, pair;                   // pair < 0: copied
-        Unit<T, V> x, y;
-    };
-    auto take = [&](int at, Item& it) {
-        const int r = at / row_items, e = at - r * row_items;
+    // the rows' places; from < 0: the row is left out
+    int64_t from[R], to[R];
+    bool bad = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t token = first + r;
+        from[r] = r < n ? token : -1;
+        to[r] = token;
+        if (r < n && P.src_row != nullptr) {
+            from[r] = P.src_row[token];
+            if (from[r] < 0 || from[r] >= P.n_rows) { bad = true; from[r] = -1; }
+        }
+        if (r < n && P.slots != nullptr) {
+            to[r] = P.slots[token];
+            if (to[r] >= P.cache_rows) { bad = true; to[r] = -1; }
+        }
+    }
+    if (bad && threadIdx.x == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
+
+    const T* in;                         // of the thread's item: its head in row 0
+    T* out;
+    int64_t in_row, out_row;
+    int u0, u1, pair;                    // first elements of its units (u1 < 0: it has one), its pairs' number (below 0: copied)
+    bool queries;
+    Unit<T, V> x[R], y[R];
+    auto here = [&](int r) { return from[r] >= 0 && (queries || to[r] >= 0); };
+    auto take = [&](int e) {
         const int what = e < q_items ? 0 : e < qk_items ? 1 : 2;
         const int in_part = e - (what == 0 ? 0 : what == 1 ? q_items : qk_items), per = what == 2 ? P.copy_items : turned;
         const int head = in_part / per, item = in_part - head * per;
-        const int64_t token = first + r;
-        int64_t from = token, to = token;
-        it.a = nullptr;
-        if (P.src_row != nullptr) {
-            from = P.src_row[token];
-            if (from < 0 || from >= P.n_rows) { set_status(P.status, RADAR_ERR_INVALID_ARG); return; }
-        }
-        if (what > 0 && P.slots != nullptr) {
-            to = P.slots[token];
-            if (to < 0) return;
-            if (to >= P.cache_rows) { set_status(P.status, RADAR_ERR_INVALID_ARG); return; }
-        }
-        int u0, u1;                      // the units' first elements
-        it.row = r;
-        it.pair = -1;
+        queries = what == 0;
+        pair = -1;
         if (what < 2 && item < P.turn_items) {
-            it.pair = item;
-            if (!P.r.neighbours) { u0 = item * V; u1 = u0 + pairs; }
-            else if (V > 1) { u0 = item * V; u1 = u0 + pairs; }      // (units in the first and in the second half: neighbouring lanes read neighbouring units)
-            else { u0 = 2 * item; u1 = u0 + 1; }
+            // (neighbours: a unit of the first and one of the second half of the pairs, so that neighbouring lanes have neighbouring units)
+            pair = item;
+            const bool lone = V == 1 && P.r.neighbours;
+            u0 = lone ? 2 * item : item * V;
+            u1 = lone ? u0 + 1 : u0 + pairs;
         } else {
             const int i = what < 2 ? item - P.turn_items : item, items = what < 2 ? P.rest_items : P.copy_items, units = what < 2 ? P.rest_units : P.copy_units;
-            const int base = what < 2 ? 2 * pairs : 0;
-            u0 = base + i * V;
+            u0 = (what < 2 ? 2 * pairs : 0) + i * V;
             u1 = i + items < units ? u0 + items * V : -1;
         }
-        const T* in = reinterpret_cast<const T*>(P.in[what]) + layer * P.in_layer[what] + from * P.in_row[what] + (int64_t)head * P.d;
-        T* out = reinterpret_cast<T*>(P.out[what]) + layer * P.out_layer[what] + to * P.out_row[what] + (int64_t)head * P.d;
-        it.a = in + u0; it.to_a = out + u0;
-        it.b = u1 >= 0 ? in + u1 : nullptr; it.to_b = out + u1;
-        it.x = load_unit<T, V>(it.a);
-        if (it.b != nullptr) it.y = load_unit<T, V>(it.b);
+        in = reinterpret_cast<const T*>(P.in[what]) + layer * P.in_layer[what] + (int64_t)head * P.d;
+        out = reinterpret_cast<T*>(P.out[what]) + layer * P.out_layer[what] + (int64_t)head * P.d;
+        in_row = P.in_row[what];
+        out_row = P.out_row[what];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (here(r)) {
+                x[r] = load_unit<T, V>(in + from[r] * in_row + u0);
+                if (u1 >= 0) y[r] = load_unit<T, V>(in + from[r] * in_row + u1);
+            }
     };
-    auto finish = [&](Item& it) {
-        if (it.a == nullptr) return;
-        if (it.pair >= 0) {
-            const float *co = s_cos + it.row * pairs, *si = s_sin + it.row * pairs;
-            if (V > 1 && P.r.neighbours) {
+    auto finish = [&]() {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    Unit<T, V>& u = h ? it.y : it.x;
-                    const int p = (it.pair * V + (h ? pairs : 0)) / 2;
+        for (int r = 0; r < R; ++r) {
+            if (!here(r)) continue;
+            if (pair >= 0) {
+                const float *co = s_cos + r * pairs, *si = s_sin + r * pairs;
+                if (V > 1 && P.r.neighbours) {
 #pragma unroll
-                    for (int e = 0; e < V / 2; ++e) {
-                        const float c = co[p + e], s = si[p + e], x = to_float(u.x[2 * e]), y = to_float(u.x[2 * e + 1]);
-                        from_float(u.x[2 * e], fmaf(x, c, -(y * s)));
-                        from_float(u.x[2 * e + 1], fmaf(y, c, x * s));
+                    for (int h = 0; h < 2; ++h) {
+                        Unit<T, V>& u = h ? y[r] : x[r];
+                        const int p = (pair * V + (h ? pairs : 0)) / 2;
+#pragma unroll
+                        for (int e = 0; e < V / 2; ++e) {
+                            const float c = co[p + e], s = si[p + e], a = to_float(u.x[2 * e]), b = to_float(u.x[2 * e + 1]);
+                            from_float(u.x[2 * e], fmaf(a, c, -(b * s)));
+                            from_float(u.x[2 * e + 1], fmaf(b, c, a * s));
+                        }
+                    }
+                } else {
+                    const int p = pair * V;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float c = co[p + e], s = si[p + e], a = to_float(x[r].x[e]), b = to_float(y[r].x[e]);
+                        from_float(x[r].x[e], fmaf(a, c, -(b * s)));
+                        from_float(y[r].x[e], fmaf(b, c, a * s));
                     }
                 }
-            } else {
-                const int p = it.pair * V;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float c = co[p + e], s = si[p + e], x = to_float(it.x.x[e]), y = to_float(it.y.x[e]);
-                    from_float(it.x.x[e], fmaf(x, c, -(y * s)));
-                    from_float(it.y.x[e], fmaf(y, c, x * s));
-                }
             }
+            T* const at = out + (queries ? first + r : to[r]) * out_row;
+            store_unit<T, V>(at + u0, x[r]);
+            if (u1 >= 0) store_unit<T, V>(at + u1, y[r]);
         }
-        store_unit<T, V>(it.to_a, it.x);
-        if (it.b != nullptr) store_unit<T, V>(it.to_b, it.y);
     };
 
-    Item it;
-    int at = (int)blockIdx.z * kThreads + (int)threadIdx.x;
-    if (at < total) take(at, it);
+    int e = (int)(blockIdx.z * blockDim.x + threadIdx.x);
+    if (e < row_items) take(e);
     if (P.r.pos != nullptr) {
-        for (int i = threadIdx.x; i < n * pairs; i += kThreads) {
+        for (int i = threadIdx.x; i < n * pairs; i += blockDim.x) {
             const int r = i / pairs, p = i - r * pairs;
             int axis = P.r.pair_axis != nullptr ? P.r.pair_axis[p] : 0;
             if (axis >= P.r.n_axes) { set_status(P.status, RADAR_ERR_INVALID_ARG); axis = 0; }
@@ -169,9 +184,9 @@ __global__ void __launch_bounds__(kThreads, 6) paged_rows_kernel(const PagedPara
         }
         __syncthreads();
     }
-    for (; at < total; at += step) {
-        finish(it);
-        if (at + step < total) take(at + step, it);
+    for (; e < row_items; e += step) {
+        finish();
+        if (e + step < row_items) take(e + step);
     }
 }
 
@@ -195,23 +210,29 @@ int launch(radar_ctx* ctx, PagedParams& P, int dtype, int n_layers, int kernel_i
     P.copy_items = (P.copy_units + 1) / 2;
     P.status = ctx->d_status;
     const int64_t row_items = (int64_t)(P.heads[0] + P.heads[1]) * (P.turn_items + P.rest_items) + (int64_t)P.heads[2] * P.copy_items;
-    if (row_items * kMaxRows > INT_MAX) return RADAR_ERR_UNSUPPORTED;
-    // Rows of a block: as many as there are threads for angles, unless that leaves SMs without one.
+    if (row_items > INT_MAX / 2) return RADAR_ERR_UNSUPPORTED;
+    // few rows: one to a block, and a row's items over several blocks, which take the angles each for themselves
     const int64_t wave = 4ll * ctx->sm_count;
-    int rows = kMaxRows;
-    while (rows > 1 && (P.n_tokens + rows - 1) / rows * n_layers < wave) rows /= 2;
-    P.rows = rows;
-    const int64_t blocks = (P.n_tokens + rows - 1) / rows;
-    // few rows: a row's items over several blocks, which take the angles each for themselves
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>((rows * row_items + kThreads - 1) / kThreads, 64));
-    const int64_t split = std::max<int64_t>(1, std::min(most, wave / std::max<int64_t>(1, blocks * n_layers)));
+    const bool many = (P.n_tokens + kRows - 1) / kRows * n_layers >= wave;
+    const int64_t blocks = many ? (P.n_tokens + kRows - 1) / kRows : P.n_tokens;
+    const int64_t passes = (row_items + kThreads - 1) / kThreads;
+    const int64_t split = std::max<int64_t>(1, std::min(std::min<int64_t>(passes, 64), wave / std::max<int64_t>(1, blocks * n_layers)));
+    const int threads = (int)(((row_items + passes - 1) / passes + 31) / 32 * 32);      // the passes' items in equal parts
     if (blocks > INT_MAX) return RADAR_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)blocks, (unsigned)n_layers, (unsigned)split);
-    radar_launch_scope scope(ctx, kernel_id, stream);
-    cudaError_t e;
-    if (dtype == RADAR_F32) e = launch_chained(wide ? paged_rows_kernel<float, 4> : paged_rows_kernel<float, 1>, grid, dim3(kThreads), 0, stream, P);
-    else e = launch_chained(wide ? paged_rows_kernel<__nv_bfloat16, 8> : paged_rows_kernel<__nv_bfloat16, 1>, grid, dim3(kThreads), 0, stream, P);
-    RADAR_CUDA_CHECK(e);
+    const size_t smem = 2 * (size_t)(many ? kRows : 1) * P.r.n_pairs * sizeof(float);
+    auto go = [&](auto kernel) {
+        radar_launch_scope scope(ctx, kernel_id, stream);
+        return launch_chained(kernel, grid, dim3((unsigned)threads), smem, stream, P);
+    };
+    auto by_rows = [&](auto t, auto v_) {
+        using T = decltype(t);
+        constexpr int V = decltype(v_)::value;
+        return many ? go(paged_rows_kernel<T, V, kRows>) : go(paged_rows_kernel<T, V, 1>);
+    };
+    using one = std::integral_constant<int, 1>;
+    if (dtype == RADAR_F32) RADAR_CUDA_CHECK(wide ? by_rows(0.f, std::integral_constant<int, 4>{}) : by_rows(0.f, one{}));
+    else RADAR_CUDA_CHECK(wide ? by_rows(__nv_bfloat16{}, std::integral_constant<int, 8>{}) : by_rows(__nv_bfloat16{}, one{}));
     return RADAR_OK;
 }
 
@@ -225,8 +246,8 @@ using namespace radar;
 extern "C" int radar_rotate(radar_ctx* ctx, const radar_rotate_args* a, void* stream_) {
     if (!ctx || !a || a->Hq < 0 || a->Hkv < 0 || a->Hq + (int64_t)a->Hkv == 0 || a->n_rows < 0 || a->d <= 0) return RADAR_ERR_INVALID_ARG;
     if ((a->dtype != RADAR_F32 && a->dtype != RADAR_BF16) || a->d > 2 * kMaxPairs || a->n_rows > INT_MAX) return RADAR_ERR_UNSUPPORTED;
-    if (!a->rotation.pos || !rotation_ok(a->rotation, a->d, a->n_rows)) return RADAR_ERR_INVALID_ARG;
     if (a->n_rows == 0) return RADAR_OK;
+    if (!a->rotation.pos || !rotation_ok(a->rotation, a->d, a->n_rows)) return RADAR_ERR_INVALID_ARG;
     const size_t es = a->dtype == RADAR_F32 ? 4 : 2;
     PagedParams P = {};
     P.in[0] = a->Q; P.in[1] = a->K;
@@ -249,9 +270,9 @@ extern "C" int radar_rotate(radar_ctx* ctx, const radar_rotate_args* a, void* st
 extern "C" int radar_paged_store(radar_ctx* ctx, const radar_paged_store_args* a, void* stream_) {
     if (!ctx || !a || a->n_layers <= 0 || a->Hq < 0 || a->Hkv <= 0 || a->d <= 0 || a->n_tokens < 0 || a->n_rows < 0 || a->cache_rows < 0) return RADAR_ERR_INVALID_ARG;
     if ((a->dtype != RADAR_F32 && a->dtype != RADAR_BF16) || a->d > 2 * kMaxPairs || a->n_layers > 65535 || a->n_tokens > INT_MAX || a->n_rows > INT_MAX) return RADAR_ERR_UNSUPPORTED;
+    if (a->n_tokens == 0) return RADAR_OK;
     if (a->rotation.pos && !rotation_ok(a->rotation, a->d, a->n_tokens)) return RADAR_ERR_INVALID_ARG;
     if (!a->src_row && a->n_rows < a->n_tokens) return RADAR_ERR_INVALID_ARG;
-    if (a->n_tokens == 0) return RADAR_OK;
     const int64_t kv = (int64_t)a->Hkv * a->d, q = (int64_t)a->Hq * a->d;
     const bool layers = a->n_layers > 1, rows = a->n_rows > 1;
     if (!a->K || !a->V || !a->Kc || !a->Vc || !a->slots || (rows && a->kv_row_stride < kv) || (layers && (a->kv_layer_stride <= 0 || a->cache_layer_stride < a->cache_rows * kv)))
