@@ -4,6 +4,7 @@
 // by all heads.  Every row is read and written once, so memory bounds it (and a launch behind a lookup where there is little).
 #include <algorithm>
 #include <climits>
+#include <cstring>
 #include <type_traits>
 
 #include "common.cuh"
@@ -12,7 +13,7 @@ namespace radar {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 4;                 // rows of a block, where there are many
+constexpr int kRows = 2;                 // rows of a block, where there are many
 constexpr int kMaxPairs = 512;
 
 struct PagedParams {
@@ -32,7 +33,9 @@ struct PagedParams {
     int* status;
 };
 
-// A unit is V elements, 16 bytes of them (or one element, for rows of any alignment).
+// A unit is V elements that a thread moves in one access: 32, 16 or 8 bytes of them, or one element, by what the sizes and
+// addresses are multiples of (us with the four: 8192 bf16 rows of 28 / 4 heads of 128 turned 25.1 / 27.3 / 35.1 / 89.3; 8192 tokens of 32 / 8
+// heads stored 34.2 / 38.3 / 49.7 / 130; 5329 rows of 16 / 16 heads of 72, which 8 bytes divide, 15.3 and with elements 37.6).
 template <typename T, int V>
 struct Unit {
     T x[V];
@@ -40,9 +43,15 @@ struct Unit {
 template <typename T, int V>
 __device__ __forceinline__ Unit<T, V> load_unit(const T* p) {
     Unit<T, V> u;
-    if (V > 1) {
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-        *reinterpret_cast<uint4*>(&u) = w;
+    if constexpr (sizeof(u) == 32) {
+        uint32_t w[8];
+        asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+        memcpy(&u, w, sizeof(u));
+    } else if constexpr (V > 1) {
+        using W = std::conditional_t<sizeof(u) == 16, uint4, uint2>;
+        const W w = __ldcs(reinterpret_cast<const W*>(p));
+        memcpy(&u, &w, sizeof(u));
     } else {
         u.x[0] = *p;
     }
@@ -50,8 +59,19 @@ __device__ __forceinline__ Unit<T, V> load_unit(const T* p) {
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_unit(T* p, const Unit<T, V>& u) {
-    if (V > 1) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&u);
-    else *p = u.x[0];
+    if constexpr (sizeof(u) == 32) {
+        uint32_t w[8];
+        memcpy(w, &u, sizeof(u));
+        asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                     :: "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
+    } else if constexpr (V > 1) {
+        using W = std::conditional_t<sizeof(u) == 16, uint4, uint2>;
+        W w;
+        memcpy(&w, &u, sizeof(u));
+        *reinterpret_cast<W*>(p) = w;
+    } else {
+        *p = u.x[0];
+    }
 }
 __device__ __forceinline__ void from_float(float& y, float x) { y = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
@@ -70,7 +90,9 @@ __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
 
 // A block takes up to R rows of one layer: its threads first load their items of all of these rows (two units of a head that are turned together, or
 // copied), then take the rows' angles, one each, into shared memory, then turn and store.  A thread's items stand at the same place in every row,
-// so where they lie is worked out once.
+// so where they lie is worked out once.  Two rows and 4 blocks of 256 threads an SM: 128 bytes a thread in flight (one row and 6 blocks 24.7 /
+// 34.3 us for the first two above, but small calls 2.6 instead of 2.3; four rows of 16 bytes 26.1 / 37.4).
+// What bounds it: memory.  The two above 5.3 and 5.9 TB/s, 157 accepted tokens in 40 layers of 40 heads 41.7 us, 6.2 TB/s.
 template <typename T, int V, int R>
 __global__ void __launch_bounds__(kThreads, 4) paged_rows_kernel(const PagedParams P) {
     extern __shared__ __align__(16) float s_angles[];
@@ -195,14 +217,15 @@ bool rotation_ok(const radar_rotation& r, int d, int64_t n) {
 }
 
 int launch(radar_ctx* ctx, PagedParams& P, int dtype, int n_layers, int kernel_id, cudaStream_t stream) {
-    const int es = dtype == RADAR_F32 ? 4 : 2, v = 16 / es;
+    const int es = dtype == RADAR_F32 ? 4 : 2;
     if (P.r.pos == nullptr) P.r.n_pairs = 0;
-    bool wide = P.d % v == 0 && P.r.n_pairs % v == 0;
+    uint64_t all = (uint64_t)P.d * es | (uint64_t)P.r.n_pairs * es;          // sizes, addresses and strides: the powers of two that divide all of them
     for (int i = 0; i < 3; ++i)
-        if (P.heads[i] > 0)
-            wide = wide && ((reinterpret_cast<uintptr_t>(P.in[i]) | reinterpret_cast<uintptr_t>(P.out[i])) & 15) == 0 &&
-                   ((P.in_row[i] | P.out_row[i] | (n_layers > 1 ? P.in_layer[i] | P.out_layer[i] : 0)) & (v - 1)) == 0;
-    const int unit = wide ? v : 1;
+        if (P.heads[i] > 0) {
+            all |= reinterpret_cast<uintptr_t>(P.in[i]) | reinterpret_cast<uintptr_t>(P.out[i]) | (uint64_t)(P.in_row[i] | P.out_row[i]) * es;
+            if (n_layers > 1) all |= (uint64_t)(P.in_layer[i] | P.out_layer[i]) * es;
+        }
+    const int bytes = all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : es, unit = bytes / es;
     P.turn_items = P.r.n_pairs / unit;
     P.rest_units = (P.d - 2 * P.r.n_pairs) / unit;
     P.copy_units = P.d / unit;
@@ -225,14 +248,17 @@ int launch(radar_ctx* ctx, PagedParams& P, int dtype, int n_layers, int kernel_i
         radar_launch_scope scope(ctx, kernel_id, stream);
         return launch_chained(kernel, grid, dim3((unsigned)threads), smem, stream, P);
     };
-    auto by_rows = [&](auto t, auto v_) {
+    auto by_rows = [&](auto t, auto v) {
         using T = decltype(t);
-        constexpr int V = decltype(v_)::value;
+        constexpr int V = decltype(v)::value;
         return many ? go(paged_rows_kernel<T, V, kRows>) : go(paged_rows_kernel<T, V, 1>);
     };
-    using one = std::integral_constant<int, 1>;
-    if (dtype == RADAR_F32) RADAR_CUDA_CHECK(wide ? by_rows(0.f, std::integral_constant<int, 4>{}) : by_rows(0.f, one{}));
-    else RADAR_CUDA_CHECK(wide ? by_rows(__nv_bfloat16{}, std::integral_constant<int, 8>{}) : by_rows(__nv_bfloat16{}, one{}));
+    auto by_unit = [&](auto t) {
+        constexpr int E = sizeof(t);
+        return unit == 1 ? by_rows(t, std::integral_constant<int, 1>{}) : bytes == 8 ? by_rows(t, std::integral_constant<int, 8 / E>{}) :
+               bytes == 16 ? by_rows(t, std::integral_constant<int, 16 / E>{}) : by_rows(t, std::integral_constant<int, 32 / E>{});
+    };
+    RADAR_CUDA_CHECK(dtype == RADAR_F32 ? by_unit(0.f) : by_unit(__nv_bfloat16{}));
     return RADAR_OK;
 }
 
