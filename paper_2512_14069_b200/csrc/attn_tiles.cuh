@@ -12,7 +12,6 @@ namespace {
 using namespace tc05;
 
 constexpr int kTileKeys = 128;       // keys per prefix tile
-constexpr int kFirstKeys = 64;       // keys of a tile whose products start before the rest of its probabilities is there
 constexpr int kPairRows = 256;       // query rows of a row-block pair (and the stride of partial records)
 constexpr float kRescaleThreshold = 8.f;   // in log2 units: P stays below 2^8
 constexpr int kSegRing = 4;          // segments on their way from the producer to the other warps
@@ -46,6 +45,27 @@ __device__ __forceinline__ float2 add2_in_order(float2 a, float2 b) {
     float2 d;
     asm volatile("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
                  : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float add_in_order(float a, float b) {
+    float d;
+    asm volatile("add.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float sub_in_order(float a, float b) {
+    float d;
+    asm volatile("sub.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float fma_in_order(float a, float b, float c) {
+    float d;
+    asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// the larger one, or NaN if one is
+__device__ __forceinline__ float max_nan_in_order(float a, float b) {
+    float d;
+    asm volatile("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
 __device__ __forceinline__ uint32_t bf16x2_in_order(float lo, float hi) {

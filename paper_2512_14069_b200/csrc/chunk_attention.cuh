@@ -141,19 +141,21 @@ struct Walk {
 template <class C>
 __device__ __forceinline__ Walk<C> first_segment(const ChunkParams& P, int ci, long long& tot) {
     const int lane = threadIdx.x & 31, B = P.a.B;
-    tot = 0;
+    bool ok = true;
+    ChunkSeq mine;                       // of request lane: with up to 32 of them every size is read once
+    mine.n = 0;
+    if (lane < B) mine = chunk_seq(P.a, lane, ok);
+    const long long my_size = lane < B ? seq_size<C>(P, mine) : 0;
+    tot = warp_sum(my_size);
 #pragma unroll 1
-    for (int b0 = 0; b0 < B; b0 += 32) {
+    for (int b0 = 32; b0 < B; b0 += 32) {
         const int b = b0 + lane;
-        long long size = 0;
-        if (b < B) {
-            bool ok;
-            const ChunkSeq s = chunk_seq(P.a, b, ok);
-            if (!ok && ci == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
-            size = seq_size<C>(P, s);
-        }
+        bool ok_b = true;
+        const long long size = b < B ? seq_size<C>(P, chunk_seq(P.a, b, ok_b)) : 0;
+        ok = ok && ok_b;
         tot += warp_sum(size);
     }
+    if (!ok && ci == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
     Walk<C> cur;
     const long long lo = tot * ci / P.n_cta;
     cur.hi = tot * (ci + 1) / P.n_cta;
@@ -167,8 +169,8 @@ __device__ __forceinline__ Walk<C> first_segment(const ChunkParams& P, int ci, l
 #pragma unroll 1
     for (int b0 = 0; b0 < B && cur.b < 0; b0 += 32) {
         const int b = b0 + lane;
-        bool ok;
-        const long long size = b < B ? seq_size<C>(P, chunk_seq(P.a, b, ok)) : 0;
+        bool ok_b;
+        const long long size = b0 == 0 ? my_size : b < B ? seq_size<C>(P, chunk_seq(P.a, b, ok_b)) : 0;
         long long incl = size;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -180,7 +182,7 @@ __device__ __forceinline__ Walk<C> first_segment(const ChunkParams& P, int ci, l
             const int src = __ffs(hit) - 1;
             const long long before = cum + __shfl_sync(kFull, incl - size, src), head = __shfl_sync(kFull, size, src) / P.groups;
             cur.b = b0 + src;
-            cur.s = chunk_seq(P.a, cur.b, ok);
+            cur.s = chunk_seq(P.a, cur.b, ok_b);
             cur.nq = units_of(P, cur.s);
             cur.g = (int)((lo - before) / head);
             const long long at = lo - before - cur.g * head;

@@ -5,14 +5,15 @@
 //
 // Inside the CTA (16 warps; the registers are shared out by warpgroup):
 //   warp 12    TMA producer: works out the CTA's segments (unit, tile range) for itself and, through a ring in shared memory, for the others;
-//              per segment the Q rows, then K and V tiles into two rings (128-byte swizzle), page by page.
+//              per segment the Q rows, and K tiles into a ring (128-byte swizzle), page by page.
+//   warp 14    V tiles into theirs.  (With pages of 16 tokens a tile is 16 copies, and one warp issues them one behind the other.)
 //   warp 13    MMA issuer: S = Q K^T into one of two tensor-memory score buffers, and O (+)= P V with P read back from
 //              tensor memory (bf16, overlaying S) and V consumed N-major straight from the row-major tile.
 //   warps 0-3 / 4-7  softmax groups 0 / 1, one thread per query row.  Unit with two live row blocks: group s owns row block s and sees
 //              every tile, so each K/V tile is loaded once for 256 query rows.  Unit with one: the groups take alternate
 //              tiles with separate (m, l, O) and are merged at the end.  Either way one group's softmax overlaps the other's MMAs.
 //   warps 8-11 epilogue: a finished accumulator to O or to the partials, while the others are in the next segment.
-//   warps 14, 15 only fill up the producer's warpgroup.
+//   warp 15 only fills up the producer's warpgroup.
 // Every mbarrier wait is bounded; a wait that runs out sets RADAR_ERR_TIMEOUT on the device status word, the CTA drains, frees its
 // tensor memory and returns.
 #include <algorithm>
@@ -25,7 +26,7 @@ namespace radar {
 namespace {
 
 constexpr int kChunkThreads = 512;
-constexpr int kEpilogueWarp = 8, kProducerWarp = 12, kMmaWarp = 13;
+constexpr int kEpilogueWarp = 8, kProducerWarp = 12, kMmaWarp = 13, kValueWarp = 14;
 // Registers a thread: 128 at launch, then shared out by warpgroup (two of softmax; what they take the other two give).
 constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
 static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
@@ -44,6 +45,8 @@ struct Smem {
     static constexpr int kDynamic = kQBytes + (kRingK + kRingV) * kTileBytes;     // starts on a 1024-byte boundary behind the static block
 };
 
+constexpr int kFirstKeys = 64, kFirstSteps = kFirstKeys / 16;   // keys of a tile whose products start before the rest of its probabilities is there
+
 struct Costs {
     static constexpr int kTile = kTileKeys, kOne = 3, kTwo = 5, kUnit = 15 * kTileKeys;
 };
@@ -52,7 +55,34 @@ struct Costs {
 struct __align__(16) Segment {
     int n;                               // tiles; 0: there is no further segment
     int t0, nt;                          // first tile, tiles of the unit
-    int seen, keys, rows, row0, g;       // of the unit (keys: 0 where its last token sees none)
+    int seen, keys, rows, row0, b, g;    // of the unit (keys: 0 where its last token sees none)
+};
+
+// The pages of a tile: lane p of a warp looks up and fetches page p, up to eight boxes of a tile (one where a page holds whole tiles).  Only
+// pages that hold keys which the unit sees are fetched; what stays stale in the slot is masked or never read.
+struct Pages {
+    int n_cache_pages, per, box_shift, tiles_per_page;
+    __device__ __forceinline__ explicit Pages(const radar_chunk_attn_args& a)
+        : n_cache_pages((int)(a.cache_rows / a.page_size)), per(min(a.page_size, kTileKeys)), box_shift(a.page_size == 16 ? 4 : a.page_size == 32 ? 5 : a.page_size == 64 ? 6 : 7),
+          tiles_per_page(max(a.page_size / kTileKeys, 1)) {}       // (cache_rows: below 2^31)
+    __device__ __forceinline__ int boxes(const Segment& s, int t) const { return (min(kTileKeys, s.keys - t * kTileKeys) + per - 1) >> box_shift; }
+    // cache row of the lane's page
+    __device__ __forceinline__ int row_of(const ChunkParams& P, const Segment& s, int t, int lane) const {
+        if (lane >= boxes(s, t)) return 0;
+        const int index = (tiles_per_page > 1 ? t / tiles_per_page : t << (7 - box_shift)) + lane;
+        int page = P.a.block_table[(long long)s.b * P.a.max_pages + index];
+        if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
+        return page * P.a.page_size + (tiles_per_page > 1 ? (t - index * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
+    }
+    template <int D>
+    __device__ __forceinline__ void fetch(const Segment& s, int t, int row, unsigned char* dst, const CUtensorMap* tm, uint64_t* full, int lane) const {
+        const int n = boxes(s, t);
+        if (lane == 0) mbar_arrive_expect_tx(full, n * per * D * 2);
+        __syncwarp();
+        if (lane < n)
+            for (int h = 0; h < D / 64; ++h) tma_load_3d(dst + h * (kTileKeys * 128) + lane * per * 128, tm, full, h * 64, s.g, row);
+        __syncwarp();
+    }
 };
 
 template <int D>
@@ -107,7 +137,7 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
                 mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
             }
-            for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 1); }
+            for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 2); }
             mbar_init(&st.bar_idle, 1);
             st.q_last = 1;
             mbar_init(&st.bar_mlfull, 8);
@@ -188,19 +218,25 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                         tmem_wait_st();
                     }
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sv[c]);
+                    tmem_ld32(tS, sv[0]);
+                    tmem_ld32(tS + 32, sv[1]);
                     tmem_wait_ld();
-                    float mxa[4];
+                    tmem_ld32(tS + 64, sv[2]);
+                    tmem_ld32(tS + 96, sv[3]);
+                    float mxa[8];
+                    auto half_max = [&](const uint32_t (&u)[32], const uint32_t (&v)[32], const bool first) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        mxa[c] = __uint_as_float(sv[c][0]);
+                        for (int e = 0; e < 32; e += 8)                      // eight chains, three inputs an instruction
 #pragma unroll
-                        for (int e = 1; e < 31; e += 2)                     // three-input maxima: half the instructions
-                            mxa[c] = max3(mxa[c], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
-                        mxa[c] = fmaxf(mxa[c], __uint_as_float(sv[c][31]));
-                    }
-                    const float mx = fmaxf(max3(mxa[0], mxa[1], mxa[2]), mxa[3]);
+                            for (int c = 0; c < 8; ++c) {
+                                const float x = __uint_as_float(u[e + c]), y = __uint_as_float(v[e + c]);
+                                mxa[c] = first && e == 0 ? fmaxf(x, y) : max3(mxa[c], x, y);
+                            }
+                    };
+                    half_max(sv[0], sv[1], true);
+                    tmem_wait_ld();
+                    half_max(sv[2], sv[3], false);
+                    const float mx = max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7]));
                     // ---- running max (log2 units), lazy rescale of the accumulator when some row of the warp moved its max ----
                     const float m_tile = mx * P.scale_log2;
                     float factor = 1.f;
@@ -384,8 +420,6 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         chain_sync();                            // every global access of the CTA comes behind one
         if (warp == kProducerWarp) {
             // =================================== TMA producer ===================================
-            // The whole warp walks the loop; lane p looks up and fetches page p of a tile (up to eight boxes per tile), the
-            // leading lane does the waits, the byte counts and Q.
             const bool lead = lane == 0;
             const bool usable = (smem_u32(smem_raw) & 1023u) == 0 && st.tmem_base == 0;     // (else the tiles would not sit on their swizzle boundary)
             if (!usable && lead) set_status(P.status, RADAR_ERR_CUDA);
@@ -395,127 +429,129 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if (!usable) cur.t0 = cur.t1 = 0;
             __syncwarp();
             if (lead) { cut.unit.valid = 0; cut.tot = tot; }
-            uint32_t k_slot = 0, k_par = 1, v_slot = 0, v_par = 1;   // ring slot to fill next and the phase that frees it
-            const int n_cache_pages = (int)(a.cache_rows / a.page_size);                       // (cache_rows: below 2^31)
-            const int box_shift = __ffs(min(a.page_size, kTileKeys)) - 1, tiles_per_page = max(a.page_size / kTileKeys, 1);
-            auto first_page = [&](int t) { return tiles_per_page > 1 ? t / tiles_per_page : t << (7 - box_shift); };     // of tile t
-            // asks for the lines of the block table that tiles [t0, t1) of a request are looked up in
-            auto fetch_pages = [&](int b, int t0, int t1) {
-                const int last = min(first_page(t1), a.max_pages - 1);
-                for (int i = first_page(t0) + lane * 32; i <= last; i += 32 * 32)
-                    asm volatile("prefetch.global.L1 [%0];" ::"l"(a.block_table + (long long)b * a.max_pages + i));
-            };
+            Pages pages(a);
+            uint32_t slot = 0, par = 1;                              // ring slot to fill next and the phase that frees it
             for (uint32_t seg = 0;; ++seg) {
                 const bool on = cur.valid();
-                const int b = cur.b, g = cur.g, n = cur.t1 - cur.t0, t0 = cur.t0, row0 = cur.u.row0;
-                const int keys = min(cur.u.keys, max(cur.u.seen + cur.u.tokens - 1, 0));
-                const bool two = cur.u.rows > P.rb_rows;
+                Segment s;                           // (behind a wait that ran out the others are sent home)
+                s.n = cur.t1 - cur.t0; s.t0 = cur.t0; s.nt = cur.u.nt; s.seen = cur.u.seen; s.rows = cur.u.rows; s.row0 = cur.u.row0; s.b = cur.b; s.g = cur.g;
+                s.keys = min(cur.u.keys, max(cur.u.seen + cur.u.tokens - 1, 0));
                 if (lead) {
                     ok = mbar_wait_while(ok, &st.bar_segempty[seg % kSegRing], ((seg / kSegRing) & 1) ^ 1);
-                    Segment s;                       // (behind a wait that ran out the others are sent home)
-                    s.n = on && ok ? n : 0; s.t0 = t0; s.nt = cur.u.nt; s.seen = cur.u.seen; s.keys = keys; s.rows = cur.u.rows; s.row0 = row0; s.g = g;
                     st.seg[seg % kSegRing] = s;
+                    if (!(on && ok)) st.seg[seg % kSegRing].n = 0;
                     mbar_arrive(&st.bar_segfull[seg % kSegRing]);
                 }
                 if (!on) break;
-                if (lead && t0 == 0 && n < cur.u.nt) {               // necessarily the last segment of this CTA
-                    cut.unit.valid = 1; cut.unit.row0 = row0; cut.unit.g = g; cut.unit.slot = seg == 0 ? 0 : 1; cut.unit.rows = cur.u.rows;
-                    cut.nt = cur.u.nt; cut.w = cur.u.w; cut.size_keys = cur.u.keys; cut.u0 = cur.U;
+                if (lead && s.t0 == 0 && s.n < s.nt) {               // necessarily the last segment of this CTA
+                    cut.unit.valid = 1; cut.unit.row0 = s.row0; cut.unit.g = s.g; cut.unit.slot = seg == 0 ? 0 : 1; cut.unit.rows = s.rows;
+                    cut.nt = s.nt; cut.w = cur.u.w; cut.size_keys = cur.u.keys; cut.u0 = cur.U;
                 }
-                cur.next(P);
-                // Order: the first K tile(s), Q (behind them, for its slot is free only after the last S of the segment before; the
-                // CTA's first segment finds it free), then V(i), K(i + la), the order in which the MMA warp consumes them.
-                const int la = two ? 1 : 2;
-#pragma unroll 1
-                for (int j = -2 * la; j < 2 * n; ++j) {              // even: V(j / 2), odd: K(j / 2 + la)
-                    const bool is_k = (j & 1) != 0;
-                    const int i = (j >> 1) + (is_k ? la : 0);
-                    if (i >= 0 && i < n) {
-                        const int t = t0 + i;
-                        // one box per page (or per tile when a page holds whole tiles); only pages that hold keys which the unit sees are
-                        // fetched, what stays stale in the slot is masked / never read.  The pages are looked up while the
-                        // slot is not free yet.
-                        const int per = min(a.page_size, kTileKeys);
-                        const int n_ld = (min(kTileKeys, keys - t * kTileKeys) + per - 1) >> box_shift;
-                        int page_row = 0;
-                        if (lane < n_ld) {
-                            const int index = first_page(t) + lane;
-                            int page = a.block_table[(long long)b * a.max_pages + index];
-                            if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
-                            page_row = page * a.page_size + (tiles_per_page > 1 ? (t - index * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
-                        }
-                        const uint32_t slot = is_k ? k_slot : v_slot;
-                        uint64_t* full = is_k ? &st.bar_kfull[slot] : &st.bar_vfull[slot];
-                        unsigned char* dst = (is_k ? sK : sV) + slot * SM::kTileBytes;
-                        if (lead) ok = mbar_wait_while(ok, is_k ? &st.bar_kempty[slot] : &st.bar_vempty[slot], is_k ? k_par : v_par);
-                        ok = __shfl_sync(kFull, ok, 0);
-                        if (!ok) break;                              // (the ring's position stays that of the last load)
-                        if (is_k) { if (++k_slot == RK) { k_slot = 0; k_par ^= 1; } }
-                        else if (++v_slot == RV) { v_slot = 0; v_par ^= 1; }
-                        if (lead) mbar_arrive_expect_tx(full, n_ld * per * D * 2);
-                        __syncwarp();
-                        if (lane < n_ld)
+                auto fetch_q = [&]() {
+                    ok = mbar_wait_while(ok, &st.bar_qempty, (seg & 1) ^ 1);
+                    const int blocks = s.rows > P.rb_rows ? 2 : 1;
+                    if (ok) {
+                        st.q_last = seg & 1;
+                        mbar_arrive_expect_tx(&st.bar_qfull, blocks * P.rb_rows * D * 2);   // rows past rb_rows stay stale: never read back
+                        for (int q = 0; q < blocks; ++q)
                             for (int h = 0; h < H; ++h)
-                                tma_load_3d(dst + h * (kTileKeys * 128) + lane * per * 128, is_k ? &tmK : &tmV, full, h * 64, g, page_row);
+                                tma_load_3d(sQ + q * SM::kQBlock + h * (128 * 128), &tmQ, &st.bar_qfull, h * 64, s.g * G, s.row0 + q * P.tokens_per_rb);
                     }
-                    if (j == (seg == 0 ? -2 * la : -1) && lead) {
-                        ok = mbar_wait_while(ok, &st.bar_qempty, (seg & 1) ^ 1);
-                        const int blocks = two ? 2 : 1;
-                        if (ok) {
-                            st.q_last = seg & 1;
-                            mbar_arrive_expect_tx(&st.bar_qfull, blocks * P.rb_rows * D * 2);   // rows past rb_rows stay stale: never read back
-                            for (int q = 0; q < blocks; ++q)
-                                for (int h = 0; h < H; ++h)
-                                    tma_load_3d(sQ + q * SM::kQBlock + h * (128 * 128), &tmQ, &st.bar_qfull, h * 64, g * G, row0 + q * P.tokens_per_rb);
-                        }
-                    }
-                    if (j == 0 && cur.valid()) fetch_pages(cur.b, cur.t0, cur.t1);
+                };
+                // Q's slot is free only after the last S of the segment before, so the first K tiles go ahead of it; the CTA's first segment finds
+                // it free, and its keys have to be looked up first.
+                if (seg == 0 && lead) fetch_q();
+                cur.next(P);
+                int row = pages.row_of(P, s, s.t0, lane);
+#pragma unroll 1
+                for (int i = 0; i < s.n; ++i) {
+                    const int here = row;
+                    if (i + 1 < s.n) row = pages.row_of(P, s, s.t0 + i + 1, lane);       // (its page is looked up while the slot is not free yet)
+                    if (lead) ok = mbar_wait_while(ok, &st.bar_kempty[slot], par);
+                    ok = __shfl_sync(kFull, ok, 0);
+                    if (!ok) break;                                  // (the ring's position stays that of the last load)
+                    pages.template fetch<D>(s, s.t0 + i, here, sK + slot * SM::kTileBytes, &tmK, &st.bar_kfull[slot], lane);
+                    if (++slot == RK) { slot = 0; par ^= 1; }
+                    if (i == min(s.n, 2) - 1 && seg > 0 && lead) fetch_q();
                 }
             }
             __syncwarp();
             write_cut<Costs>(P, blockIdx.x, cut);
-            if (lead) { st.k_next = k_slot | k_par << 8; st.v_next = v_slot | v_par << 8; }
+            if (lead) st.k_next = slot | par << 8;
+            __syncwarp();
+        } else if (warp == kValueWarp) {
+            // =================================== V tiles ===================================
+            Pages pages(a);
+            uint32_t slot = 0, par = 1;
+            Segment s;
+            for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
+                int row = pages.row_of(P, s, s.t0, lane);
+#pragma unroll 1
+                for (int i = 0; i < s.n; ++i) {
+                    const int here = row;
+                    if (i + 1 < s.n) row = pages.row_of(P, s, s.t0 + i + 1, lane);
+                    if (lane == 0) ok = mbar_wait_while(ok, &st.bar_vempty[slot], par);
+                    ok = __shfl_sync(kFull, ok, 0);
+                    if (!ok) break;
+                    pages.template fetch<D>(s, s.t0 + i, here, sV + slot * SM::kTileBytes, &tmV, &st.bar_vfull[slot], lane);
+                    if (++slot == RV) { slot = 0; par ^= 1; }
+                }
+            }
+            if (lane == 0) st.v_next = slot | par << 8;
             __syncwarp();
         } else if (warp == kMmaWarp) {
             // =================================== MMA issuer ===================================
-            // The warp runs converged: every lane waits on the barriers and executes the same straight-line issue
-            // sequences with warp-uniform descriptor words, and the elected lane issues the instructions and the
-            // commits (predicated, no branch around them).  No control flow depends on a wait's outcome: after a wait that ran out the
-            // predicate is off and the loops run dry.
+            // Every lane waits on the barriers (and helps to clear what lies behind the last key), one issues the products and the commits.  No
+            // control flow depends on a wait's outcome but that: after a wait that ran out nothing is issued and the loops run dry.
+            // Some eight products queue up in front of the tensor cores, so that they have work while this warp is in a wait.
             constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTileKeys, false, false);
             constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, false, true);
-            // high word of every shared-memory descriptor (stride between 8-row groups 1024 B, version, swizzle)
-            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            // descriptors: stride between 8-row groups 1024 B, version, swizzle; in units of 16 bytes
+            constexpr uint64_t kDesc = (uint64_t)((1024u >> 4) | (1u << 14) | (2u << 29)) << 32;
             constexpr uint32_t kHalfTile = kTileKeys * 128 >> 4;     // between the 64-column blocks of a tile
-            const uint32_t q_lo = ((smem_u32(sQ) & 0x3ffff) >> 4) | (1u << 16);
-            const uint32_t k_lo = ((smem_u32(sK) & 0x3ffff) >> 4) | (1u << 16);
-            const uint32_t v_lo = ((smem_u32(sV) & 0x3ffff) >> 4) | (kHalfTile << 16);     // N-major: 64-column blocks are a half tile apart
-            const uint32_t elected = elect_one();
+            auto place = [](const void* p) { return (uint64_t)((smem_u32(p) & 0x3ffff) >> 4); };
+            const uint64_t q_desc = kDesc | place(sQ) | (1u << 16), k_desc = kDesc | place(sK) | (1u << 16);
+            const uint64_t v_desc = kDesc | place(sV) | (kHalfTile << 16);                 // N-major: 64-column blocks are a half tile apart
+            const bool leader = elect_one() != 0;
             uint32_t k_next = 0, k_par = 0, v_next = 0, v_par = 0;   // ring slot to take next and its phase parity
             uint32_t p_par[2] = {0, 0};              // phase parity of the next P tile per group
-            // The segment's shape comes from memory; passing it through a broadcast from lane 0 tells the
-            // compiler that it is the same in every lane.
-            auto uni = [](int v) { return __shfl_sync(kFull, v, 0); };
             Segment s;
             for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
-                const int seg_t0 = uni(s.t0), n = uni(s.n), keys = uni(s.keys);
-                const bool two = uni(s.rows) > P.rb_rows;
+                const int seg_t0 = s.t0, n = s.n, keys = s.keys;
+                const bool two = s.rows > P.rb_rows;
                 ok = mbar_wait_while(ok, &st.bar_qfull, seg & 1);
                 uint32_t k_slot = 0, v_slot = 0;      // ring slots of the K and V tiles in use
+                uint32_t k_wait = 0, v_wait = 0;      // ... and the parities to wait for them with
                 bool acc[2] = {false, false};         // accumulator holds a product of this segment
                 auto take_v = [&]() {
                     v_slot = v_next;
-                    ok = mbar_wait_while(ok, &st.bar_vfull[v_slot], v_par);
+                    v_wait = v_par;
                     if (++v_next == RV) { v_next = 0; v_par ^= 1; }
                 };
                 auto take_k = [&]() {
                     k_slot = k_next;
-                    ok = mbar_wait_while(ok, &st.bar_kfull[k_slot], k_par);
+                    k_wait = k_par;
                     if (++k_next == RK) { k_next = 0; k_par ^= 1; }
                 };
                 // the accumulator's first product of the segment: the epilogue of the previous one has read it
                 auto take_o = [&](const int q) {
                     if (!acc[q]) ok = mbar_wait_while(ok, &st.bar_ofree[q], (seg & 1) ^ 1);
+                };
+                // products of 16 keys each: O[q] (+)= P[q] V, steps [from, to) of tile v_slot
+                auto issue_pv = [&](const int q, const int from, const int to, const bool first) {
+                    const uint64_t b = v_desc + v_slot * (SM::kTileBytes >> 4);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i >= from && i < to) mma_ts(tmem + 256 + q * 128, tmem + q * 128 + 8 * i, b + 128 * i, idesc_pv, !first || i > 0);
+                };
+                // S[q] = Q K^T.  Nothing in tensor memory changes hands here: K arrives through the async proxy, and the buffer was
+                // last read by this thread's own P V, which runs first.
+                auto issue_s = [&](const int q, const int block) {
+                    const uint64_t a0 = q_desc + block * (SM::kQBlock >> 4), b = k_desc + k_slot * (SM::kTileBytes >> 4);
+#pragma unroll
+                    for (int h = 0; h < H; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_ss(tmem + q * 128, a0 + h * kHalfTile + 2 * i, b + h * kHalfTile + 2 * i, idesc_s, h + i > 0);
                 };
 
                 // ---- O[q] (+)= P[q] V for tile i (q is a literal at every call site) ----
@@ -524,6 +560,7 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     const int ksteps = (valid + 15) >> 4;
                     if (fresh_v) {
                         take_v();
+                        ok = mbar_wait_while(ok, &st.bar_vfull[v_slot], v_wait);
                         if (valid < ksteps * 16) {
                             // rows past the last key meet P = 0; they must not hold NaN/Inf bit patterns
                             unsigned char* vtile = sV + v_slot * SM::kTileBytes;
@@ -542,65 +579,73 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
                     p_par[q] ^= 1;
                     tc_fence_after_sync();
-                    const uint32_t go = ok ? elected : 0u;
-                    const uint32_t b_lo = v_lo + v_slot * (SM::kTileBytes >> 4);
-                    mma_ts_x4(go, ksteps, tmem + 256 + q * 128, tmem + q * 128, b_lo, kDescHi, idesc_pv, acc[q]);
-                    mma_ts_x4(go, ksteps - 4, tmem + 256 + q * 128, tmem + q * 128 + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
+                    if (__all_sync(kFull, ok)) {
+                        if (leader) {
+                        issue_pv(q, 0, ksteps, !acc[q]);
+                        if (release_v) mma_commit(&st.bar_vempty[v_slot]);
+                        if (two ? i == n - 1 : i + 2 >= n) mma_commit(&st.bar_odone[q]);
+                    } }
+                    __syncwarp();
                     acc[q] = true;
-                    if (release_v) mma_commit_if(go, &st.bar_vempty[v_slot]);
-                    if (two ? i == n - 1 : i + 2 >= n) mma_commit_if(go, &st.bar_odone[q]);
                 };
-                // ---- S[q] = Q K^T for tile si.  Nothing in tensor memory changes hands here: K arrives through the
-                // async proxy, and the buffer was last read by this thread's own P V, which runs first. ----
+                // ---- S[q] = Q K^T for tile si ----
                 auto qk = [&](const int q, const int si, const bool fresh_k, const bool release_k) {
-                    if (fresh_k) take_k();
-                    const uint32_t go = ok ? elected : 0u;
-                    const uint32_t a0 = q_lo + (two ? q : 0) * (SM::kQBlock >> 4);
-                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
-                    mma_ss_x4(go, tmem + q * 128, a0, b0, kDescHi, idesc_s, false);
-                    if (D == 128) mma_ss_x4(go, tmem + q * 128, a0 + kHalfTile, b0 + kHalfTile, kDescHi, idesc_s, true);   // second 64-column block
-                    if (release_k) mma_commit_if(go, &st.bar_kempty[k_slot]);
-                    mma_commit_if(go, &st.bar_sfull[q]);
-                    // the last S of the segment: Q may be overwritten once it has run
-                    if (si == n - 1 && release_k) mma_commit_if(go, &st.bar_qempty);
+                    if (fresh_k) {
+                        take_k();
+                        ok = mbar_wait_while(ok, &st.bar_kfull[k_slot], k_wait);
+                    }
+                    if (__all_sync(kFull, ok)) {
+                        if (leader) {
+                        issue_s(q, two ? q : 0);
+                        if (release_k) mma_commit(&st.bar_kempty[k_slot]);
+                        mma_commit(&st.bar_sfull[q]);
+                        // the last S of the segment: Q may be overwritten once it has run
+                        if (si == n - 1 && release_k) mma_commit(&st.bar_qempty);
+                    } }
+                    __syncwarp();
                 };
                 // Schedule.  Two live row blocks: group s owns row block s; per tile PV0(i) S0(i+1) PV1(i) S1(i+1),
                 // both groups sharing K(i+1) and V(i).  One live row block: the groups take alternate tiles,
                 // PV(i) S(i+2) for group i & 1.  S of the first tile(s) comes from the iterations with i < 0.
-                // Steady state (all tiles involved are full): the same steps with nothing to decide,
-                // so that the issuing warp executes as few instructions per MMA as possible.  The waits for K and V, which are
-                // there most of the time, stand where the warp would wait for P.
-                auto full = [&](const int q, const uint32_t a0, const bool fresh, const bool release) {
-                    static_assert(kFirstKeys == 64 && kTileKeys == 128, "four steps before and behind the second wait");
-                    const uint32_t o_col = tmem + 256 + q * 128, p_col = tmem + q * 128;
-                    if (fresh) take_v();
+                // Steady state (all tiles involved are full): the same steps with nothing to decide and few waits.
+                auto full = [&](const int q, const int block, const bool fresh, const bool release, const bool last_s) {
                     take_o(q);
-                    const uint32_t b_lo = v_lo + v_slot * (SM::kTileBytes >> 4);
-                    ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
+                    if (fresh) {
+                        take_v();
+                        take_k();
+                        ok = mbar_wait_both(ok, &st.bar_vfull[v_slot], v_wait, &st.bar_pfirst[q], p_par[q]);
+                    } else {
+                        ok = mbar_wait_while(ok, &st.bar_pfirst[q], p_par[q]);
+                    }
                     tc_fence_after_sync();
-                    mma_ts_x4(ok ? elected : 0u, o_col, p_col, b_lo, kDescHi, idesc_pv, acc[q]);
-                    if (fresh) take_k();
-                    const uint32_t b0 = k_lo + k_slot * (SM::kTileBytes >> 4);
-                    ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
+                    if (__all_sync(kFull, ok)) {
+                        if (leader) issue_pv(q, 0, kFirstSteps, !acc[q]);
+                    }
+                    __syncwarp();
+                    if (fresh) ok = mbar_wait_both(ok, &st.bar_kfull[k_slot], k_wait, &st.bar_pready[q], p_par[q]);
+                    else ok = mbar_wait_while(ok, &st.bar_pready[q], p_par[q]);
                     p_par[q] ^= 1;
                     acc[q] = true;
                     tc_fence_after_sync();
-                    const uint32_t go = ok ? elected : 0u;
-                    mma_ts_x4(go, o_col, p_col + 32, b_lo + 4 * 128, kDescHi, idesc_pv, true);
-                    if (release) mma_commit_if(go, &st.bar_vempty[v_slot]);
-                    mma_ss_x4(go, p_col, a0, b0, kDescHi, idesc_s, false);
-                    if (D == 128) mma_ss_x4(go, p_col, a0 + kHalfTile, b0 + kHalfTile, kDescHi, idesc_s, true);
-                    mma_commit_if(go, &st.bar_sfull[q]);
-                    if (release) mma_commit_if(go, &st.bar_kempty[k_slot]);
+                    if (__all_sync(kFull, ok)) {
+                        if (leader) {
+                            issue_pv(q, kFirstSteps, 8, false);
+                            if (release) mma_commit(&st.bar_vempty[v_slot]);
+                            issue_s(q, block);
+                            mma_commit(&st.bar_sfull[q]);
+                            if (release) mma_commit(&st.bar_kempty[k_slot]);
+                            if (last_s) mma_commit(&st.bar_qempty);
+                        }
+                    }
+                    __syncwarp();
                 };
-                const uint32_t a_q0 = q_lo, a_q1 = q_lo + (SM::kQBlock >> 4);
                 const int n_full = min(n, keys / kTileKeys - seg_t0);   // tiles [0, n_full) of the segment are full
                 if (two) {
 #pragma unroll 1
                     for (int i = -1; i < n; ++i) {
-                        if (i >= 0 && i + 2 < n_full) {           // tiles i and i+1 full, and S(i+1) is not the segment's last
-                            full(0, a_q0, true, false);
-                            full(1, a_q1, false, true);
+                        if (i >= 0 && i < n_full && i + 1 < n) {
+                            full(0, 0, true, false, false);
+                            full(1, 1, false, true, i + 2 == n);
                         } else {
                             if (i >= 0) pv(0, i, true, false);
                             if (i + 1 < n) qk(0, i + 1, true, false);
@@ -611,9 +656,9 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 } else {
 #pragma unroll 1
                     for (int i = -2; i < n; i += 2) {
-                        if (i >= 0 && i + 4 < n_full) {           // tiles i to i+3 full, S(i+3) not the last
-                            full(0, a_q0, true, true);
-                            full(1, a_q0, true, true);
+                        if (i >= 0 && i + 1 < n_full && i + 3 < n) {
+                            full(0, 0, true, true, false);
+                            full(1, 0, true, true, i + 4 == n);
                         } else {
                             if (i >= 0) pv(0, i, true, true);
                             if (i + 2 < n) qk(0, i + 2, true, true);
@@ -624,7 +669,8 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 }
             }
             // no product may read shared memory or write tensor memory that the CTA has given back
-            mma_commit_if(elected, &st.bar_idle);
+            if (leader) mma_commit(&st.bar_idle);
+            __syncwarp();
             ok &= mbar_drain(&st.bar_idle, 0);
             __syncwarp();
         }

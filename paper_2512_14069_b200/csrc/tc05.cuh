@@ -57,6 +57,27 @@ __device__ __forceinline__ bool mbar_wait_while(bool ok, uint64_t* bar, uint32_t
         : "memory");
     return ok && r != 0;
 }
+// Two barriers in one wait: a poll that succeeds takes some 100 cycles, two behind one another 200.
+__device__ __forceinline__ bool mbar_wait_both(bool ok, uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1, uint32_t limit = 1u << 20) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q, s;\n\t.reg .u32 n;\n\t"
+        "mov.u32 n, %5;\n\t"
+        "WAIT:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4, 1000000;\n\t"
+        "and.pred p, p, q;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 s, n, 0;\n\t"
+        "@s bra WAIT;\n\t"
+        "DONE:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(smem_u32(bar0)), "r"(parity0), "r"(smem_u32(bar1)), "r"(parity1), "r"(ok ? limit : 1u)
+        : "memory");
+    return ok && r != 0;
+}
 // For a wait that is long and whose end nothing hurries after: naps between the polls (limit: about 4.5 s).
 __device__ __forceinline__ bool mbar_wait_lazy(bool ok, uint64_t* bar, uint32_t parity, uint32_t limit = 1u << 20) {
 #pragma unroll 1
@@ -268,6 +289,19 @@ __device__ __forceinline__ void mma_ts_two_x2x2_full(uint32_t pred, uint32_t d_t
         ::"r"(pred), "r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)acc_first)
         : "memory");
 #undef RADAR_TS_STEP
+}
+// One MMA, for one thread in a branch of its own: 15 to 25 cycles an instruction, where the predicated sequences above, with a predicate that
+// depends on a wait, take 60 (128 x 128 x 16: the tensor cores take 64).
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // ---- tensor-memory loads / stores (warp-collective; lane l of warp w touches TMEM lane 32 (w % 4) + l) ----
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {

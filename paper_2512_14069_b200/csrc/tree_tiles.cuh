@@ -12,6 +12,7 @@ namespace {
 // how the prefix is held: what the tile space has to look up
 enum CacheKind { kContiguous = 0, kPaged = 1, kFourBit = 2 };
 
+constexpr int kFirstKeys = 64;       // keys of a tile whose products start before the rest of its probabilities is there
 constexpr int kTreeKeys = 64;        // keys of the tree tile (RADAR_MAX_NODES)
 
 // Written by every CTA of the attention kernel, read by the combine kernel: the pieces are worked out by the producer warp
