@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libradar_b200.so")
 SOURCES = ["api.cu", "vocab_pass.cu", "row_topk.cu", "expand.cu", "expand_calls.cu", "tree_build.cu", "tree_attention.cu", "tree_attention_tc.cu", "verify_accept.cu", "train.cu",
-           "cache.cu", "cache_attention.cu", "cache_attention_tc.cu", "paged.cu", "chunk_attention.cu", "chunk_attention_tc.cu"]
+           "cache.cu", "cache_attention.cu", "cache_attention_tc.cu", "paged.cu", "chunk_attention.cu", "chunk_attention_tc.cu", "chunk_attention_rows.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
          "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

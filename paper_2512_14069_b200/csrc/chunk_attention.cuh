@@ -391,5 +391,8 @@ int chunk_combine(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream) {
 bool chunk_tc_supported(const radar_chunk_attn_args* a);
 size_t chunk_tc_workspace_bytes(const radar_ctx* ctx, int d);
 int chunk_tc_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream_t stream);
+// --- few rows (chunk_attention_rows.cu) ---
+// taken: it was launched (or the launch failed); false: the call is the tensor cores'
+int chunk_rows_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream_t stream, bool& taken);
 
 }  // namespace radar

@@ -99,3 +99,86 @@ def test_repeats_are_bit_equal(ctx, dtype):
         rb.radar_chunk_attention(ctx, **kw)
         torch.cuda.synchronize()
         assert torch.equal(kw["O"], first[0]) and torch.equal(kw["lse"], first[1])
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 1), (4, 2), (9, 1), (16, 1), (32, 2), (17, 1), (6, 6)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_rows(ctx, Hq, Hkv, d):
+    """Single tokens and two of them, at lengths around a chunk, a block's keys, a cluster's, and behind the bound of the form."""
+    import paged_harness as T
+    lens = [1, 15, 16, 17, 127, 128, 129, 250]
+    T.check_chunk(ctx, _rng(Hq, d), [1] * 8, lens, Hq, Hkv, d, 16)
+    T.check_chunk(ctx, _rng(Hq, d, 1), [2, 1, 0, 2], [2, 1, 5, 640], Hq, Hkv, d, 32)
+    for n in (300, 2047, 2048, 2049, 5000, 17000):
+        T.check_chunk(ctx, _rng(Hq, n), [1], [n], Hq, Hkv, d, 64)
+    T.check_chunk(ctx, _rng(Hq, d, 2), [2, 1], [0, 0], Hq, Hkv, d, 16, max_len=400)
+
+
+def test_few_rows_of_many_requests(ctx):
+    import paged_harness as T
+    T.check_chunk(ctx, _rng(1), [1] * 150, [3 * i % 700 for i in range(150)], 4, 2, 128, 16)
+    T.check_chunk(ctx, _rng(2), [2] * 40, [11 * i % 500 + 2 for i in range(40)], 8, 1, 64, 128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news,lens,d", [([1, 1], [40, 300], 128), ([30, 1, 200], [200, 900, 200], 64), ([300], [3000], 128)])
+def test_keys_and_values_that_are_no_numbers(ctx, news, lens, d, dtype):
+    """A NaN key makes exactly the rows that see it NaN; keys behind a row's last, and infinite ones there, reach nothing."""
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    rng = _rng(len(news), d)
+    Hq, Hkv, page = 4, 2, 16
+    kw = T.check_chunk(ctx, rng, news, lens, Hq, Hkv, d, page, dtype)
+    want = kw["O"].clone()
+    for value in (float("nan"), float("inf")):
+        b = len(news) - 1
+        n, L = news[b], lens[b]
+        j = L - max(1, n // 2)                                    # hidden from the rows before token j
+        table = kw["block_table"][b].tolist()
+        slot = table[j // page] * page + j % page
+        keep = kw["Kc"][slot, 0].clone()
+        kw["Kc"][slot, 0] = value
+        kw["O"].fill_(5.0)
+        rb.radar_chunk_attention(ctx, **kw)
+        torch.cuda.synchronize()
+        ctx.check_device_status()
+        kw["Kc"][slot, 0] = keep
+        first = int(kw["q_start"][b]) + n - (L - j)               # the first row that sees the key
+        G = Hq // Hkv
+        assert torch.equal(kw["O"][:first], want[:first]) and torch.equal(kw["O"][:, G:], want[:, G:])
+        if value != value:
+            last = int(kw["q_start"][b + 1])
+            assert torch.isnan(kw["O"][first:last, :G]).all() and torch.isnan(kw["lse"][first:last, :G]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bad_pages_and_requests(ctx, dtype):
+    """A page that is not in the cache is told and read as page 0; a request out of bounds is told and skipped, the others are as ever."""
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    for news, lens in (([20, 1, 70], [200, 300, 90]), ([1, 1, 1], [50, 300, 90])):
+        kw = T.check_chunk(ctx, _rng(9), news, lens, 4, 2, 64, 16, dtype)
+        start = kw["q_start"].tolist()
+        for name, at, value in (("cache_len", 1, -1), ("cache_len", 1, max(lens) + 1), ("cache_len", 1, 2 ** 31 - 1), ("block_table", (1, 2), 10 ** 6), ("block_table", (1, 2), -3)):
+            x = kw[name]
+            keep = x[at].clone()
+            x[at] = value
+            kw["O"].fill_(5.0)
+            rb.radar_chunk_attention(ctx, **kw)
+            assert ctx.read_device_status() == -1, (name, value)
+            x[at] = keep
+            T.hold_again(kw, [0, 2])
+            if name == "cache_len":
+                assert torch.all(kw["O"][start[1]:start[2]] == 5.0)
+        bad = kw["q_start"].clone()
+        bad[1], bad[2] = start[2] + 1, start[1]                     # request 1 runs backwards, 0 and 2 have too many rows or others'
+        rb.radar_chunk_attention(ctx, **dict(kw, q_start=bad))
+        assert ctx.read_device_status() == -1
+        bad = torch.tensor([start[0], start[1], start[2], kw["Q"].shape[0] + 1], dtype=torch.int32, device="cuda")
+        kw["O"].fill_(5.0)
+        rb.radar_chunk_attention(ctx, **dict(kw, q_start=bad))
+        assert ctx.read_device_status() == -1
+        T.hold_again(kw, [0, 1])
+        assert torch.all(kw["O"][start[2]:] == 5.0)
