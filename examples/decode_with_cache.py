@@ -1,11 +1,13 @@
-"""Speculative decoding of a small model over the 4-bit paged cache, from admission to release.
+"""Speculative decoding of a small model over a paged cache, from admission to release.
 
 A random-weight transformer decodes for a batch of requests: a bigram table is the draft model, a step's tree is verified in one
-pass whose attention reads the 4-bit cache, and what was accepted is appended to it.  Requests that reach their length give their
+pass whose attention reads the cache, and what was accepted is appended to it.  Requests that reach their length give their
 pages back, and prompts that wait take their places.  Between steps the host reads only the tokens.
 
-    python examples/decode_with_cache.py
+    python examples/decode_with_cache.py            # the 4-bit cache; learned positions, a prompt attends by itself
+    python examples/decode_with_cache.py --paged    # the bf16 cache; rotary positions, a prompt comes in chunks and attends over the cache
 """
+import argparse
 import os
 import sys
 
@@ -14,20 +16,21 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2512_14069_b200 import binding as rb  # noqa: E402
 from paper_2512_14069_b200 import workloads as W  # noqa: E402
-from paper_2512_14069_b200.cache import FourBitCache  # noqa: E402
+from paper_2512_14069_b200.cache import FourBitCache, PagedCache  # noqa: E402
 from paper_2512_14069_b200.pipeline import SpecStep  # noqa: E402
 
 ROWS = rb.RADAR_MAX_NODES
 
 
 class Model:
-    """Decoder layers of fused projection, attention and output projection; positions are learned."""
+    """Decoder layers of fused projection, attention and output projection; positions are learned, or (inv_freq) turn queries and keys."""
 
-    def __init__(self, *, layers, Hq, Hkv, d, V, max_len, seed=0):
+    def __init__(self, *, layers, Hq, Hkv, d, V, max_len, seed=0, rotary=False):
         g = torch.Generator().manual_seed(seed)
         w = lambda *shape: (torch.randn(*shape, generator=g) * shape[-1] ** -0.5).bfloat16().cuda()
         self.layers, self.Hq, self.Hkv, self.d, self.V, D = layers, Hq, Hkv, d, V, Hq * d
         self.E, self.pos, self.draft = w(V, D) * D ** 0.5, w(max_len, D) * D ** 0.5, w(V, V) * V ** 0.5
+        self.inv_freq = 10000.0 ** (-torch.arange(0, d, 2, device="cuda") / d) if rotary else None
         self.qkv, self.out = [w((Hq + 2 * Hkv) * d, D) for _ in range(layers)], [w(D, D) for _ in range(layers)]
 
     def split(self, qkv):
@@ -36,7 +39,7 @@ class Model:
 
     def forward(self, tokens, positions, attend):
         """Logits of tokens [B, rows]; attend(layer, Q, K, V) gives that layer's attention output [B, rows, Hq, d]."""
-        x = (self.E[tokens] + self.pos[positions]).float()
+        x = (self.E[tokens] if self.inv_freq is not None else self.E[tokens] + self.pos[positions]).float()
         for i in range(self.layers):
             h = torch.nn.functional.normalize(x, dim=-1).mul(x.shape[-1] ** 0.5).bfloat16()
             o = attend(i, *self.split((h @ self.qkv[i].T).unflatten(-1, (-1, self.d))))
@@ -45,11 +48,12 @@ class Model:
 
 
 class Decoder:
-    def __init__(self, ctx, model, *, B, k=4, t_max=4, N=16, page_size=16, n_pages=64, max_len=256, max_prompt=64):
+    def __init__(self, ctx, model, *, B, k=4, t_max=4, N=16, page_size=16, n_pages=64, max_len=256, max_prompt=64, chunk=24):
         self.ctx, self.model, self.B, self.k, self.t_max = ctx, model, B, k, t_max
         m = model
         self.step = SpecStep(ctx, B=B, V=m.V, k=k, t_max=t_max, N=N, Hq=m.Hq, Hkv=m.Hkv, d=m.d, kv_dtype=torch.bfloat16, max_prefix_len=max_len)
-        self.cache = FourBitCache(ctx, n_layers=m.layers, B=B, Hq=m.Hq, Hkv=m.Hkv, d=m.d, page_size=page_size, n_pages=n_pages, max_len=max_len,
+        self.paged, self.chunk = model.inv_freq is not None, chunk
+        self.cache = (PagedCache if self.paged else FourBitCache)(ctx, n_layers=m.layers, B=B, Hq=m.Hq, Hkv=m.Hkv, d=m.d, page_size=page_size, n_pages=n_pages, max_len=max_len,
                                   max_new=max(B * (t_max + 1), max_prompt))
         self.gate = {n: torch.from_numpy(v).cuda() for n, v in W.gate_weights(W.shrink(W.CONFIGS[1], k=k)).items()}
         self.draft_logits = torch.zeros(B, self.step.R, m.V, device="cuda")
@@ -60,6 +64,8 @@ class Decoder:
     def admit(self, b, prompt):
         """A prompt for request b, which must be empty.  Its last token becomes the root of the first step.  False: there are no pages
         for it."""
+        if self.paged:
+            return self.admit_chunks(b, prompt)
         m, n = self.model, len(prompt) - 1
         tokens = torch.tensor(prompt, device="cuda")
         K = torch.empty(m.layers, n, m.Hkv, m.d, dtype=torch.bfloat16, device="cuda")
@@ -77,6 +83,29 @@ class Decoder:
         self.root[b] = int(prompt[-1])
         return bool(self.cache.granted[b])
 
+    def admit_chunks(self, b, prompt):
+        """The prompt in chunks: a layer's rows are stored, their keys turned on the way, and attend to all that is there."""
+        m, c = self.model, self.cache
+        which = torch.arange(self.B, device="cuda") == b
+        tokens = torch.tensor(prompt, device="cuda")
+        for first in range(0, max(len(prompt) - 1, 1), self.chunk):
+            n = min(self.chunk, len(prompt) - 1 - first)
+            c.begin(torch.where(which, n, 0).to(torch.int32), n, requests=which)
+            if not c.granted[b]:                         # what is there goes back
+                c.release(which)
+                return False
+            if n == 0:
+                break
+
+            def attend(layer, Q, K, V):
+                turned, O = Q[0].contiguous(), torch.empty_like(Q[0])
+                c.store(layer, K[0], V[0], Q=turned, Q_out=turned, inv_freq=m.inv_freq)
+                c.attention(layer, turned, O)
+                return O[None]
+            m.forward(tokens[None, first:first + n], c.pos[None, :n].long(), attend)
+        self.root[b] = int(prompt[-1])
+        return True
+
     def draft(self):
         """The draft calls of a step: rows of the bigram table for the root, then for each call's frontier."""
         s, k = self.step, self.k
@@ -91,7 +120,13 @@ class Decoder:
         s, c = self.step, self.cache
 
         def attend(layer, Q, Kt, Vt):
-            s.attention_cached(c, layer, Q, Kt, Vt)
+            if self.paged:
+                Q, Kt, Vt = Q.contiguous(), Kt.contiguous(), Vt.contiguous()
+                rb.radar_rotate(self.ctx, Q=Q.flatten(0, 1), Q_out=Q.flatten(0, 1), K=Kt.flatten(0, 1), K_out=Kt.flatten(0, 1), pos=s.tree_pos.flatten(),
+                                inv_freq=self.model.inv_freq)
+                s.attention_paged(c, layer, Q, Kt, Vt)
+            else:
+                s.attention_cached(c, layer, Q, Kt, Vt)
             self.K[layer], self.V[layer] = Kt, Vt
             if check is not None:
                 check(layer, Q, Kt, Vt)
@@ -114,10 +149,10 @@ class Decoder:
         return [path[b][1:1 + lens[b]] + [nxt[b]] if took[b] else [] for b in range(self.B)]
 
 
-def main(requests=6, B=3, tokens=24, seed=1, n_pages=64):
+def main(requests=6, B=3, tokens=24, seed=1, n_pages=64, paged=False):
     torch.manual_seed(seed)
     ctx = rb.Context(0)
-    model = Model(layers=2, Hq=8, Hkv=2, d=64, V=512, max_len=256)
+    model = Model(layers=2, Hq=8, Hkv=2, d=64, V=512, max_len=256, rotary=paged)
     dec = Decoder(ctx, model, B=B, n_pages=n_pages)
     prompts = [torch.randint(0, model.V, (int(n),)).tolist() for n in torch.randint(5, 60, (requests,))]
     waiting, text = list(range(requests)), [[] for _ in range(requests)]
@@ -156,4 +191,6 @@ def main(requests=6, B=3, tokens=24, seed=1, n_pages=64):
 
 
 if __name__ == "__main__":
-    main()
+    parser = argparse.ArgumentParser(description="speculative decoding over a paged cache")
+    parser.add_argument("--paged", action="store_true", help="the bf16 cache, rotary positions, prompts in chunks")
+    main(paged=parser.parse_args().paged)

@@ -229,6 +229,12 @@ class SpecStep:
         """The tree's attention in one layer over a `cache.FourBitCache` of the step's requests."""
         cache.attention(layer, Q, Kt, Vt, self.O, self.lse, mask=self.tree_mask, n_nodes=self.n_nodes, max_cache_len=max_cache_len)
 
+    def attention_paged(self, cache, layer, Q, Kt, Vt):
+        """The tree's attention in one layer over a `cache.PagedCache` of the step's requests."""
+        if cache.max_len < self.max_prefix_len:
+            raise ValueError(f"the step is made for prefixes of {self.max_prefix_len} tokens, the cache's table has room for {cache.max_len}")
+        self.attention(Q, cache.Kc[layer], cache.Vc[layer], None, cache.cache_len, Kt, Vt, block_table=cache.block_table, page_size=cache.page_size)
+
     def accept(self, target_logits, draft_logits=None, u_accept=None, u_sample=None):
         rb.radar_verify_accept(
             self.ctx, B=self.B, V=self.V, t_max=self.t_max, N=self.N, mode=self.mode, temperature=self.temperature,
