@@ -212,3 +212,35 @@ def test_refusals(ctx):
     s = SpecStep(ctx, B=3, V=64, k=4, t_max=4, N=16, Hq=6, Hkv=2, d=64, kv_dtype=torch.bfloat16, max_prefix_len=400)
     with pytest.raises(ValueError, match="has room for"):
         s.attention_paged(c, 0, None, None, None)
+    bf = lambda *x: torch.zeros(*x, dtype=torch.bfloat16, device="cuda")
+    i32 = lambda *x: torch.zeros(*x, dtype=torch.int32, device="cuda")
+    f32 = lambda *x: torch.zeros(*x, device="cuda")
+    rotate = dict(Q=bf(4, 2, 64), Q_out=bf(4, 2, 64), pos=i32(4), inv_freq=f32(32))
+    rb.radar_rotate(ctx, **rotate)
+    for change in (dict(Q=None), dict(Q_out=None), dict(Q_out=bf(4, 3, 64)), dict(Q_out=f32(4, 2, 64)), dict(K=bf(5, 2, 64), K_out=bf(5, 2, 64)), dict(pos=None), dict(pos=i32(3)),
+                   dict(pos=torch.zeros(4, dtype=torch.int64, device="cuda")), dict(pos=i32(2, 2, 4)), dict(inv_freq=bf(32)), dict(pair_axis=torch.zeros(31, dtype=torch.uint8, device="cuda")),
+                   dict(Q=bf(4, 2, 64).cpu()), dict(Q=bf(4, 64, 2).transpose(1, 2)), dict(Q=bf(8, 64)), dict(Q=bf(4, 2, 64).half(), Q_out=bf(4, 2, 64).half())):
+        with pytest.raises((ValueError, TypeError)):
+            rb.radar_rotate(ctx, **dict(rotate, **change))
+    with pytest.raises(rb.RadarError):
+        rb.radar_rotate(ctx, **dict(rotate, inv_freq=f32(33)))
+    store = dict(K=bf(4, 2, 64), V=bf(4, 2, 64), slots=torch.arange(4, device="cuda"), Kc=bf(16, 2, 64), Vc=bf(16, 2, 64))
+    rb.radar_paged_store(ctx, **store)
+    rb.radar_paged_store(ctx, **dict(store, Kc=bf(1, 16, 2, 64), Vc=bf(1, 16, 2, 64)))          # (pages of 16 rows)
+    for change in (dict(V=bf(3, 2, 64)), dict(V=f32(4, 2, 64)), dict(V=bf(4, 4, 64)[:, :2]), dict(slots=i32(4)), dict(slots=torch.arange(5, device="cuda")), dict(src_row=i32(3)), dict(Kc=f32(16, 2, 64)),
+                   dict(Kc=bf(16, 3, 64), Vc=bf(16, 3, 64)), dict(Vc=bf(17, 2, 64)), dict(Q=bf(4, 6, 64)), dict(Q_out=bf(4, 6, 64)), dict(Q=bf(5, 6, 64), Q_out=bf(5, 6, 64)),
+                   dict(Q=bf(4, 6, 64), Q_out=bf(3, 6, 64)), dict(Q=f32(4, 6, 64), Q_out=f32(4, 6, 64)), dict(K=bf(4, 2, 64).cpu(), V=bf(4, 2, 64).cpu()), dict(pos=i32(3), inv_freq=f32(8))):
+        with pytest.raises((ValueError, TypeError)):
+            rb.radar_paged_store(ctx, **dict(store, **change))
+    attend = dict(Q=bf(5, 6, 64), q_start=i32(3), Kc=bf(64, 2, 64), Vc=bf(64, 2, 64), page_size=16, block_table=i32(2, 4), cache_len=i32(2), max_new=5, max_cache_len=64, O=bf(5, 6, 64),
+                  workspace=c.workspace)
+    rb.radar_chunk_attention(ctx, **attend)
+    for change in (dict(Q=f32(5, 6, 64)), dict(O=bf(4, 6, 64)), dict(O=bf(5, 12, 64)[:, ::2]), dict(q_start=i32(2)), dict(block_table=i32(3, 4)), dict(block_table=i32(8)), dict(Vc=bf(63, 2, 64)),
+                   dict(Kc=bf(64, 2, 128), Vc=bf(64, 2, 128)), dict(lse=f32(6, 5)), dict(lse=bf(5, 6)), dict(cache_len=torch.zeros(2, dtype=torch.int64, device="cuda")), dict(workspace=f32(1 << 20)),
+                   dict(page_size=None), dict(max_new=1 << 40)):
+        with pytest.raises((ValueError, TypeError, OverflowError)):
+            rb.radar_chunk_attention(ctx, **dict(attend, **change))
+    for change in (dict(page_size=24), dict(max_cache_len=65), dict(workspace=c.workspace[:1024]), dict(workspace=c.workspace[16:]), dict(Kc=bf(64, 4, 64), Vc=bf(64, 4, 64))):
+        with pytest.raises(rb.RadarError):
+            rb.radar_chunk_attention(ctx, **dict(attend, **change))
+    assert ctx.read_device_status() == 0
