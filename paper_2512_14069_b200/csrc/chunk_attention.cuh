@@ -32,6 +32,7 @@ struct ChunkParams {
     int unit_tokens;         // of one row block or a pair of them
     int unit_records;        // partial records of a unit; the second row block's start at half of it
     int n_cta;
+    uint64_t cta_magic;      // floor(2^64 / n_cta): see bound_of
     float scale_log2;
     float2* part_ml;         // [n_cta][2][unit_records]     (m in log2 units, l)
     float* part_o;           // [n_cta][2][unit_records][D]
@@ -80,27 +81,33 @@ __device__ __forceinline__ Unit<C> unit_of(const ChunkParams& P, const ChunkSeq&
     u.w = u.rows > P.rb_rows ? C::kTwo : C::kOne;
     return u;
 }
-// size of a request's first m units of one KV head, none of them its last; unit i has max(base + (i + 1) T, 1) keys
+// size of a request's first m units of one head group, none of them its last; unit i has max(base + (i + 1) T, 1) keys
 template <class C>
 __device__ __forceinline__ long long size_before(const ChunkParams& P, const ChunkSeq& s, int m) {
-    const long long T = P.unit_tokens, base = (long long)s.len - s.n;
-    const long long none = base >= 0 ? 0 : min((long long)m, -base / T);       // units whose last token sees nothing (or one key)
+    const int T = P.unit_tokens, base = s.len - s.n;
+    const long long none = base >= 0 ? 0 : min((unsigned)m, (unsigned)-base / (unsigned)T);       // units whose last token sees nothing (or one key)
     const long long keys = none + (m - none) * base + T * ((long long)m * (m + 1) - none * (none + 1)) / 2;
-    return keys * (P.unit_tokens > P.tokens_per_rb ? C::kTwo : C::kOne) + (long long)m * C::kUnit;
+    return keys * (T > P.tokens_per_rb ? C::kTwo : C::kOne) + (long long)m * C::kUnit;
 }
+// ... of all of them
 template <class C>
-__device__ __forceinline__ long long seq_size(const ChunkParams& P, const ChunkSeq& s) {
+__device__ __forceinline__ long long head_size(const ChunkParams& P, const ChunkSeq& s) {
     if (s.n == 0) return 0;
     const int nq = units_of(P, s);
-    return P.groups * (size_before<C>(P, s, nq - 1) + unit_of<C>(P, s, nq - 1).size());
+    return size_before<C>(P, s, nq - 1) + unit_of<C>(P, s, nq - 1).size();
 }
 // number of tiles of a unit at position U that start before position x
 template <class C>
 __device__ __forceinline__ int tiles_before(long long x, long long U, int nt, int w) {
     const long long d = x - U - C::kUnit;
     if (d <= 0) return 0;
-    if (d >= (long long)nt * C::kTile * w) return nt;
-    return (int)((d + C::kTile * w - 1) / (C::kTile * w));
+    const long long t = (d + C::kTile - 1) / C::kTile;       // (a tile is kTile w; below nt w it fits an int)
+    if (t >= (long long)nt * w) return nt;
+    return w == C::kTwo ? ((unsigned)t + C::kTwo - 1) / C::kTwo : ((unsigned)t + C::kOne - 1) / C::kOne;
+}
+// where CTA c's range begins, for a space of size tot: tot c / n_cta or a little less, without a division
+__device__ __forceinline__ long long bound_of(const ChunkParams& P, long long tot, int c) {
+    return c >= P.n_cta ? tot : (long long)__umul64hi((unsigned long long)tot * (unsigned)c, P.cta_magic);
 }
 
 // One CTA's walk over its range [.., hi): segments (unit, tiles [t0, t1)).
@@ -137,28 +144,38 @@ struct Walk {
 };
 
 // The first segment of CTA ci, by a whole warp: the unit that contains the start of its range, from the unit's first tile that starts at
-// or after it.  tot: size of the space.
+// or after it.  tot: size of the space.  (What a launch waits for before its first load: 3600 to 4600 cycles with 64-bit divisions and the sizes
+// read twice.)
 template <class C>
 __device__ __forceinline__ Walk<C> first_segment(const ChunkParams& P, int ci, long long& tot) {
     const int lane = threadIdx.x & 31, B = P.a.B;
     bool ok = true;
-    ChunkSeq mine;                       // of request lane: with up to 32 of them every size is read once
-    mine.n = 0;
+    ChunkSeq mine;                       // of request lane, and its sizes: with up to 32 of them everything is read once
+    mine.q0 = mine.n = mine.len = 0;
     if (lane < B) mine = chunk_seq(P.a, lane, ok);
-    const long long my_size = lane < B ? seq_size<C>(P, mine) : 0;
-    tot = warp_sum(my_size);
+    const long long my_head = head_size<C>(P, mine);
+    auto running = [&](long long v) {    // sums over the lanes up to this one
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(kFull, v, o);
+            if (lane >= o) v += x;
+        }
+        return v;
+    };
+    const long long my_incl = B == 1 ? my_head * P.groups : running(my_head * P.groups);
+    tot = __shfl_sync(kFull, my_incl, B == 1 ? 0 : 31);
 #pragma unroll 1
     for (int b0 = 32; b0 < B; b0 += 32) {
         const int b = b0 + lane;
         bool ok_b = true;
-        const long long size = b < B ? seq_size<C>(P, chunk_seq(P.a, b, ok_b)) : 0;
+        const long long size = b < B ? head_size<C>(P, chunk_seq(P.a, b, ok_b)) * P.groups : 0;
         ok = ok && ok_b;
         tot += warp_sum(size);
     }
     if (!ok && ci == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
     Walk<C> cur;
-    const long long lo = tot * ci / P.n_cta;
-    cur.hi = tot * (ci + 1) / P.n_cta;
+    const long long lo = bound_of(P, tot, ci);
+    cur.hi = bound_of(P, tot, ci + 1);
     cur.t0 = cur.t1 = 0;
     cur.b = -1;
     cur.g = cur.i = cur.nq = 0;
@@ -170,29 +187,33 @@ __device__ __forceinline__ Walk<C> first_segment(const ChunkParams& P, int ci, l
     for (int b0 = 0; b0 < B && cur.b < 0; b0 += 32) {
         const int b = b0 + lane;
         bool ok_b;
-        const long long size = b0 == 0 ? my_size : b < B ? seq_size<C>(P, chunk_seq(P.a, b, ok_b)) : 0;
-        long long incl = size;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(kFull, incl, o);
-            if (lane >= o) incl += v;
+        ChunkSeq s = mine;
+        long long head = my_head, incl = my_incl;
+        if (b0 > 0) {
+            s.q0 = s.n = s.len = 0;
+            if (b < B) s = chunk_seq(P.a, b, ok_b);
+            head = head_size<C>(P, s);
+            incl = running(head * P.groups);
         }
-        const unsigned hit = __ballot_sync(kFull, cum + incl > lo);
+        const unsigned hit = __ballot_sync(kFull, b < B && cum + incl > lo);
         if (hit) {
             const int src = __ffs(hit) - 1;
-            const long long before = cum + __shfl_sync(kFull, incl - size, src), head = __shfl_sync(kFull, size, src) / P.groups;
+            const long long size = __shfl_sync(kFull, head, src), at = lo - cum - __shfl_sync(kFull, incl - head * P.groups, src);
             cur.b = b0 + src;
-            cur.s = chunk_seq(P.a, cur.b, ok_b);
+            cur.s.q0 = __shfl_sync(kFull, s.q0, src); cur.s.n = __shfl_sync(kFull, s.n, src); cur.s.len = __shfl_sync(kFull, s.len, src);
             cur.nq = units_of(P, cur.s);
-            cur.g = (int)((lo - before) / head);
-            const long long at = lo - before - cur.g * head;
-            int m0 = 0, m1 = cur.nq - 1;                         // the last unit that starts at or before `at`
+            int g = (int)((double)at / (double)size);            // (off by one at most)
+            if (g * size > at) --g;
+            else if ((g + 1) * size <= at) ++g;
+            cur.g = g;
+            const long long in_head = at - g * size;
+            int m0 = 0, m1 = cur.nq - 1;                         // the last unit that starts at or before it
             while (m0 < m1) {
                 const int m = m0 + (m1 - m0 + 1) / 2;
-                if (size_before<C>(P, cur.s, m) <= at) m0 = m; else m1 = m - 1;
+                if (size_before<C>(P, cur.s, m) <= in_head) m0 = m; else m1 = m - 1;
             }
             cur.i = m0;
-            cur.U = before + cur.g * head + size_before<C>(P, cur.s, m0);
+            cur.U = lo - in_head + size_before<C>(P, cur.s, m0);
             cur.u = unit_of<C>(P, cur.s, m0);
         }
         cum += __shfl_sync(kFull, incl, 31);
@@ -221,7 +242,7 @@ __device__ __forceinline__ void write_cut(const ChunkParams& P, int ci, const Ch
 #pragma unroll 1
         for (int k = 0; k < kMaxCtas / 32; ++k) {
             const int c = ci + k * 32 + lane;
-            const long long lo = cut.tot * c / P.n_cta, hi = cut.tot * (c + 1) / P.n_cta;
+            const long long lo = bound_of(P, cut.tot, c), hi = bound_of(P, cut.tot, c + 1);
             const bool piece = c < P.n_cta && lo < u1;
             const bool live = piece && tiles_before<C>(hi, u0, cut.nt, cut.w) > tiles_before<C>(lo, u0, cut.nt, cut.w);
             const uint32_t pieces = __ballot_sync(kFull, piece), bits = __ballot_sync(kFull, live);
@@ -357,6 +378,7 @@ inline size_t chunk_partial_bytes(size_t grid, int unit_records, int d) {
     return align_up(rec * sizeof(float2), 256) + align_up(rec * d * sizeof(float), 256) + align_up(grid * sizeof(ChunkCut), 256);
 }
 inline void chunk_carve(ChunkParams& P) {
+    P.cta_magic = P.n_cta > 1 ? ~0ull / (unsigned)P.n_cta : ~0ull;
     const size_t rec = (size_t)P.n_cta * 2 * P.unit_records;
     P.part_ml = reinterpret_cast<float2*>(P.a.workspace);
     P.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(P.a.workspace) + align_up(rec * sizeof(float2), 256));

@@ -18,6 +18,7 @@
 // tensor memory and returns.
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 
 #include "attn_tiles.cuh"
 #include "chunk_attention.cuh"
@@ -66,13 +67,17 @@ struct Pages {
         : n_cache_pages((int)(a.cache_rows / a.page_size)), per(min(a.page_size, kTileKeys)), box_shift(a.page_size == 16 ? 4 : a.page_size == 32 ? 5 : a.page_size == 64 ? 6 : 7),
           tiles_per_page(max(a.page_size / kTileKeys, 1)) {}       // (cache_rows: below 2^31)
     __device__ __forceinline__ int boxes(const Segment& s, int t) const { return (min(kTileKeys, s.keys - t * kTileKeys) + per - 1) >> box_shift; }
-    // cache row of the lane's page
-    __device__ __forceinline__ int row_of(const ChunkParams& P, const Segment& s, int t, int lane) const {
-        if (lane >= boxes(s, t)) return 0;
-        const int index = (tiles_per_page > 1 ? t / tiles_per_page : t << (7 - box_shift)) + lane;
-        int page = P.a.block_table[(long long)s.b * P.a.max_pages + index];
-        if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
-        return page * P.a.page_size + (tiles_per_page > 1 ? (t - index * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
+    // the lane's page of a tile, and the cache row that it begins at
+    __device__ __forceinline__ int index_of(int t, int lane) const { return (tiles_per_page > 1 ? t / tiles_per_page : t << (7 - box_shift)) + lane; }
+    __device__ __forceinline__ int page_of(const ChunkParams& P, const Segment& s, int t, int lane) const {
+        return lane < boxes(s, t) ? P.a.block_table[(long long)s.b * P.a.max_pages + index_of(t, lane)] : 0;
+    }
+    __device__ __forceinline__ int row_of(const ChunkParams& P, const Segment& s, int page, int t, int lane) const {
+        if (page < 0 || page >= n_cache_pages) {
+            if (lane < boxes(s, t)) set_status(P.status, RADAR_ERR_INVALID_ARG);
+            page = 0;
+        }
+        return page * P.a.page_size + (tiles_per_page > 1 ? (t - index_of(t, lane) * tiles_per_page) * kTileKeys : 0);   // (below cache_rows)
     }
     template <int D>
     __device__ __forceinline__ void fetch(const Segment& s, int t, int row, unsigned char* dst, const CUtensorMap* tm, uint64_t* full, int lane) const {
@@ -99,12 +104,16 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     // Static block first (padded to a multiple of 1024 bytes and aligned to it), the tiles behind it: the
     // swizzled tiles need a 1024-byte boundary and there is no room left for alignment slack.
     struct Shared {
+        // (in the order of barrier_arrivals)
         uint64_t bar_qfull, bar_qempty, bar_kfull[RK], bar_kempty[RK], bar_vfull[RV], bar_vempty[RV];
-        uint64_t bar_sfull[2], bar_odone[2], bar_ofree[2], bar_mlfull, bar_mlempty;
+        uint64_t bar_sfull[2], bar_odone[2];
         uint64_t bar_idle;               // every product issued has run
+        uint64_t bar_segfull[kSegRing];
         uint64_t bar_pfirst[2];          // the probabilities of the tile's first kFirstKeys keys are there
         uint64_t bar_pready[2];          // ... all of them
-        uint64_t bar_segfull[kSegRing], bar_segempty[kSegRing];
+        uint64_t bar_ofree[2], bar_mlempty;
+        uint64_t bar_mlfull;
+        uint64_t bar_segempty[kSegRing];
         uint32_t q_last, k_next, v_next; // the producer's: phase parity of the last Q, slot and parity of the next K and V
         uint32_t tmem_base;
         int abort;
@@ -127,22 +136,14 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 
     // ---- set-up ----
     if (warp == 0) {
+        constexpr int kOnes = 2 + 2 * RK + 2 * RV + 5 + kSegRing, kFours = 7, kBarriers = kOnes + kFours + 1 + kSegRing;
+        static_assert(offsetof(Shared, bar_pfirst) == 8 * kOnes && offsetof(Shared, bar_mlfull) == 8 * (kOnes + kFours) && offsetof(Shared, q_last) == 8 * kBarriers, "barriers in order");
+        for (int i = lane; i < kBarriers; i += 32)
+            mbar_init(&st.bar_qfull + i, i < kOnes ? 1 : i < kOnes + kFours ? 4 : i == kOnes + kFours ? 8 : kProducerWarp + 2);
+        fence_barrier_init();
         if (lane == 0) {
             st.abort = 0;
-            mbar_init(&st.bar_qfull, 1);
-            mbar_init(&st.bar_qempty, 1);
-            for (int i = 0; i < RK; ++i) { mbar_init(&st.bar_kfull[i], 1); mbar_init(&st.bar_kempty[i], 1); }
-            for (int i = 0; i < RV; ++i) { mbar_init(&st.bar_vfull[i], 1); mbar_init(&st.bar_vempty[i], 1); }
-            for (int i = 0; i < 2; ++i) {
-                mbar_init(&st.bar_sfull[i], 1); mbar_init(&st.bar_pfirst[i], 4); mbar_init(&st.bar_pready[i], 4);
-                mbar_init(&st.bar_odone[i], 1); mbar_init(&st.bar_ofree[i], 4);
-            }
-            for (int i = 0; i < kSegRing; ++i) { mbar_init(&st.bar_segfull[i], 1); mbar_init(&st.bar_segempty[i], kProducerWarp + 2); }
-            mbar_init(&st.bar_idle, 1);
             st.q_last = 1;
-            mbar_init(&st.bar_mlfull, 8);
-            mbar_init(&st.bar_mlempty, 4);
-            fence_barrier_init();
         }
     } else if (warp == kMmaWarp) {
         tmem_alloc(&st.tmem_base, 512);
@@ -459,14 +460,13 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                 };
                 // Q's slot is free only after the last S of the segment before, so the first K tiles go ahead of it; the CTA's first segment finds
-                // it free, and its keys have to be looked up first.
+                // it free, while its keys are looked up.
+                int page = pages.page_of(P, s, s.t0, lane);
                 if (seg == 0 && lead) fetch_q();
-                cur.next(P);
-                int row = pages.row_of(P, s, s.t0, lane);
 #pragma unroll 1
                 for (int i = 0; i < s.n; ++i) {
-                    const int here = row;
-                    if (i + 1 < s.n) row = pages.row_of(P, s, s.t0 + i + 1, lane);       // (its page is looked up while the slot is not free yet)
+                    const int here = pages.row_of(P, s, page, s.t0 + i, lane);
+                    if (i + 1 < s.n) page = pages.page_of(P, s, s.t0 + i + 1, lane);     // (looked up while the slot is not free yet)
                     if (lead) ok = mbar_wait_while(ok, &st.bar_kempty[slot], par);
                     ok = __shfl_sync(kFull, ok, 0);
                     if (!ok) break;                                  // (the ring's position stays that of the last load)
@@ -474,6 +474,7 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     if (++slot == RK) { slot = 0; par ^= 1; }
                     if (i == min(s.n, 2) - 1 && seg > 0 && lead) fetch_q();
                 }
+                cur.next(P);
             }
             __syncwarp();
             write_cut<Costs>(P, blockIdx.x, cut);
@@ -485,11 +486,11 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             uint32_t slot = 0, par = 1;
             Segment s;
             for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
-                int row = pages.row_of(P, s, s.t0, lane);
+                int page = pages.page_of(P, s, s.t0, lane);
 #pragma unroll 1
                 for (int i = 0; i < s.n; ++i) {
-                    const int here = row;
-                    if (i + 1 < s.n) row = pages.row_of(P, s, s.t0 + i + 1, lane);
+                    const int here = pages.row_of(P, s, page, s.t0 + i, lane);
+                    if (i + 1 < s.n) page = pages.page_of(P, s, s.t0 + i + 1, lane);
                     if (lane == 0) ok = mbar_wait_while(ok, &st.bar_vempty[slot], par);
                     ok = __shfl_sync(kFull, ok, 0);
                     if (!ok) break;
