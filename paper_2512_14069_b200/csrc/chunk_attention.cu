@@ -258,10 +258,10 @@ extern "C" int radar_chunk_attention(radar_ctx* ctx, const radar_chunk_attn_args
         a->workspace_bytes < radar_chunk_attn_workspace_bytes(ctx, a->B, a->Hq, a->Hkv, a->d, a->dtype, a->max_new, a->max_cache_len))
         return RADAR_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-    if (a->dtype == RADAR_F32) return a->d == 128 ? fma_launch<128>(ctx, *a, stream) : fma_launch<64>(ctx, *a, stream);
     bool taken;
     const int status = chunk_rows_launch(ctx, a, stream, taken);
     if (taken || status != RADAR_OK) return status;
+    if (a->dtype == RADAR_F32) return a->d == 128 ? fma_launch<128>(ctx, *a, stream) : fma_launch<64>(ctx, *a, stream);
     if (!chunk_tc_supported(a)) return RADAR_ERR_CUDA;
     return chunk_tc_launch(ctx, a, stream);
 }

@@ -1,8 +1,8 @@
-// Chunk attention of few rows (single tokens above all) over the paged bf16 cache, where there is little to read: what bounds such a call is the
+// Chunk attention of few rows (single tokens above all) over the paged cache, where there is little to read: what bounds such a call is the
 // way from the block table to a key and back, so every warp of the machine takes a few keys at once and a unit's blocks merge in
 // their cluster's shared memory, in one launch.
 //
-// A unit (request, KV head) has up to 8 NT rows (token * G + head in group).  A warp takes 16 keys at a time, keys and values straight from
+// A unit (request, KV head) has up to 8 NT rows (token * G + head in group).  bf16: a warp takes 16 keys at a time, keys and values straight from
 // memory into the fragments of mma.sync (m16n8k16), keys as M, rows as N:
 //   S^T (16 keys x 8 rows) = K Q^T.  The sum over channels may run in any order, so lane (g, q) = (lane / 4, lane % 4) holds of keys g and
 //       g + 8 the 16 channels from 16 q on of every 64, 32 bytes that lie together, and of row g the same channels.
@@ -10,9 +10,11 @@
 //   O^T (16 channels x 8 rows) += V^T P^T.  The channels may stand in any order, so lane (g, q) holds of keys 2 q, 2 q + 1, 2 q + 8 and
 //       2 q + 9 the D / 8 channels from D g / 8 on; two keys' halves are put together by byte permutation.  A lane ends with these channels
 //       of rows 2 q and 2 q + 1.
+// fp32: a warp takes 8 keys at a time on the FMA units, four lanes to a key for the scores (queries from shared memory, two exchanges a row), then
+// all lanes to a value's channels (a probability by one exchange).
 // The reference of a row's exponentials moves only when a score passes it by 2^8 (for all lanes at once), so the loop has one vote and no
 // exchange.  Sums are fp32; a probability enters its product as bf16.
-#include <algorithm>
+#include <type_traits>
 
 #include "attn_tiles.cuh"
 #include "chunk_attention.cuh"
@@ -23,9 +25,9 @@ namespace {
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kChunk = 16;        // keys of a chunk: they lie in one page
 constexpr int kMostSplit = 16;                                        // blocks of a unit: a cluster
 
-template <int D, int NT>
+template <int D, int R>
 struct RowsSmem {
-    static constexpr int kRows = 8 * NT;
+    static constexpr int kRows = R;
     float o[kWarps][kRows][D];           // of each warp
     float2 ml[kWarps][kRows];            // (m in log2 units, l)
     float block_o[kRows][D];             // of the block, for its cluster
@@ -68,10 +70,67 @@ __device__ __forceinline__ float2 load_cluster2(uint32_t at) {
 // weight of a part with maximum m in a whole with maximum top (-inf: nothing there)
 __device__ __forceinline__ float part_weight(float m, float top) { return ex2(m - (top == -CUDART_INF_F ? 0.f : top)); }
 
+// The unit's output from its warps' parts, by all threads of its blocks.
+template <typename T, int D, int R>
+__device__ __forceinline__ void merge_parts(RowsSmem<D, R>& sm, const ChunkParams& P, const ChunkSeq& s, int g, int rows, int rank, int split) {
+    const radar_chunk_attn_args& a = P.a;
+    const int tid = threadIdx.x;
+    __syncthreads();
+    auto write = [&](int r, int c4, float4 v, float top, float sum) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int token = r / P.G;
+        const int64_t out_row = (int64_t)(s.q0 + token) * a.Hq + g * P.G + r - token * P.G;
+        T* const to = reinterpret_cast<T*>(a.O) + out_row * D + c4 * 4;
+        if constexpr (sizeof(T) == 2) {
+            const __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+            *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        } else {
+            *reinterpret_cast<float4*>(to) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        }
+        if (c4 == 0 && a.lse != nullptr) a.lse[out_row] = sum == 0.f ? -CUDART_INF_F : lse_of(top, sum);
+    };
+    // parts: their (m, l) and four channels; added up in order.  A part that saw no key has l = 0 and O = 0; one whose sum is NaN makes the row NaN
+    auto merge = [&](int n, auto ml_of, auto o_of, float4& v, float& top, float& sum) {
+        top = -CUDART_INF_F;
+        for (int i = 0; i < n; ++i) top = fmaxf(top, ml_of(i).x);
+        v = make_float4(0.f, 0.f, 0.f, 0.f);
+        sum = 0.f;
+        for (int i = 0; i < n; ++i) {
+            const float2 ml = ml_of(i);
+            const float4 x = o_of(i);
+            const float w = part_weight(ml.x, top);
+            sum = fmaf(ml.y, w, sum);
+            v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(x.z, w, v.z); v.w = fmaf(x.w, w, v.w);
+        }
+    };
+    for (int e = tid; e < rows * (D / 4); e += kThreads) {
+        const int r = e / (D / 4), c4 = e % (D / 4);
+        float4 v;
+        float top, sum;
+        merge(kWarps, [&](int i) { return sm.ml[i][r]; }, [&](int i) { return *reinterpret_cast<const float4*>(&sm.o[i][r][c4 * 4]); }, v, top, sum);
+        if (split == 1) {
+            write(r, c4, v, top, sum);
+        } else {
+            *reinterpret_cast<float4*>(&sm.block_o[r][c4 * 4]) = v;
+            if (c4 == 0) sm.block_ml[r] = make_float2(top, sum);
+        }
+    }
+    if (split == 1) return;
+    cluster_barrier();
+    for (int e = rank * kThreads + tid; e < rows * (D / 4); e += split * kThreads) {
+        const int r = e / (D / 4), c4 = e % (D / 4);
+        float4 v;
+        float top, sum;
+        merge(split, [&](int i) { return load_cluster2(cluster_addr(&sm.block_ml[r], i)); }, [&](int i) { return load_cluster4(cluster_addr(&sm.block_o[r][c4 * 4], i)); }, v, top, sum);
+        write(r, c4, v, top, sum);
+    }
+    cluster_barrier();                                       // nobody leaves while its shared memory is read
+}
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) chunk_attn_rows_kernel(const ChunkParams P, const int split) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    using Smem = RowsSmem<D, NT>;
+    using Smem = RowsSmem<D, 8 * NT>;
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
     constexpr int kBlocks = D / 64, MT = D / 16, kVWords = D / 16;     // 64-channel blocks, 16-channel tiles of O, words of a lane's values
     const radar_chunk_attn_args& a = P.a;
@@ -212,51 +271,131 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) chunk_attn_rows_ker
 #pragma unroll
             for (int j = 0; j < MT; ++j) *reinterpret_cast<float2*>(&sm.o[warp][r][lg * (D / 8) + 2 * j]) = make_float2(o[t][j][i], o[t][j][i + 2]);
         }
+    merge_parts<__nv_bfloat16>(sm, P, s, g, rows, rank, split);
+}
+
+constexpr int kChunkF32 = 8;             // keys of a chunk
+
+template <int D, int R>
+__global__ void __launch_bounds__(kThreads, R == 8 ? 2 : 1) chunk_attn_rows_f32_kernel(const ChunkParams P, const int split) {
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    using Smem = RowsSmem<D, R>;
+    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+    float (*const sq)[D] = sm.block_o;                       // the queries, until the warps' parts are merged
+    constexpr int kBlocks = D / 32, E = D / 32;              // 32-channel blocks, channels of a lane's values
+    const radar_chunk_attn_args& a = P.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lq = lane & 3;
+    const int rank = blockIdx.x % split, unit = blockIdx.x / split, b = unit / a.Hkv, g = unit - b * a.Hkv;
+    chain_wait();
+    bool seq_ok;
+    const ChunkSeq s = chunk_seq(a, b, seq_ok);
+    if (!seq_ok && rank == 0 && g == 0 && tid == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
+    const int rows = s.n * P.G;                              // (at most R: the host has looked at max_new)
+    if (rows == 0) return;                                   // (the whole cluster)
+    const int chunks = (s.len + kChunkF32 - 1) / kChunkF32, step = split * kWarps, per_page = a.page_size / kChunkF32;
+    const int n_cache_pages = (int)(a.cache_rows / a.page_size);
+    const int* const table = a.block_table + (int64_t)b * a.max_pages;
+    const int64_t row_elems = (int64_t)a.Hkv * D;
+    const float *const Kc = reinterpret_cast<const float*>(a.Kc) + g * D, *const Vc = reinterpret_cast<const float*>(a.Vc) + g * D;
+    auto page_of = [&](int chunk) { return chunk < chunks ? table[chunk / per_page] : 0; };
+    int chunk = rank * kWarps + warp;
+    int page = page_of(chunk);
+    for (int e = tid; e < R * (D / 4); e += kThreads) {
+        const int r = e / (D / 4), c = e % (D / 4) * 4, token = r / P.G;
+        float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows) q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.Q) + (int64_t)(s.q0 + token) * a.q_row_stride + (int64_t)(g * P.G + r - token * P.G) * D + c);
+        *reinterpret_cast<float4*>(&sq[r][c]) = q;
+    }
     __syncthreads();
-    auto write = [&](int r, int c4, float4 v, float top, float sum) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int token = r / P.G;
-        const int64_t out_row = (int64_t)(s.q0 + token) * a.Hq + g * P.G + r - token * P.G;
-        const __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.O) + out_row * D + c4 * 4) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        if (c4 == 0 && a.lse != nullptr) a.lse[out_row] = sum == 0.f ? -CUDART_INF_F : lse_of(top, sum);
-    };
-    // parts: their (m, l) and four channels; added up in order.  A part that saw no key has l = 0 and O = 0; one whose sum is NaN makes the row NaN
-    auto merge = [&](int n, auto ml_of, auto o_of, float4& v, float& top, float& sum) {
-        top = -CUDART_INF_F;
-        for (int i = 0; i < n; ++i) top = fmaxf(top, ml_of(i).x);
-        v = make_float4(0.f, 0.f, 0.f, 0.f);
-        sum = 0.f;
-        for (int i = 0; i < n; ++i) {
-            const float2 ml = ml_of(i);
-            const float4 x = o_of(i);
-            const float w = part_weight(ml.x, top);
-            sum = fmaf(ml.y, w, sum);
-            v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(x.z, w, v.z); v.w = fmaf(x.w, w, v.w);
-        }
-    };
-    for (int e = tid; e < rows * (D / 4); e += kThreads) {
-        const int r = e / (D / 4), c4 = e % (D / 4);
-        float4 v;
-        float top, sum;
-        merge(kWarps, [&](int i) { return sm.ml[i][r]; }, [&](int i) { return *reinterpret_cast<const float4*>(&sm.o[i][r][c4 * 4]); }, v, top, sum);
-        if (split == 1) {
-            write(r, c4, v, top, sum);
-        } else {
-            *reinterpret_cast<float4*>(&sm.block_o[r][c4 * 4]) = v;
-            if (c4 == 0) sm.block_ml[r] = make_float2(top, sum);
-        }
+    const int seen = s.len - s.n + 1;                        // keys that the first token sees
+    float o[R][E], m[R], l[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -CUDART_INF_F;
+        l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[r][e] = 0.f;
     }
-    if (split == 1) return;
-    cluster_barrier();
-    for (int e = rank * kThreads + tid; e < rows * (D / 4); e += split * kThreads) {
-        const int r = e / (D / 4), c4 = e % (D / 4);
-        float4 v;
-        float top, sum;
-        merge(split, [&](int i) { return load_cluster2(cluster_addr(&sm.block_ml[r], i)); }, [&](int i) { return load_cluster4(cluster_addr(&sm.block_o[r][c4 * 4], i)); }, v, top, sum);
-        write(r, c4, v, top, sum);
+#pragma unroll 1
+    for (; chunk < chunks; chunk += step) {
+        if (page < 0 || page >= n_cache_pages) { if (lane == 0) set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
+        const int first = chunk * kChunkF32;
+        const int64_t row0 = (int64_t)page * a.page_size + (chunk % per_page) * kChunkF32;
+        const int there = (int)min((int64_t)(s.len - first), a.cache_rows - row0);
+        uint32_t kw[kBlocks][8], vw[kChunkF32][E];
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) load_words<8>(Kc + (row0 + lg) * row_elems + k * 32 + lq * 8, lg < there, kw[k]);
+#pragma unroll
+        for (int i = 0; i < kChunkF32; ++i) {
+            const float* at = Vc + (row0 + i) * row_elems + lane * E;
+            if constexpr (E == 4) {
+                load_words<4>(at, i < there, vw[i]);
+            } else {
+                const float2 x = i < there ? *reinterpret_cast<const float2*>(at) : make_float2(0.f, 0.f);
+                vw[i][0] = __float_as_uint(x.x);
+                vw[i][1] = __float_as_uint(x.y);
+            }
+        }
+        page = page_of(chunk + step);
+        // ---- scores of key lg, in its four lanes ----
+        float c[R];
+        bool passed = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 q = *reinterpret_cast<const float4*>(&sq[r][k * 32 + lq * 8 + h * 4]);
+                    t.x = fmaf(q.x, __uint_as_float(kw[k][h * 4]), t.x);
+                    t.y = fmaf(q.y, __uint_as_float(kw[k][h * 4 + 1]), t.y);
+                    t.x = fmaf(q.z, __uint_as_float(kw[k][h * 4 + 2]), t.x);
+                    t.y = fmaf(q.w, __uint_as_float(kw[k][h * 4 + 3]), t.y);
+                }
+            float x = t.x + t.y;
+            x += __shfl_xor_sync(kFull, x, 1);
+            x += __shfl_xor_sync(kFull, x, 2);
+            c[r] = first + lg < seen + r / P.G ? x * P.scale_log2 : -CUDART_INF_F;
+            passed |= c[r] > m[r] + kRescaleThreshold;
+        }
+        if (__any_sync(kFull, passed)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float top = c[r];
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+                top = fmaxf(top, m[r]);
+                const float factor = part_weight(m[r], top);
+                m[r] = top;
+                l[r] *= factor;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[r][e] *= factor;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            c[r] = ex2(c[r] - (m[r] == -CUDART_INF_F ? 0.f : m[r]));
+            l[r] += c[r];
+        }
+#pragma unroll
+        for (int i = 0; i < kChunkF32; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float p = __shfl_sync(kFull, c[r], 4 * i);
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[r][e] = fmaf(p, __uint_as_float(vw[i][e]), o[r][e]);
+            }
     }
-    cluster_barrier();                                       // nobody leaves while its shared memory is read
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(kFull, l[r], d);      // (four lanes have a key's)
+        if (lane == 0) sm.ml[warp][r] = make_float2(m[r], l[r]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sm.o[warp][r][lane * E + e] = o[r][e];
+    }
+    merge_parts<float>(sm, P, s, g, rows, rank, split);
 }
 
 struct RowsLaunch {
@@ -286,17 +425,23 @@ struct RowsLaunch {
 // one, 32 / 8 heads of 128: B = 1, 1024 tokens 6.3 / 12.5, 4096 (2 chunks a warp) 11.3 / 16.0, 16384 (8) 25.8 / 24.4, 65536 (32) 76 / 54; B = 2, 4096
 // (4) 15.4 / 18.0, 16384 (16) 41 / 34; B = 8, 4096 (8) 27.8 / 32.8; filled: B = 32, 1024 (8) 27 / 36, 4096 (32) 88 / 93; B = 128, 1024 (8) 98 / 102, 4096
 // (32) 344 / 327; 16 / 1 heads: B = 1, 16384 (8) 16.6 / 27.3; B = 8, 16384 (16) 32 / 25; B = 64, 4096 (16, filled) 32 / 35.
-template <int D, int NT>
+// fp32 against the form of whole tiles: this one but for a few units over very many keys, which that one spreads over the machine.  32 / 8 heads: B =
+// 1, 1024 tokens 10.7 / 29.3, 65536 270 / 559; B = 32, 4096 269 / 1107; 16 / 1 heads: B = 1, 16384 (16 chunks a warp, 16 blocks) 68 / 69, 65536 253 / 137; B = 4,
+// 65536 (64 blocks) 255 / 301.
+template <typename T, int D, int R>
 int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool& taken) {
-    auto* const kernel = chunk_attn_rows_kernel<D, NT>;
-    const size_t smem = sizeof(RowsSmem<D, NT>);
-    const int variant = 2 * (D == 128) + NT - 1;
+    void (*kernel)(ChunkParams, int);
+    if constexpr (sizeof(T) == 2) kernel = chunk_attn_rows_kernel<D, R / 8>;
+    else kernel = chunk_attn_rows_f32_kernel<D, R>;
+    constexpr int kKeys = sizeof(T) == 2 ? kChunk : kChunkF32;
+    const size_t smem = sizeof(RowsSmem<D, R>);
+    const int variant = 4 * (sizeof(T) == 4) + 2 * (D == 128) + R / 8 - 1;
     const bool first = ctx->smem_room[RADAR_SMEM_CHUNK_ROWS + variant] == 0;
     RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CHUNK_ROWS + variant, kernel, smem));
     if (first) RADAR_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     const long long units = (long long)P.a.B * P.a.Hkv;
     int split = 1;
-    for (int i = 0; 2 * split <= kMostSplit && (long long)split * kWarps * kChunk < P.a.max_cache_len; ++i) {
+    for (int i = 0; 2 * split <= kMostSplit && (long long)split * kWarps * kKeys < P.a.max_cache_len; ++i) {
         int& clusters = ctx->chunk_clusters[variant][i];     // of 2 * split blocks
         if (clusters == 0) {
             RowsLaunch l(1, 2 * split, smem, stream);
@@ -306,8 +451,9 @@ int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool&
         if (units > clusters) break;
         split *= 2;
     }
-    const bool filled = units * split * 5 >= 4ll * ctx->sm_count * (NT == 1 ? 2 : 1);
-    taken = P.a.max_cache_len <= (filled ? 24ll : 8ll) * split * kWarps * kChunk;
+    const bool filled = units * split * 5 >= 4ll * ctx->sm_count * (R == 8 ? 2 : 1);
+    if (sizeof(T) == 2) taken = P.a.max_cache_len <= (filled ? 24ll : 8ll) * split * kWarps * kKeys;
+    else taken = units * split * 4 >= ctx->sm_count || P.a.max_cache_len <= 16ll * split * kWarps * kKeys;
     if (!taken) return RADAR_OK;
     RowsLaunch l(units, split, smem, stream);
     radar_launch_scope scope(ctx, RADAR_K_CHUNK_ATTN, stream);
@@ -323,8 +469,15 @@ int chunk_rows_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream
     taken = false;
     if (rows > 16 || (long long)a->B * a->Hkv > INT32_MAX / kMostSplit || ((reinterpret_cast<uintptr_t>(a->Kc) | reinterpret_cast<uintptr_t>(a->Vc)) & 31) != 0) return RADAR_OK;
     const ChunkParams P = chunk_params(ctx, *a, G, 128, 1);
-    if (a->d == 128) return rows > 8 ? launch_rows<128, 2>(ctx, P, stream, taken) : launch_rows<128, 1>(ctx, P, stream, taken);
-    return rows > 8 ? launch_rows<64, 2>(ctx, P, stream, taken) : launch_rows<64, 1>(ctx, P, stream, taken);
+    auto go = [&](auto t, auto d) {
+        using T = decltype(t);
+        constexpr int D = decltype(d)::value;
+        return rows > 8 ? launch_rows<T, D, 16>(ctx, P, stream, taken) : launch_rows<T, D, 8>(ctx, P, stream, taken);
+    };
+    using d64 = std::integral_constant<int, 64>;
+    using d128 = std::integral_constant<int, 128>;
+    if (a->dtype == RADAR_F32) return a->d == 128 ? go(0.f, d128{}) : go(0.f, d64{});
+    return a->d == 128 ? go(__nv_bfloat16{}, d128{}) : go(__nv_bfloat16{}, d64{});
 }
 
 }  // namespace radar

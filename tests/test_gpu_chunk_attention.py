@@ -182,3 +182,14 @@ def test_bad_pages_and_requests(ctx, dtype):
         assert ctx.read_device_status() == -1
         T.hold_again(kw, [0, 1])
         assert torch.all(kw["O"][start[2]:] == 5.0)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 1), (4, 2), (9, 1), (16, 1), (17, 1), (6, 6)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_rows_f32(ctx, Hq, Hkv, d):
+    import paged_harness as T
+    T.check_chunk(ctx, _rng(Hq, d), [1] * 8, [1, 7, 8, 9, 63, 64, 65, 250], Hq, Hkv, d, 16, "f32")
+    T.check_chunk(ctx, _rng(Hq, d, 1), [2, 1, 0, 2], [2, 1, 5, 640], Hq, Hkv, d, 32, "f32")
+    for n in (300, 1023, 1024, 1025, 5000, 17000):
+        T.check_chunk(ctx, _rng(Hq, n), [1], [n], Hq, Hkv, d, 64, "f32")
+    T.check_chunk(ctx, _rng(Hq, d, 2), [2, 1], [0, 0], Hq, Hkv, d, 16, "f32", max_len=400)
