@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) chunk_attn_rows_ker
 constexpr int kChunkF32 = 8;             // keys of a chunk
 
 template <int D, int R>
-__global__ void __launch_bounds__(kThreads, R == 8 ? 2 : 1) chunk_attn_rows_f32_kernel(const ChunkParams P, const int split) {
+__global__ void __launch_bounds__(kThreads, R <= 8 ? 2 : 1) chunk_attn_rows_f32_kernel(const ChunkParams P, const int split) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     using Smem = RowsSmem<D, R>;
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
@@ -431,11 +431,11 @@ struct RowsLaunch {
 template <typename T, int D, int R>
 int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool& taken) {
     void (*kernel)(ChunkParams, int);
-    if constexpr (sizeof(T) == 2) kernel = chunk_attn_rows_kernel<D, R / 8>;
+    if constexpr (sizeof(T) == 2) kernel = chunk_attn_rows_kernel<D, (R + 7) / 8>;
     else kernel = chunk_attn_rows_f32_kernel<D, R>;
     constexpr int kKeys = sizeof(T) == 2 ? kChunk : kChunkF32;
     const size_t smem = sizeof(RowsSmem<D, R>);
-    const int variant = 4 * (sizeof(T) == 4) + 2 * (D == 128) + R / 8 - 1;
+    constexpr int variant = sizeof(T) == 2 ? 2 * (D == 128) + R / 8 - 1 : 4 + 3 * (D == 128) + (R == 4 ? 0 : R / 8);
     const bool first = ctx->smem_room[RADAR_SMEM_CHUNK_ROWS + variant] == 0;
     RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CHUNK_ROWS + variant, kernel, smem));
     if (first) RADAR_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
@@ -451,7 +451,7 @@ int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool&
         if (units > clusters) break;
         split *= 2;
     }
-    const bool filled = units * split * 5 >= 4ll * ctx->sm_count * (R == 8 ? 2 : 1);
+    const bool filled = units * split * 5 >= 4ll * ctx->sm_count * (R <= 8 ? 2 : 1);
     if (sizeof(T) == 2) taken = P.a.max_cache_len <= (filled ? 24ll : 8ll) * split * kWarps * kKeys;
     else taken = units * split * 4 >= ctx->sm_count || P.a.max_cache_len <= 16ll * split * kWarps * kKeys;
     if (!taken) return RADAR_OK;
@@ -472,6 +472,8 @@ int chunk_rows_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream
     auto go = [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
+        if constexpr (sizeof(T) == 4)
+            if (rows <= 4) return launch_rows<T, D, 4>(ctx, P, stream, taken);
         return rows > 8 ? launch_rows<T, D, 16>(ctx, P, stream, taken) : launch_rows<T, D, 8>(ctx, P, stream, taken);
     };
     using d64 = std::integral_constant<int, 64>;

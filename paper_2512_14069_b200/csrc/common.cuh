@@ -58,8 +58,8 @@ enum radar_smem_slot {
     RADAR_SMEM_CACHE_SMALL = RADAR_SMEM_CACHE_ATTN_TC + 4,    // + 2 * (d == 128) + row tiles of eight - 1
     RADAR_SMEM_CHUNK_TC = RADAR_SMEM_CACHE_SMALL + 4,         // + (d == 128)
     RADAR_SMEM_CHUNK_FMA = RADAR_SMEM_CHUNK_TC + 2,           // + (d == 128)
-    RADAR_SMEM_CHUNK_ROWS = RADAR_SMEM_CHUNK_FMA + 2,         // + 4 * (fp32) + 2 * (d == 128) + row tiles of eight - 1
-    RADAR_SMEM_COUNT = RADAR_SMEM_CHUNK_ROWS + 8
+    RADAR_SMEM_CHUNK_ROWS = RADAR_SMEM_CHUNK_FMA + 2,         // + its variant
+    RADAR_SMEM_COUNT = RADAR_SMEM_CHUNK_ROWS + 10
 };
 
 struct radar_ctx {
@@ -70,7 +70,7 @@ struct radar_ctx {
     size_t smem_room[RADAR_SMEM_COUNT];
     int* d_status;          // sticky device status word
     int acclen_clusters[4][4];   // clusters of 1, 2, 4, 8 of each per-row kernel of Eq. 11-13 that are resident at once (0: not asked yet)
-    int chunk_clusters[8][4];    // ... of 2, 4, 8, 16 of each kernel of the chunk attention of few rows
+    int chunk_clusters[10][4];    // ... of 2, 4, 8, 16 of each kernel of the chunk attention of few rows
     // launch accounting (host side)
     long long launches[RADAR_K_COUNT];
     // optional per-kernel CUDA-event timing
