@@ -193,3 +193,58 @@ def test_few_rows_f32(ctx, Hq, Hkv, d):
     for n in (300, 1023, 1024, 1025, 5000, 17000):
         T.check_chunk(ctx, _rng(Hq, n), [1], [n], Hq, Hkv, d, 64, "f32")
     T.check_chunk(ctx, _rng(Hq, d, 2), [2, 1], [0, 0], Hq, Hkv, d, 16, "f32", max_len=400)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 384])
+def test_few_rows_in_pages_of_all_sizes_from_a_fused_projection(ctx, page, dtype):
+    import paged_harness as T
+    T.check_chunk(ctx, _rng(page), [1, 2, 0, 1], [500, 385, 7, 900], 8, 2, 128, page, dtype, fused=True, lead=2, tail=3, rows_behind=2)
+
+
+def test_more_requests_than_a_warp_has_lanes(ctx):
+    """Ranges over 70 requests of 5 and more rows, some of them empty, in one launch of the tensor cores' form."""
+    import paged_harness as T
+    news = [0 if i % 9 == 4 else 5 + i % 7 for i in range(70)]
+    T.check_chunk(ctx, _rng(3), news, [n + (37 * i) % 600 for i, n in enumerate(news)], 4, 1, 128, 32)
+    T.check_chunk(ctx, _rng(4), [0] * 33 + [140] + [0] * 40, [50] * 33 + [1400] + [3] * 40, 4, 2, 64, 16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1], [40, 7]])
+def test_the_first_call_of_a_context_may_be_captured(dtype, news):
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    c = rb.Context(0)
+    kw = T.check_chunk(c, _rng(5), news, [300, 100], 4, 2, 64, 16, dtype)
+    c.close()
+    want, c = kw["O"].clone(), rb.Context(0)
+    kw["O"].fill_(5.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rb.radar_chunk_attention(c, **kw)
+    assert torch.all(kw["O"] == 5.0)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(kw["O"], want) and c.read_device_status() == 0
+    del graph
+    c.close()
+
+
+def test_two_calls_at_once(ctx):
+    """On two streams, with a workspace each: what either gives alone."""
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    calls = [T.check_chunk(ctx, _rng(i), news, lens, 8, 2, 128, 64) for i, (news, lens) in enumerate([([300, 40], [4000, 900]), ([130, 1, 60], [2000, 3000, 60])])]
+    want = [(k["O"].clone(), k["lse"].clone()) for k in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for k, s in zip(calls, streams):
+            rb.radar_chunk_attention(ctx, stream=s, **k)
+    torch.cuda.synchronize()
+    for k, w in zip(calls, want):
+        assert torch.equal(k["O"], w[0]) and torch.equal(k["lse"], w[1])
+    assert ctx.read_device_status() == 0

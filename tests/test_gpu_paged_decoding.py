@@ -244,3 +244,15 @@ def test_refusals(ctx):
         with pytest.raises(rb.RadarError):
             rb.radar_chunk_attention(ctx, **dict(attend, **change))
     assert ctx.read_device_status() == 0
+
+
+def test_a_chunk_of_nothing(ctx):
+    import torch
+    c = _cache(ctx, B=2, n_layers=1)
+    c.begin(torch.tensor([0, 0], dtype=torch.int32, device="cuda"), 0, requests=torch.tensor([0, 1], device="cuda"))
+    z = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros(0, 6, 64, dtype=torch.bfloat16, device="cuda")
+    c.store(0, z, z, Q=q, Q_out=q, inv_freq=torch.ones(32, device="cuda"))
+    c.attention(0, q, q)
+    ctx.check_device_status()
+    assert c.cache_len.tolist() == [0, 0] and c.live.tolist() == [False, True]
