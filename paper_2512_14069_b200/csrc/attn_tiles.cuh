@@ -47,27 +47,6 @@ __device__ __forceinline__ float2 add2_in_order(float2 a, float2 b) {
                  : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-__device__ __forceinline__ float add_in_order(float a, float b) {
-    float d;
-    asm volatile("add.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ float sub_in_order(float a, float b) {
-    float d;
-    asm volatile("sub.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ float fma_in_order(float a, float b, float c) {
-    float d;
-    asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-// the larger one, or NaN if one is
-__device__ __forceinline__ float max_nan_in_order(float a, float b) {
-    float d;
-    asm volatile("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
 __device__ __forceinline__ uint32_t bf16x2_in_order(float lo, float hi) {
     uint32_t d;
     asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));

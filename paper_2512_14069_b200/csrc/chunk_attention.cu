@@ -1,12 +1,13 @@
 // radar_chunk_attention: the entry point, and the form for fp32 rows, on the FMA units.
 //
-// Scores s = scale q.k of the keys a row sees, online softmax over tiles of 64 keys: m = running maximum, l = sum exp(s - m),
-// O = sum exp(s - m) v, rescaled when m moves; everything in fp32.
+// Scores s = scale q.k of the keys a row sees, online softmax over tiles of 64 keys: m = a row's maximum so far, moved (and l = sum exp(s - m),
+// O = sum exp(s - m) v with it) only where a score passes it by 2^8; everything in fp32.
 //
 // A head group is a KV head's G query heads (one query head where G is above 64, so that a unit holds a whole token), a unit 64 rows.  A block of
-// 128 threads has Q (64 rows), K and V (64 keys each) and P in shared memory; a thread holds 8 rows x 4 keys of the scores, then 8 rows x
-// d / 16 channels of O, and reads 12 (16) bytes from shared memory for every 32 FMAs.  What bounds it: shared-memory reads
-// and FMAs, about alike.
+// 128 threads, two to an SM, has Q (64 rows), K and V (64 keys each) and P in shared memory; a thread holds 8 rows x 4 keys of the scores, then 8
+// rows x d / 16 channels of O, in pairs of rows that one instruction multiplies by a value.  (The scores in pairs of channels were slower, as was O one
+// by one: 2048 tokens over 2048 cached ones, 32 / 8 heads of 128: 885 us, 924 with O one by one, 1191 with one block an SM, a row of padding in P and
+// every tile rescaled.)  What bounds it: the issue of FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
 #include <algorithm>
 #include <climits>
 
@@ -16,18 +17,41 @@
 namespace radar {
 namespace {
 
-constexpr int kFmaThreads = 128, kFmaRows = 64, kFmaKeys = 64, kPStride = kFmaRows + 4;
+constexpr int kFmaThreads = 128, kFmaRows = 64, kFmaKeys = 64, kPStride = 4 * kFmaRows + 4;
 
 struct FmaCosts {
-    static constexpr int kTile = kFmaKeys, kOne = 1, kTwo = 1, kUnit = 2 * kFmaKeys;
+    static constexpr int kTile = kFmaKeys, kOne = 1, kTwo = 1, kUnit = kFmaKeys;
 };
 
 template <int D>
 struct FmaSmem {
-    float q[kFmaRows * D], k[kFmaKeys * D], v[kFmaKeys * D], p[kFmaKeys * kPStride];
-    long long at[2][kFmaKeys];           // cache rows of a tile's keys; below 0: there is none
+    float q[kFmaRows * D], k[kFmaKeys * D], v[kFmaKeys * D];
+    float p[16 * kPStride];              // [key % 16][key / 16][row]: writes of neighbouring keys meet in no bank, and two blocks fit an SM
+    int at[2][kFmaKeys];                 // cache rows of a tile's keys; below 0: there is none
 };
 
+// two fp32 numbers in a register pair, and the arithmetic on both at once
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two_of(float x, float y) {
+    Two t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t) : "f"(x), "f"(y));
+    return t;
+}
+__device__ __forceinline__ float2 both(Two t) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(t));
+    return v;
+}
+__device__ __forceinline__ Two fma_two(Two a, Two b, Two c) {
+    Two d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Two mul_two(Two a, Two b) {
+    Two d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ void copy16(float* to, const float* from, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
@@ -62,12 +86,12 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
         auto look_up = [&](int t, int buffer) {
             if (tid < kFmaKeys) {
                 const int j = t * kFmaKeys + tid;
-                long long at = -1;
+                int at = -1;
                 if (j < keys) {
                     int page = a.block_table[(int64_t)b * a.max_pages + j / a.page_size];
                     if (page < 0 || page >= n_cache_pages) { set_status(P.status, RADAR_ERR_INVALID_ARG); page = 0; }
-                    at = (int64_t)page * a.page_size + j % a.page_size;
-                    if (at >= a.cache_rows) at = -1;         // (a cache of less than one page)
+                    const int64_t row = (int64_t)page * a.page_size + j % a.page_size;
+                    if (row < a.cache_rows) at = (int)row;   // (a cache of less than one page; cache_rows: below 2^31)
                 }
                 sm.at[buffer][tid] = at;
             }
@@ -77,8 +101,8 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
 #pragma unroll 4
             for (int i = tid; i < kFmaKeys * kVec; i += kFmaThreads) {
                 const int r = i / kVec, c = i % kVec;
-                const long long at = sm.at[buffer][r];
-                copy16(to + r * D + (exchange ? c ^ (r & 7) : c) * 4, reinterpret_cast<const float*>(base) + max(at, 0ll) * row_elems + (int64_t)kv_head * D + c * 4, at >= 0);
+                const int at = sm.at[buffer][r];
+                copy16(to + r * D + (exchange ? c ^ (r & 7) : c) * 4, reinterpret_cast<const float*>(base) + max(at, 0) * row_elems + (int64_t)kv_head * D + c * 4, at >= 0);
             }
             copies_end();
         };
@@ -93,16 +117,19 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
         __syncthreads();
         fetch(a.Kc, sm.k, 0, true);
         fetch(a.Vc, sm.v, 0, false);
-        float o[8][4 * kCols], m[8], l[8];
+        Two o[4][4 * kCols];                                 // of rows 2 i and 2 i + 1
+        float m[8], l[8];
         int lim[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             m[i] = -CUDART_INF_F;
             l[i] = 0.f;
             lim[i] = u.seen + (int)(((uint32_t)(ty * 8 + i) * P.g_magic) >> 16);
-#pragma unroll
-            for (int e = 0; e < 4 * kCols; ++e) o[i][e] = 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4 * kCols; ++e) o[i][e] = 0;
 #pragma unroll 1
         for (int t = t0; t < t0 + n; ++t) {
             const bool more = t + 1 < t0 + n;
@@ -110,11 +137,11 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             copies_wait<1>();
             __syncthreads();
             // ---- 8 rows x 4 keys of S: the keys tx, tx + 16, .. ----
-            float s[8][4];
+            float part[8][4];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+                for (int j = 0; j < 4; ++j) part[i][j] = 0.f;
 #pragma unroll 2
             for (int c = 0; c < kVec; ++c) {
                 float4 k4[4];
@@ -124,37 +151,51 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
                 for (int i = 0; i < 8; ++i) {
                     const float4 q4 = *reinterpret_cast<const float4*>(sm.q + (ty * 8 + i) * D + (c ^ ty) * 4);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[i][j] = fmaf(q4.x, k4[j].x, fmaf(q4.y, k4[j].y, fmaf(q4.z, k4[j].z, fmaf(q4.w, k4[j].w, s[i][j]))));
+                    for (int j = 0; j < 4; ++j) part[i][j] = fmaf(q4.x, k4[j].x, fmaf(q4.y, k4[j].y, fmaf(q4.z, k4[j].z, fmaf(q4.w, k4[j].w, part[i][j]))));
                 }
             }
             __syncthreads();
             if (more) fetch(a.Kc, sm.k, (t + 1 - t0) & 1, true);
             else copies_end();
             // ---- softmax ----
+            float s[8][4];
+            bool passed = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float mx = -CUDART_INF_F;
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? s[i][j] * P.scale_log2 : -CUDART_INF_F;
-                    mx = fmaxf(mx, s[i][j]);
+                    s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? part[i][j] * P.scale_log2 : -CUDART_INF_F;
+                    passed |= s[i][j] > m[i] + kRescaleThreshold;
+                }
+            if (__any_sync(kFull, passed)) {
+                float factor[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+#pragma unroll
+                    for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+                    top = fmaxf(top, m[i]);
+                    factor[i] = ex2(m[i] - (top == -CUDART_INF_F ? 0.f : top));
+                    m[i] = top;
+                    l[i] *= factor[i];
                 }
 #pragma unroll
-                for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, d));
-                const float top = fmaxf(m[i], mx), use = top == -CUDART_INF_F ? 0.f : top, factor = ex2(m[i] - use);
-                m[i] = top;
-                l[i] *= factor;
+                for (int i = 0; i < 4; ++i) {
+                    const Two f = two_of(factor[2 * i], factor[2 * i + 1]);
+#pragma unroll
+                    for (int e = 0; e < 4 * kCols; ++e) o[i][e] = mul_two(o[i][e], f);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[i][j] = ex2(s[i][j] - use);
+                    s[i][j] = ex2(s[i][j] - (m[i] == -CUDART_INF_F ? 0.f : m[i]));
                     l[i] += s[i][j];
                 }
 #pragma unroll
-                for (int e = 0; e < 4 * kCols; ++e) o[i][e] *= factor;
-            }
-#pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float* to = sm.p + (tx + 16 * j) * kPStride + ty * 8;
+                float* to = sm.p + tx * kPStride + j * kFmaRows + ty * 8;
                 *reinterpret_cast<float4*>(to) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
                 *reinterpret_cast<float4*>(to + 4) = make_float4(s[4][j], s[5][j], s[6][j], s[7][j]);
             }
@@ -162,21 +203,22 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             __syncthreads();
             // ---- O += P V ----
 #pragma unroll 4
-            for (int k = 0; k < kFmaKeys; ++k) {
-                const float4 p0 = *reinterpret_cast<const float4*>(sm.p + k * kPStride + ty * 8), p1 = *reinterpret_cast<const float4*>(sm.p + k * kPStride + ty * 8 + 4);
-                const float p[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+            for (int h = 0; h < 16; ++h)
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    const float4 v4 = *reinterpret_cast<const float4*>(sm.v + k * D + c * 64 + tx * 4);
+                for (int j = 0; j < 4; ++j) {
+                    const float* at = sm.p + h * kPStride + j * kFmaRows + ty * 8;
+                    const ulonglong2 p0 = *reinterpret_cast<const ulonglong2*>(at), p1 = *reinterpret_cast<const ulonglong2*>(at + 4);
+                    const Two p[4] = {p0.x, p0.y, p1.x, p1.y};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        o[i][4 * c] = fmaf(p[i], v4.x, o[i][4 * c]);
-                        o[i][4 * c + 1] = fmaf(p[i], v4.y, o[i][4 * c + 1]);
-                        o[i][4 * c + 2] = fmaf(p[i], v4.z, o[i][4 * c + 2]);
-                        o[i][4 * c + 3] = fmaf(p[i], v4.w, o[i][4 * c + 3]);
+                    for (int c = 0; c < kCols; ++c) {
+                        const float4 v4 = *reinterpret_cast<const float4*>(sm.v + (h + 16 * j) * D + c * 64 + tx * 4);
+                        const Two v[4] = {two_of(v4.x, v4.x), two_of(v4.y, v4.y), two_of(v4.z, v4.z), two_of(v4.w, v4.w)};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[i][4 * c + e] = fma_two(p[i], v[e], o[i][4 * c + e]);
                     }
                 }
-            }
             __syncthreads();
             if (more) fetch(a.Vc, sm.v, (t + 1 - t0) & 1, false);
             else copies_end();
@@ -196,8 +238,12 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             const float inv = !final_rows ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
             float* to = final_rows ? reinterpret_cast<float*>(a.O) + out_row * D : P.part_o + rec * D;
 #pragma unroll
-            for (int c = 0; c < kCols; ++c)
-                *reinterpret_cast<float4*>(to + c * 64 + tx * 4) = make_float4(o[i][4 * c] * inv, o[i][4 * c + 1] * inv, o[i][4 * c + 2] * inv, o[i][4 * c + 3] * inv);
+            for (int c = 0; c < kCols; ++c) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (i & 1 ? both(o[i >> 1][4 * c + e]).y : both(o[i >> 1][4 * c + e]).x) * inv;
+                *reinterpret_cast<float4*>(to + c * 64 + tx * 4) = make_float4(x[0], x[1], x[2], x[3]);
+            }
             if (tx == 0) {
                 if (!final_rows) P.part_ml[rec] = make_float2(l[i] == 0.f ? -CUDART_INF_F : m[i], l[i]);
                 else if (a.lse != nullptr) a.lse[out_row] = l[i] == 0.f ? -CUDART_INF_F : lse_of(m[i], l[i]);

@@ -11,7 +11,7 @@
 namespace radar {
 namespace {
 
-constexpr int kMaxCtas = 640;        // of a launch
+constexpr int kMaxCtas = 320;        // of a launch
 
 // The first piece of a unit that continues in the following CTAs, written by the CTA that has it, read by the combine kernel.
 struct __align__(16) ChunkCut {

@@ -504,7 +504,9 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             // =================================== MMA issuer ===================================
             // Every lane waits on the barriers (and helps to clear what lies behind the last key), one issues the products and the commits.  No
             // control flow depends on a wait's outcome but that: after a wait that ran out nothing is issued and the loops run dry.
-            // Some eight products queue up in front of the tensor cores, so that they have work while this warp is in a wait.
+            // The vote on the waits comes first, and the branch of the one lane inside its branch: a product then takes 20 to 30 cycles to
+            // issue, and 66 where one branch asks for both.  Some eight products queue up in front of the tensor cores, so that they have work
+            // while this warp is in a wait.
             constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTileKeys, false, false);
             constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, false, true);
             // descriptors: stride between 8-row groups 1024 B, version, swizzle; in units of 16 bytes
@@ -582,10 +584,11 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     tc_fence_after_sync();
                     if (__all_sync(kFull, ok)) {
                         if (leader) {
-                        issue_pv(q, 0, ksteps, !acc[q]);
-                        if (release_v) mma_commit(&st.bar_vempty[v_slot]);
-                        if (two ? i == n - 1 : i + 2 >= n) mma_commit(&st.bar_odone[q]);
-                    } }
+                            issue_pv(q, 0, ksteps, !acc[q]);
+                            if (release_v) mma_commit(&st.bar_vempty[v_slot]);
+                            if (two ? i == n - 1 : i + 2 >= n) mma_commit(&st.bar_odone[q]);
+                        }
+                    }
                     __syncwarp();
                     acc[q] = true;
                 };
@@ -597,12 +600,13 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                     if (__all_sync(kFull, ok)) {
                         if (leader) {
-                        issue_s(q, two ? q : 0);
-                        if (release_k) mma_commit(&st.bar_kempty[k_slot]);
-                        mma_commit(&st.bar_sfull[q]);
-                        // the last S of the segment: Q may be overwritten once it has run
-                        if (si == n - 1 && release_k) mma_commit(&st.bar_qempty);
-                    } }
+                            issue_s(q, two ? q : 0);
+                            if (release_k) mma_commit(&st.bar_kempty[k_slot]);
+                            mma_commit(&st.bar_sfull[q]);
+                            // the last S of the segment: Q may be overwritten once it has run
+                            if (si == n - 1 && release_k) mma_commit(&st.bar_qempty);
+                        }
+                    }
                     __syncwarp();
                 };
                 // Schedule.  Two live row blocks: group s owns row block s; per tile PV0(i) S0(i+1) PV1(i) S1(i+1),
