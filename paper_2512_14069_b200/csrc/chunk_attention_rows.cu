@@ -425,9 +425,11 @@ struct RowsLaunch {
 // one, 32 / 8 heads of 128: B = 1, 1024 tokens 6.3 / 12.5, 4096 (2 chunks a warp) 11.3 / 16.0, 16384 (8) 25.8 / 24.4, 65536 (32) 76 / 54; B = 2, 4096
 // (4) 15.4 / 18.0, 16384 (16) 41 / 34; B = 8, 4096 (8) 27.8 / 32.8; filled: B = 32, 1024 (8) 27 / 36, 4096 (32) 88 / 93; B = 128, 1024 (8) 98 / 102, 4096
 // (32) 344 / 327; 16 / 1 heads: B = 1, 16384 (8) 16.6 / 27.3; B = 8, 16384 (16) 32 / 25; B = 64, 4096 (16, filled) 32 / 35.
-// fp32 against the form of whole tiles: this one but for a few units over very many keys, which that one spreads over the machine.  32 / 8 heads: B =
-// 1, 1024 tokens 10.7 / 29.3, 65536 270 / 559; B = 32, 4096 269 / 1107; 16 / 1 heads: B = 1, 16384 (16 chunks a warp, 16 blocks) 68 / 69, 65536 253 / 137; B = 4,
-// 65536 (64 blocks) 255 / 301.
+// fp32 against the form of whole tiles: up to 8 rows this one, but for a few units over very many keys, which that one spreads over the machine: 32 / 8
+// heads of 128 (4 rows): B = 1, 1024 tokens 8.3 / 24.3, 65536 174 / 427; B = 32, 4096 183 / 831; 8 / 1 heads of 64: B = 1, 16384 (16 chunks a warp,
+// 16 blocks) 30 / 58, 65536 113 / 84; B = 4, 65536 (64 blocks) 115 / 128.  16 rows, one block an SM: this one up to 8 chunks a warp or where the blocks fill
+// the machine: 16 / 1 heads of 128: B = 1, 4096 (4) 25 / 35, 16384 (16) 70 / 67; B = 4, 16384 (8) 71 / 81, 65536 (32) 255 / 228; B = 16, 16384 (64)
+// 252 / 219; B = 32, 16384 (64, filled) 254 / 423.
 template <typename T, int D, int R>
 int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool& taken) {
     void (*kernel)(ChunkParams, int);
@@ -453,7 +455,7 @@ int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool&
     }
     const bool filled = units * split * 5 >= 4ll * ctx->sm_count * (R <= 8 ? 2 : 1);
     if (sizeof(T) == 2) taken = P.a.max_cache_len <= (filled ? 24ll : 8ll) * split * kWarps * kKeys;
-    else taken = units * split * 4 >= ctx->sm_count || P.a.max_cache_len <= 16ll * split * kWarps * kKeys;
+    else taken = (R <= 8 ? units * split * 4 >= ctx->sm_count : filled) || P.a.max_cache_len <= (R <= 8 ? 16ll : 8ll) * split * kWarps * kKeys;
     if (!taken) return RADAR_OK;
     RowsLaunch l(units, split, smem, stream);
     radar_launch_scope scope(ctx, RADAR_K_CHUNK_ATTN, stream);
