@@ -569,8 +569,8 @@ typedef struct {
  * is the gradient of the rotation (its transpose) and takes rows back to where they were.  Row i of Q: Hq heads of d channels at
  * i * q_row_stride (elements; parts of a fused projection are read in place).  An output may be its own input (same address and
  * stride); otherwise it must not overlap one.
- * Limits: 1 <= d <= 1024, 1 <= n_pairs <= d / 2, n_rows < 2^31.  Rows of any alignment are taken; 16 bytes at a time where all addresses and
- * strides are multiples of 16 bytes and d and n_pairs of 16 bytes' elements, one element at a time elsewhere. */
+ * Limits: 1 <= d <= 1024, 1 <= n_pairs <= d / 2, n_rows < 2^31.  Rows of any alignment are taken; 32, 16 or 8 bytes at a time where all
+ * addresses, strides, d and n_pairs (times the element size) are multiples of that, one element at a time elsewhere. */
 typedef struct {
     int Hq, Hkv, d;
     int dtype;                          /* RADAR_F32 or RADAR_BF16 */
@@ -622,7 +622,9 @@ int radar_paged_store(radar_ctx* ctx, const radar_paged_store_args* args, void* 
  * as page 0.  Requests must not share rows.  scale <= 0 selects 1/sqrt(d).
  * Values of the tokens that any row of a request sees have to be finite (a probability of 0 times infinity or NaN is NaN); keys that a row does
  * not attend to may hold anything, and so may the cache behind a request's last token.
- * RADAR_BF16: products on the tensor cores, probabilities enter P V as bf16, sums in fp32.  RADAR_F32: fp32 throughout.
+ * RADAR_BF16: products on the tensor cores, probabilities enter P V as bf16, sums in fp32.  RADAR_F32: fp32 throughout.  Calls of up to 16
+ * rows to a KV head and request (max_new * Hq / Hkv) take a form of one launch while there is little to read; the others are an attention and a
+ * merge kernel.  Which one it is goes by the bounds and B, so the order of a row's sums does too; equal calls give equal bits.
  * Limits: d in {64, 128}; Hq a multiple of Hkv, at most 128 query heads to a KV head; B <= 65535; n_rows, cache_rows < 2^31; max_cache_len at most 2^31 -
  * 2^14 - 1.  Q, Kc, Vc and O: 16 bytes, as are the row stride times the element size; the workspace: 256.  The workspace's size is enough for fewer requests, shorter ones
  * and fewer rows; calls that may overlap need one each. */

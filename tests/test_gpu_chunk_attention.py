@@ -248,3 +248,49 @@ def test_two_calls_at_once(ctx):
     for k, w in zip(calls, want):
         assert torch.equal(k["O"], w[0]) and torch.equal(k["lse"], w[1])
     assert ctx.read_device_status() == 0
+
+
+@pytest.mark.parametrize("news,dtype", [([1, 1], "bf16"), ([40, 7], "bf16"), ([1, 1], "f32"), ([40, 7], "f32")])
+def test_a_cache_beyond_32_bits(ctx, news, dtype):
+    """Pages at the end of a pool of more than 2^31 elements give what the same pages give at the start of a small one."""
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    Hkv, d, page = 16, 128, 64
+    kw = T.check_chunk(ctx, _rng(8), news, [300, 1000], 32, Hkv, d, page, dtype)
+    want, lse = kw["O"].clone(), kw["lse"].clone()
+    small = kw["Kc"].shape[0]
+    rows = 2 ** 31 // (Hkv * d) + small
+    rows -= rows % page
+    for name in ("Kc", "Vc"):
+        big = torch.empty(rows, Hkv, d, dtype=T.DT[dtype], device="cuda")
+        big[rows - small:] = kw[name]
+        kw[name] = big
+    table = kw["block_table"]
+    kw["block_table"] = torch.where(table >= 0, table + (rows - small) // page, table)
+    kw["O"].fill_(7.0)
+    rb.radar_chunk_attention(ctx, **kw)
+    torch.cuda.synchronize()
+    ctx.check_device_status()
+    assert torch.equal(kw["O"], want) and torch.equal(kw["lse"], lse)
+
+
+def test_pools_at_addresses_of_16_bytes(ctx):
+    """Single tokens over pools that 32-byte reads cannot take."""
+    import paged_harness as T
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    for dtype in ("bf16", "f32"):
+        kw = T.check_chunk(ctx, _rng(9), [1, 1, 0], [300, 70, 5], 8, 2, 64, 16, dtype)
+        for name in ("Kc", "Vc"):
+            room = torch.empty(kw[name].numel() + 16, dtype=T.DT[dtype], device="cuda")
+            at = 16 // room.element_size()
+            moved = room[at:at + kw[name].numel()].view_as(kw[name])
+            assert moved.data_ptr() % 32 == 16
+            moved.copy_(kw[name])
+            kw[name] = moved
+        kw["O"].fill_(7.0)
+        rb.radar_chunk_attention(ctx, **kw)
+        torch.cuda.synchronize()
+        ctx.check_device_status()
+        T.hold_again(kw, range(3))

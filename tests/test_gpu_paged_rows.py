@@ -214,3 +214,22 @@ def test_store_queries_in_place(ctx):
     H.hold_turned(g[:, :4].double().cpu().numpy(), want[:, :4], size[:, :4], "bf16", 64)
     H.hold_turned(Kc.double().cpu().numpy(), want[:, 4:], size[:, 4:], "bf16", 64)
     assert torch.equal(Vc.cpu(), x[:, 6:]) and torch.equal(g[:, 4:].cpu(), x[:, 4:])
+
+
+def test_slots_beyond_32_bits(ctx):
+    """Rows of two layers at the end of pools of more than 2^31 elements."""
+    import torch
+    from paper_2512_14069_b200 import binding as rb
+    Hkv, d = 8, 128
+    rows = 2 ** 31 // (Hkv * d) + 64
+    pools = [torch.empty(2, rows, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    K, V = (torch.randn(2, 5, Hkv, d, device="cuda").bfloat16() for _ in range(2))
+    slots = torch.tensor([rows - 1, rows - 40, 3, -1, rows - 64], device="cuda")
+    for p in pools:
+        p[:, slots[slots >= 0]] = 7.0
+        p[:, rows - 2] = 7.0
+    rb.radar_paged_store(ctx, K=K, V=V, slots=slots, Kc=pools[0], Vc=pools[1])
+    torch.cuda.synchronize()
+    ctx.check_device_status()
+    for p, x in zip(pools, (K, V)):
+        assert torch.equal(p[:, slots[slots >= 0]], x[:, slots >= 0]) and torch.all(p[:, rows - 2] == 7.0)
