@@ -507,8 +507,6 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             // The vote on the waits comes first, and the branch of the one lane inside its branch: a product then takes 20 to 30 cycles to
             // issue, and 66 where one branch asks for both.  Some eight products queue up in front of the tensor cores, so that they have work
             // while this warp is in a wait.
-            constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTileKeys, false, false);
-            constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, false, true);
             // descriptors: stride between 8-row groups 1024 B, version, swizzle; in units of 16 bytes
             constexpr uint64_t kDesc = (uint64_t)((1024u >> 4) | (1u << 14) | (2u << 29)) << 32;
             constexpr uint32_t kHalfTile = kTileKeys * 128 >> 4;     // between the 64-column blocks of a tile
@@ -522,6 +520,10 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
                 const int seg_t0 = s.t0, n = s.n, keys = s.keys;
                 const bool two = s.rows > P.rb_rows;
+                // Up to 16 rows lie in the same lanes of products of 64 rows, which take the tensor cores half the energy: 64 requests of 1000 to 16384
+                // tokens, one row each, 32 / 8 heads, over and over under the power limit 412 -> 372 us (clock 1.0 -> 1.3 GHz), once 384 -> 375.
+                const uint32_t idesc_s = s.rows <= 16 ? idesc_bf16_f32(64, kTileKeys, false, false) : idesc_bf16_f32(128, kTileKeys, false, false);
+                const uint32_t idesc_pv = s.rows <= 16 ? idesc_bf16_f32(64, D, false, true) : idesc_bf16_f32(128, D, false, true);
                 ok = mbar_wait_while(ok, &st.bar_qfull, seg & 1);
                 uint32_t k_slot = 0, v_slot = 0;      // ring slots of the K and V tiles in use
                 uint32_t k_wait = 0, v_wait = 0;      // ... and the parities to wait for them with
