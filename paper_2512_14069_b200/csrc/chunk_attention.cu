@@ -7,7 +7,7 @@
 // 128 threads, two to an SM, has Q (64 rows), K and V (64 keys each) and P in shared memory; a thread holds 8 rows x 4 keys of the scores, then 8
 // rows x d / 16 channels of O, in pairs of rows that one instruction multiplies by a value.  (The scores in pairs of channels were slower, as was O one
 // by one: 2048 tokens over 2048 cached ones, 32 / 8 heads of 128: 885 us, 924 with O one by one, 1191 with one block an SM, a row of padding in P and
-// every tile rescaled.)  What bounds it: the issue of FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
+// every tile rescaled.)  A warp without live rows only fetches (8 requests of 16 rows over 16384 tokens 120 -> 87).  What bounds it: the issue of FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
 #include <algorithm>
 #include <climits>
 
@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
         Two o[4][4 * kCols];                                 // of rows 2 i and 2 i + 1
         float m[8], l[8];
         int lim[8];
+        const bool live = (ty & ~1) * 8 < u.rows;            // the warp has live rows; one that has none only fetches
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             m[i] = -CUDART_INF_F;
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
 #pragma unroll
                 for (int j = 0; j < 4; ++j) part[i][j] = 0.f;
 #pragma unroll 2
-            for (int c = 0; c < kVec; ++c) {
+            for (int c = 0; c < (live ? kVec : 0); ++c) {
                 float4 k4[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(sm.k + (tx + 16 * j) * D + (c ^ (tx & 7)) * 4);
@@ -157,53 +158,55 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             __syncthreads();
             if (more) fetch(a.Kc, sm.k, (t + 1 - t0) & 1, true);
             else copies_end();
-            // ---- softmax ----
-            float s[8][4];
-            bool passed = false;
+            if (live) {
+                // ---- softmax ----
+                float s[8][4];
+                bool passed = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? part[i][j] * P.scale_log2 : -CUDART_INF_F;
+                        passed |= s[i][j] > m[i] + kRescaleThreshold;
+                    }
+                if (__any_sync(kFull, passed)) {
+                    float factor[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+#pragma unroll
+                        for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+                        top = fmaxf(top, m[i]);
+                        factor[i] = ex2(m[i] - (top == -CUDART_INF_F ? 0.f : top));
+                        m[i] = top;
+                        l[i] *= factor[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const Two f = two_of(factor[2 * i], factor[2 * i + 1]);
+#pragma unroll
+                        for (int e = 0; e < 4 * kCols; ++e) o[i][e] = mul_two(o[i][e], f);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[i][j] = ex2(s[i][j] - (m[i] == -CUDART_INF_F ? 0.f : m[i]));
+                        l[i] += s[i][j];
+                    }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? part[i][j] * P.scale_log2 : -CUDART_INF_F;
-                    passed |= s[i][j] > m[i] + kRescaleThreshold;
+                    float* to = sm.p + tx * kPStride + j * kFmaRows + ty * 8;
+                    *reinterpret_cast<float4*>(to) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+                    *reinterpret_cast<float4*>(to + 4) = make_float4(s[4][j], s[5][j], s[6][j], s[7][j]);
                 }
-            if (__any_sync(kFull, passed)) {
-                float factor[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
-#pragma unroll
-                    for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-                    top = fmaxf(top, m[i]);
-                    factor[i] = ex2(m[i] - (top == -CUDART_INF_F ? 0.f : top));
-                    m[i] = top;
-                    l[i] *= factor[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const Two f = two_of(factor[2 * i], factor[2 * i + 1]);
-#pragma unroll
-                    for (int e = 0; e < 4 * kCols; ++e) o[i][e] = mul_two(o[i][e], f);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[i][j] = ex2(s[i][j] - (m[i] == -CUDART_INF_F ? 0.f : m[i]));
-                    l[i] += s[i][j];
-                }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float* to = sm.p + tx * kPStride + j * kFmaRows + ty * 8;
-                *reinterpret_cast<float4*>(to) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
-                *reinterpret_cast<float4*>(to + 4) = make_float4(s[4][j], s[5][j], s[6][j], s[7][j]);
             }
             copies_wait<1>();
             __syncthreads();
             // ---- O += P V ----
 #pragma unroll 4
-            for (int h = 0; h < 16; ++h)
+            for (int h = 0; h < (live ? 16 : 0); ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float* at = sm.p + h * kPStride + j * kFmaRows + ty * 8;

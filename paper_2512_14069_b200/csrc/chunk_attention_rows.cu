@@ -428,8 +428,8 @@ struct RowsLaunch {
 // fp32 against the form of whole tiles: up to 8 rows this one, but for a few units over very many keys, which that one spreads over the machine: 32 / 8
 // heads of 128 (4 rows): B = 1, 1024 tokens 8.3 / 24.3, 65536 174 / 427; B = 32, 4096 183 / 831; 8 / 1 heads of 64: B = 1, 16384 (16 chunks a warp,
 // 16 blocks) 30 / 58, 65536 113 / 84; B = 4, 65536 (64 blocks) 115 / 128.  16 rows, one block an SM: this one up to 8 chunks a warp or where the blocks fill
-// the machine: 16 / 1 heads of 128: B = 1, 4096 (4) 25 / 35, 16384 (16) 70 / 67; B = 4, 16384 (8) 71 / 81, 65536 (32) 255 / 228; B = 16, 16384 (64)
-// 252 / 219; B = 32, 16384 (64, filled) 254 / 423.
+// the machine: 16 / 1 heads of 128: B = 1, 8192 tokens (8) 38 / 45, 16384 (16) 67 / 63; B = 4, 8192 (8) 41 / 43, 16384 (16) 72 / 63; B = 16, 2048 (8)
+// 39 / 34, 16384 (64) 253 / 149; B = 32, 16384 (64, filled) 255 / 278.
 template <typename T, int D, int R>
 int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool& taken) {
     void (*kernel)(ChunkParams, int);
