@@ -31,7 +31,7 @@ constexpr int kEpilogueWarp = 8, kProducerWarp = 12, kMmaWarp = 13, kValueWarp =
 // Registers a thread: 128 at launch, then shared out by warpgroup (two of softmax; what they take the other two give).
 constexpr int kSoftmaxRegs = 176, kEpilogueRegs = 88, kIssueRegs = 72;
 static_assert(2 * kSoftmaxRegs + kEpilogueRegs + kIssueRegs <= 512, "a block shares out the registers it was launched with");
-constexpr int kStaticSmem = 3072;    // barriers and exchange arrays: with the tiles exactly the 227 KB a block may have
+constexpr int kStaticSmem = 3 * 1024;    // barriers and exchange arrays: with the tiles exactly the 227 KB a block may have
 
 template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
