@@ -7,7 +7,8 @@
 // 128 threads, two to an SM, has Q (64 rows), K and V (64 keys each) and P in shared memory; a thread holds 8 rows x 4 keys of the scores, then 8
 // rows x d / 16 channels of O, in pairs of rows that one instruction multiplies by a value.  (The scores in pairs of channels were slower, as was O one
 // by one: a prompt of 2048 tokens, 32 / 8 heads of 128: 885 us, 924 with O one by one, 1191 with one block an SM, a row of padding in P and
-// every tile rescaled.)  A warp without live rows only fetches (8 requests of 16 rows over 16384 tokens 120 -> 87).  What bounds it: the issue of FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
+// every tile rescaled.)  A warp without live rows only fetches (8 requests of 16 rows over 16384 tokens 120 -> 87).  What bounds it: the issue of
+// FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
 #include <algorithm>
 #include <climits>
 
