@@ -294,3 +294,13 @@ def test_pools_at_addresses_of_16_bytes(ctx):
         torch.cuda.synchronize()
         ctx.check_device_status()
         T.hold_again(kw, range(3))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4), (32, 8), (16, 1), (17, 1)])
+def test_few_rows_in_tiles(ctx, Hq, Hkv, d):
+    """Units of up to 16 rows, and of 17, in the tiles that long caches take; pieces of them in several blocks."""
+    import paged_harness as T
+    G = Hq // Hkv
+    for news, lens in (([1, 16 // G if G <= 16 else 1, 0, 1], [5000, 700, 40, 128]), ([16 // G + 1, 1], [257, 9000])):
+        T.check_chunk(ctx, _rng(G), news, lens, Hq, Hkv, d, 32, max_len=60000)
