@@ -59,6 +59,13 @@ struct __align__(16) Segment {
     int seen, keys, rows, row0, b, g;    // of the unit (keys: 0 where its last token sees none)
 };
 
+// Units of up to kSmallRows rows are products of 64 rows, of which a warp has 16, in its first lanes (what the others hold is never read); a larger
+// row block is one of 128, 32 to a warp.  Half the rows are half the tensor cores' energy.  Over and over, under the power limit, 32 / 8 heads of
+// 128, 64 / 128 rows: 64 requests of 1000 to 16384 tokens, one row each, 372 us (clock 1.3 GHz) / 412 (1.0); 32 of 8192 tokens, 8 new ones 184 / 191;
+// 64 / 8 heads, 7 new ones 193 / 204.
+constexpr int kSmallRows = 64;
+__device__ __forceinline__ int row_at(const Segment& s, int quarter, int lane) { return quarter * (s.rows <= kSmallRows ? 16 : 32) + lane; }
+
 // The pages of a tile: lane p of a warp looks up and fetches page p, up to eight boxes of a tile (one where a page holds whole tiles).  Only
 // pages that hold keys which the unit sees are fetched; what stays stale in the slot is masked or never read.
 struct Pages {
@@ -174,22 +181,22 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         // =================================== softmax groups ===================================
         // One thread per query row, which holds the tile's 128 scores in registers.
         const int grp = warp >> 2;
-        const int row = (warp & 3) * 32 + lane;                 // row of the block == tensor-memory lane
+        const int place = (warp & 3) * 32 + lane;                // tensor-memory lane
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + grp * 128 + lane_addr;
         const uint32_t tO = tmem + 256 + grp * 128 + lane_addr;
-        const int rb_token = (int)(((uint32_t)row * P.g_magic) >> 16);       // row / G
         uint32_t sc = 0;                         // S tiles this group has waited for
         Segment s;
         for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
             const bool two = s.rows > P.rb_rows;
             const int blk = two ? grp : 0;                       // row block within the unit
+            const int row0 = row_at(s, warp & 3, 0), row = row0 + lane;      // rows of the block: the warp's first one, the thread's
             const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
             // A warp none of whose 32 rows is live does no arithmetic (the products of its rows are never read):
             // it only keeps the barriers going.
-            const bool warp_live = row - lane < rows_here;
-            const int lim = s.seen + blk * P.tokens_per_rb + rb_token;       // keys that this row sees (more than there are for rows that are not live)
-            const int lim_warp = s.seen + blk * P.tokens_per_rb + (int)(((uint32_t)(row - lane) * P.g_magic) >> 16);    // ... and the warp's first one
+            const bool warp_live = row0 < rows_here;
+            const int lim = s.seen + blk * P.tokens_per_rb + (int)(((uint32_t)row * P.g_magic) >> 16);       // keys that this row sees (more than there are for rows that are not live)
+            const int lim_warp = s.seen + blk * P.tokens_per_rb + (int)(((uint32_t)row0 * P.g_magic) >> 16);    // ... and the warp's first one
             const int n_my = two ? s.n : (s.n - grp + 1) >> 1;
             float m_run = -CUDART_INF_F, l_run = 0.f;
 
@@ -309,7 +316,7 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 
             // the rows' (m, l) go to the epilogue, which has taken those of the segment before
             ok = mbar_wait_while(ok, &st.bar_mlempty, (seg & 1) ^ 1);
-            st.ml[grp][row] = make_float2(m_run, l_run);
+            st.ml[grp][place] = make_float2(m_run, l_run);
             __syncwarp();
             if (lane == 0) mbar_arrive(&st.bar_mlfull);
         }
@@ -319,9 +326,8 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         // =================================== epilogue ===================================
         // One thread per tensor-memory lane takes the finished accumulators to O (or to the partials) while the softmax
         // groups and the tensor cores are already in the next segment; each accumulator is handed back as soon as it is read.
-        const int row = (warp - kEpilogueWarp) * 32 + lane;
+        const int place = (warp - kEpilogueWarp) * 32 + lane;
         const uint32_t tO = tmem + 256 + ((uint32_t)((warp - kEpilogueWarp) * 32) << 16);
-        const int rb_token = (int)(((uint32_t)row * P.g_magic) >> 16);       // row / G
         uint32_t oc[2] = {0, 0};             // accumulators waited for
         Segment s;
         for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
@@ -329,7 +335,9 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const bool final_rows = s.n == s.nt;                 // the whole unit
             const int slot = seg == 0 ? 0 : 1;                   // a CTA has at most a cut first and a cut last segment
             ok = mbar_wait_lazy(ok, &st.bar_mlfull, seg & 1);
-            const float2 ml0 = st.ml[0][row], ml1 = st.ml[1][row];
+            const int row = row_at(s, warp - kEpilogueWarp, lane), rb_token = (int)(((uint32_t)row * P.g_magic) >> 16);       // row / G
+            const bool held = s.rows > kSmallRows || lane < 16;
+            const float2 ml0 = st.ml[0][place], ml1 = st.ml[1][place];
             __syncwarp();
             if (lane == 0) mbar_arrive(&st.bar_mlempty);
 #pragma unroll 1
@@ -349,7 +357,7 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 ok = __all_sync(kFull, ok);
                 tc_fence_after_sync();
                 const int rows_here = min(s.rows - blk * P.rb_rows, P.rb_rows);  // live rows of this row block
-                const bool row_live = row < rows_here;
+                const bool row_live = held && row < rows_here;
                 if (ok && row - lane < rows_here) {
                     float m_out = blk == 0 ? ml0.x : ml1.x, l_out = blk == 0 ? ml0.y : ml1.y, w0 = 1.f, w1 = 0.f;
                     if (merge) {
@@ -520,10 +528,8 @@ chunk_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (uint32_t seg = 0; take_segment(seg, s); ++seg) {
                 const int seg_t0 = s.t0, n = s.n, keys = s.keys;
                 const bool two = s.rows > P.rb_rows;
-                // Up to 16 rows lie in the same lanes of products of 64 rows, which take the tensor cores half the energy: 64 requests of 1000 to 16384
-                // tokens, one row each, 32 / 8 heads, over and over under the power limit 412 -> 372 us (clock 1.0 -> 1.3 GHz), once 384 -> 375.
-                const uint32_t idesc_s = s.rows <= 16 ? idesc_bf16_f32(64, kTileKeys, false, false) : idesc_bf16_f32(128, kTileKeys, false, false);
-                const uint32_t idesc_pv = s.rows <= 16 ? idesc_bf16_f32(64, D, false, true) : idesc_bf16_f32(128, D, false, true);
+                const uint32_t idesc_s = s.rows <= kSmallRows ? idesc_bf16_f32(64, kTileKeys, false, false) : idesc_bf16_f32(128, kTileKeys, false, false);
+                const uint32_t idesc_pv = s.rows <= kSmallRows ? idesc_bf16_f32(64, D, false, true) : idesc_bf16_f32(128, D, false, true);
                 ok = mbar_wait_while(ok, &st.bar_qfull, seg & 1);
                 uint32_t k_slot = 0, v_slot = 0;      // ring slots of the K and V tiles in use
                 uint32_t k_wait = 0, v_wait = 0;      // ... and the parities to wait for them with

@@ -304,3 +304,12 @@ def test_few_rows_in_tiles(ctx, Hq, Hkv, d):
     G = Hq // Hkv
     for news, lens in (([1, 16 // G if G <= 16 else 1, 0, 1], [5000, 700, 40, 128]), ([16 // G + 1, 1], [257, 9000])):
         T.check_chunk(ctx, _rng(G), news, lens, Hq, Hkv, d, 32, max_len=60000)
+
+
+@pytest.mark.parametrize("rows", [17, 32, 33, 63, 64, 65, 100])
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 4, 128), (32, 8, 64), (17, 1, 128), (40, 1, 64)])
+def test_small_units_in_tiles(ctx, Hq, Hkv, d, rows):
+    """Units at the bounds of the products' sizes, whole and in pieces, beside smaller ones."""
+    import paged_harness as T
+    n = max(1, rows // (Hq // Hkv))
+    T.check_chunk(ctx, _rng(rows), [n, 1, max(1, n // 2)], [n + 700, 9000, 300], Hq, Hkv, d, 32, max_len=60000)
