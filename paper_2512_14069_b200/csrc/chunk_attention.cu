@@ -5,10 +5,10 @@
 //
 // A head group is a KV head's G query heads (one query head where G is above 64, so that a unit holds a whole token), a unit 64 rows.  A block of
 // 128 threads, two to an SM, has Q (64 rows), K and V (64 keys each) and P in shared memory; a thread holds 8 rows x 4 keys of the scores, then 8
-// rows x d / 16 channels of O, in pairs of rows that one instruction multiplies by a value.  (The scores in pairs of channels were slower, as was O one
-// by one: a prompt of 2048 tokens, 32 / 8 heads of 128: 885 us, 924 with O one by one, 1191 with one block an SM, a row of padding in P and
-// every tile rescaled.)  A warp without live rows only fetches (8 requests of 16 rows over 16384 tokens 120 -> 87).  What bounds it: the issue of
-// FMAs with two warps to a scheduler: 39 TFLOP/s of the 72 that FMAs alone reach.
+// rows x d / 16 channels of O, in pairs of rows that one instruction multiplies by a key's or value's channel.  A prompt of 2048 tokens, 32 / 8 heads
+// of 128: 842 us; 888 with scores one by one from rows side by side, 924 with O one by one too, 1191 with one block an SM, a row of padding in P
+// and every tile rescaled.  A warp without live rows only fetches (8 requests of 16 rows over 16384 tokens 120 -> 87).  What bounds it: the issue of
+// FMAs with two warps to a scheduler: 41 TFLOP/s of the 72 that FMAs alone reach (three blocks an SM, d = 64: no faster).
 #include <algorithm>
 #include <climits>
 
@@ -109,11 +109,13 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
         };
         __syncthreads();                                     // the segment before has read its rows
         look_up(t0, 0);
+        // queries are stored channel by channel, so that a thread has rows side by side
         for (int i = tid; i < kFmaRows * kVec; i += kFmaThreads) {
-            const int r = i / kVec, c = i % kVec, token = (int)(((uint32_t)r * P.g_magic) >> 16);
+            const int r = i % kFmaRows, c = i / kFmaRows, token = (int)(((uint32_t)r * P.g_magic) >> 16);
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < u.rows) x = *reinterpret_cast<const float4*>(Q + (int64_t)(u.row0 + token) * a.q_row_stride + (int64_t)(g * P.G + r - token * P.G) * D + c * 4);
-            *reinterpret_cast<float4*>(sm.q + r * D + (c ^ ((r >> 3) & 7)) * 4) = x;
+            float* const to = sm.q + c * 4 * kFmaRows + r;
+            to[0] = x.x; to[kFmaRows] = x.y; to[2 * kFmaRows] = x.z; to[3 * kFmaRows] = x.w;
         }
         __syncthreads();
         fetch(a.Kc, sm.k, 0, true);
@@ -139,21 +141,27 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             copies_wait<1>();
             __syncthreads();
             // ---- 8 rows x 4 keys of S: the keys tx, tx + 16, .. ----
-            float part[8][4];
+            Two part[4][4];                                  // of rows 2 i and 2 i + 1
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) part[i][j] = 0.f;
-#pragma unroll 2
+                for (int j = 0; j < 4; ++j) part[i][j] = 0;
+#pragma unroll 8
             for (int c = 0; c < (live ? kVec : 0); ++c) {
-                float4 k4[4];
+                float k4[4][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(sm.k + (tx + 16 * j) * D + (c ^ (tx & 7)) * 4);
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(k4[j]) = *reinterpret_cast<const float4*>(sm.k + (tx + 16 * j) * D + (c ^ (tx & 7)) * 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 q4 = *reinterpret_cast<const float4*>(sm.q + (ty * 8 + i) * D + (c ^ ty) * 4);
+                for (int e = 0; e < 4; ++e) {
+                    const float* at = sm.q + (c * 4 + e) * kFmaRows + ty * 8;
+                    const ulonglong2 q0 = *reinterpret_cast<const ulonglong2*>(at), q1 = *reinterpret_cast<const ulonglong2*>(at + 4);
+                    const Two q[4] = {q0.x, q0.y, q1.x, q1.y};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) part[i][j] = fmaf(q4.x, k4[j].x, fmaf(q4.y, k4[j].y, fmaf(q4.z, k4[j].z, fmaf(q4.w, k4[j].w, part[i][j]))));
+                    for (int j = 0; j < 4; ++j) {
+                        const Two k2 = two_of(k4[j][e], k4[j][e]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[i][j] = fma_two(q[i], k2, part[i][j]);
+                    }
                 }
             }
             __syncthreads();
@@ -167,7 +175,7 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
                 for (int i = 0; i < 8; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? part[i][j] * P.scale_log2 : -CUDART_INF_F;
+                        s[i][j] = t * kFmaKeys + tx + 16 * j < lim[i] ? (i & 1 ? both(part[i >> 1][j]).y : both(part[i >> 1][j]).x) * P.scale_log2 : -CUDART_INF_F;
                         passed |= s[i][j] > m[i] + kRescaleThreshold;
                     }
                 if (__any_sync(kFull, passed)) {
@@ -206,7 +214,7 @@ __global__ void __launch_bounds__(kFmaThreads, 2) chunk_attn_fma_kernel(const Ch
             copies_wait<1>();
             __syncthreads();
             // ---- O += P V ----
-#pragma unroll 4
+#pragma unroll 8
             for (int h = 0; h < (live ? 16 : 0); ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
