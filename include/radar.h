@@ -590,7 +590,8 @@ int radar_rotate(radar_ctx* ctx, const radar_rotate_args* args, void* stream);
  * cache row slots[i] of Kc and Vc, [cache_rows][Hkv][d] as radar_tree_attention and radar_chunk_attention read them (slot = page *
  * page_size + row in the page: what radar_cache_extend gives); the turned queries to row i of Q_out.  rotation.pos NULL: rows as they are
  * (what a step accepted: its keys were turned before the verification).  A slot below 0 is skipped (a token that was not granted; its query is
- * turned all the same); one at or beyond cache_rows, or a row outside [0, n_rows), records RADAR_ERR_INVALID_ARG and is skipped.
+ * turned all the same, and without queries its src_row may be anything); one at or beyond cache_rows, or another token's row outside [0, n_rows),
+ * records RADAR_ERR_INVALID_ARG and is skipped.
  * No two tokens of a call may have one slot.  K and V share strides.  Q may be NULL with Hq 0; Q_out may be Q where there is no src_row
  * (same address and strides).  d, alignment and positions as in radar_rotate; row and layer strides in elements. */
 typedef struct {

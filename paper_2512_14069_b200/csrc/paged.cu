@@ -116,14 +116,16 @@ __global__ void __launch_bounds__(kThreads, 4) paged_rows_kernel(const PagedPara
         const int64_t token = first + r;
         from[r] = r < n ? token : -1;
         to[r] = token;
+        bool lost = false;
         if (r < n && P.src_row != nullptr) {
             from[r] = P.src_row[token];
-            if (from[r] < 0 || from[r] >= P.n_rows) { bad = true; from[r] = -1; }
+            if (from[r] < 0 || from[r] >= P.n_rows) { lost = true; from[r] = -1; }
         }
         if (r < n && P.slots != nullptr) {
             to[r] = P.slots[token];
             if (to[r] >= P.cache_rows) { bad = true; to[r] = -1; }
         }
+        bad |= lost && (to[r] >= 0 || P.heads[0] > 0);       // (behind a slot below 0, where no query goes with it, stands nobody's row)
     }
     if (bad && threadIdx.x == 0) set_status(P.status, RADAR_ERR_INVALID_ARG);
 
