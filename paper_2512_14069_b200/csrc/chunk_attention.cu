@@ -273,9 +273,7 @@ int fma_most_ctas(const radar_ctx* ctx) { return std::min(2 * ctx->sm_count, kMa
 template <int D>
 int fma_launch(radar_ctx* ctx, const radar_chunk_attn_args& a, cudaStream_t stream) {
     ChunkParams P = chunk_params(ctx, a, fma_group(a.Hq, a.Hkv), kFmaRows, 1);
-    const long long units = (long long)a.B * P.groups * ((a.max_new + P.unit_tokens - 1) / P.unit_tokens);
-    const long long tiles = units * std::max(1, (a.max_cache_len + kFmaKeys - 1) / kFmaKeys);
-    P.n_cta = (int)std::max<long long>(1, std::min<long long>(fma_most_ctas(ctx), tiles));
+    P.n_cta = chunk_ctas(P, fma_most_ctas(ctx), std::max(1, (a.max_cache_len + kFmaKeys - 1) / kFmaKeys));
     chunk_carve(P);
     RADAR_CUDA_CHECK(radar_opt_in_smem(ctx, RADAR_SMEM_CHUNK_FMA + (D == 128), chunk_attn_fma_kernel<D>, sizeof(FmaSmem<D>)));
     {

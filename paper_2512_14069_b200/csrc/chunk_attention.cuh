@@ -6,6 +6,8 @@
 // diagonal costs what it holds.  A unit that falls into one CTA is normalised and written at once; the pieces of one that was cut are
 // fp32 partials (m, l, O), merged by chunk_combine_kernel.
 #pragma once
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace radar {
@@ -398,6 +400,13 @@ inline ChunkParams chunk_params(const radar_ctx* ctx, const radar_chunk_attn_arg
     P.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)a.d)) * 1.4426950408889634f;
     P.status = ctx->d_status;
     return P;
+}
+// CTAs of a launch: `pieces` for every unit that the bounds allow, `most` of them at most (which cuts every step of the product, as the bounds may be
+// any ints)
+inline int chunk_ctas(const ChunkParams& P, int most, long long pieces) {
+    long long n = 1;
+    for (const long long x : {(long long)P.a.B, (long long)P.groups, ((long long)P.a.max_new + P.unit_tokens - 1) / P.unit_tokens, pieces}) n = std::min((long long)most, n * x);
+    return (int)std::max(1ll, n);
 }
 template <typename T, int D>
 int chunk_combine(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream) {

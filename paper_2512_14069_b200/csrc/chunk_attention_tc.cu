@@ -749,9 +749,8 @@ int chunk_tc_launch(radar_ctx* ctx, const radar_chunk_attn_args* a, cudaStream_t
     // One CTA per SM, but no more than make a unit of the bounds' size the fastest by itself: a CTA takes 0.8 us a tile, the merge 0.11 a piece, so
     // sqrt(7 tiles) pieces.  (us, half as many pieces as tiles / these: one unit of 63 tiles 16.4 / 15.4, of 250 33.0 / 23.4; 8 of 4 19.1 / 17.0; 16 of
     // one 12.8 / 9.9.)
-    const long long units = (long long)a->B * a->Hkv * ((a->max_new + P.unit_tokens - 1) / P.unit_tokens);
     const long long tiles = std::max(1, (a->max_cache_len + kTileKeys - 1) / kTileKeys), pieces = std::min(tiles, (long long)std::ceil(std::sqrt(7.0 * tiles)));
-    P.n_cta = (int)std::max<long long>(1, std::min<long long>(most_ctas(ctx), units * pieces));
+    P.n_cta = chunk_ctas(P, most_ctas(ctx), pieces);
     chunk_carve(P);
     return a->d == 128 ? launch_d<128>(ctx, P, stream) : launch_d<64>(ctx, P, stream);
 }
