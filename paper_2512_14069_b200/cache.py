@@ -119,7 +119,7 @@ class PagedCache(_Requests):
         also the rows of all requests in a chunk."""
         super().__init__(ctx, n_layers, B, Hq, Hkv, d, page_size, n_pages, max_len, max_new, device)
         self.Kc, self.Vc = (torch.zeros((n_layers, n_pages * page_size, Hkv, d), dtype=dtype, device=torch.device(device)) for _ in range(2))
-        self.pos, self.n = torch.zeros(max_new, dtype=torch.int32, device=self.slots.device), 0
+        self.pos, self.n = torch.zeros(max_new, dtype=torch.int32, device=self.slots.device), None        # (n None: there is no chunk)
         self._row = torch.arange(max_new, dtype=torch.int32, device=self.slots.device)
         self._workspace(rb.radar_chunk_attn_workspace_bytes(ctx, B, Hq, Hkv, d, rb.dtype_code(self.Kc), max_new, self.max_len))
 
@@ -127,15 +127,23 @@ class PagedCache(_Requests):
         """Room for a chunk: new_len [B] int32 on the GPU, new tokens of each request, n their sum (or more: rows behind the last one are
         left out).  Behind it `slots`, `pos` (the rows' positions) and `start` (the requests' first rows) are the chunk's.  Requests that
         the pool had no pages for, or the table no room, are left as they are, as `granted` says; their rows reach no cache and their
-        attention's output says nothing.  requests as in `FourBitCache.admit`."""
+        attention's output says nothing.  requests as in `FourBitCache.admit`.
+
+        `append` and `release` share out slots and pages anew, and with them the chunk is over: `store` and `attention` refuse to run
+        until the next `begin`.  (Parts of a round that are captured as graphs of their own have to be captured, and replayed, in such an order.)"""
         self._added(new_len, n, requests)
         self.n = n
         b = torch.searchsorted(self.start[1:], self._row[:n], right=True).clamp_(max=self.B - 1)
         torch.add(self.cache_len[b] - self.start[1:][b], self._row[:n], out=self.pos[:n])
 
+    def _chunk(self):
+        if self.n is None:
+            raise ValueError("there is no chunk: begin makes room for one, and append and release end it")
+
     def store(self, layer, K, V, *, Q=None, Q_out=None, pos=None, **rotation):
         """The chunk's rows of a layer, K and V [n, Hkv, d], into their slots.  With inv_freq (and pair_axis, neighbours, as in
         `radar_rotate`) keys and queries are turned by their positions, `pos` or those given [axes, n]; Q [n, Hq, d] into Q_out."""
+        self._chunk()
         if rotation.get("inv_freq") is not None:
             rotation["pos"] = self.pos[:self.n] if pos is None else pos
         rb.radar_paged_store(self.ctx, K=K, V=V, slots=self.slots[:self.n], Kc=self.Kc[layer], Vc=self.Vc[layer], Q=Q, Q_out=Q_out, **rotation)
@@ -144,6 +152,7 @@ class PagedCache(_Requests):
         """radar_chunk_attention of the chunk's rows, Q [n, Hq, d], over one layer's pool, where `store` has put their keys and values.  max_new,
         max_cache_len: bounds of a request's rows and tokens, if the caller has nearer ones than the chunk's and the cache's: the
         form that takes the call goes by them (single tokens want max_new = 1)."""
+        self._chunk()
         rb.radar_chunk_attention(self.ctx, Q=Q, q_start=self.start, Kc=self.Kc[layer], Vc=self.Vc[layer], page_size=self.page_size, block_table=self.block_table,
                                  cache_len=self.cache_len, max_new=self.n if max_new is None else max_new,
                                  max_cache_len=self.max_len if max_cache_len is None else max_cache_len, O=O, lse=lse, workspace=self.workspace, scale=scale)
@@ -151,4 +160,9 @@ class PagedCache(_Requests):
     def append(self, step, K, V):
         """What a step accepted, as `FourBitCache.append`; the keys as they were verified, turned already."""
         slots, src_row = self._accepted(step, K.shape[2])
+        self.n = None
         rb.radar_paged_store(self.ctx, K=K.flatten(1, 2), V=V.flatten(1, 2), slots=slots, src_row=src_row, Kc=self.Kc, Vc=self.Vc)
+
+    def release(self, finished):
+        super().release(finished)
+        self.n = None
