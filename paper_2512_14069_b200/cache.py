@@ -146,6 +146,8 @@ class PagedCache(_Requests):
         self._chunk()
         if rotation.get("inv_freq") is not None:
             rotation["pos"] = self.pos[:self.n] if pos is None else pos
+        elif pos is not None or rotation.get("pair_axis") is not None or rotation.get("neighbours"):
+            raise ValueError("pos, pair_axis and neighbours: expected inv_freq beside them")
         rb.radar_paged_store(self.ctx, K=K, V=V, slots=self.slots[:self.n], Kc=self.Kc[layer], Vc=self.Vc[layer], Q=Q, Q_out=Q_out, **rotation)
 
     def attention(self, layer, Q, O, lse=None, *, max_new=None, max_cache_len=None, scale=0.0):

@@ -76,3 +76,21 @@ def test_a_chunk_of_nothing_is_one(calls):
     c.begin(torch.zeros(2, dtype=torch.int32), 0)
     c.store(0, K[:0], K[:0])
     c.attention(0, Q[:0], Q[:0])
+
+
+def test_positions_without_a_rotation_are_refused(calls):
+    """pos, pair_axis and neighbours say how inv_freq turns rows; without it they would be left out of account."""
+    c = _cache()
+    c.begin(NEW, 5)
+    n = len(calls)
+    pos, axis, freq = torch.zeros(5, dtype=torch.int32), torch.zeros(32, dtype=torch.uint8), torch.ones(32)
+    for turn in (dict(pos=pos), dict(pair_axis=axis), dict(neighbours=True), dict(pos=pos, pair_axis=axis, neighbours=True, inv_freq=None)):
+        with pytest.raises(ValueError, match="inv_freq"):
+            c.store(0, K, K, **turn)
+    assert len(calls) == n
+    c.store(0, K, K, neighbours=False, pair_axis=None, inv_freq=None)
+    assert calls[-1][1].get("pos") is None
+    c.store(0, K, K, inv_freq=freq, pair_axis=axis, neighbours=True)
+    assert calls[-1][1]["pos"].data_ptr() == c.pos.data_ptr() and calls[-1][1]["pos"].numel() == 5
+    c.store(0, K, K, inv_freq=freq, pos=pos)
+    assert calls[-1][1]["pos"] is pos
