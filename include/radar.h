@@ -624,8 +624,10 @@ int radar_paged_store(radar_ctx* ctx, const radar_paged_store_args* args, void* 
  * Values of the tokens that any row of a request sees have to be finite (a probability of 0 times infinity or NaN is NaN); keys that a row does
  * not attend to may hold anything, and so may the cache behind a request's last token.
  * RADAR_BF16: products on the tensor cores, probabilities enter P V as bf16, sums in fp32.  RADAR_F32: fp32 throughout.  Calls of up to 16
- * rows to a KV head and request (max_new * Hq / Hkv) take a form of one launch while there is little to read; the others are an attention and a
- * merge kernel.  Which one it is goes by the bounds and B, so the order of a row's sums does too; equal calls give equal bits.
+ * rows to a KV head and request (max_new * Hq / Hkv) over Kc and Vc at multiples of 32 bytes take a form of one launch while there is little to read;
+ * the others are an attention and a merge kernel.  The form goes by the bounds, B, Hq, Hkv, d, the type, whether the pool lies at such an address, and the
+ * device (its SMs and the clusters that fit it); how a form cuts the work goes by these and by all requests' sizes.  The order of a row's sums, and
+ * with it the last bits, follows from both.  Calls that agree in all of it give equal bits.
  * Limits: d in {64, 128}; Hq a multiple of Hkv, at most 128 query heads to a KV head; B <= 65535; n_rows, cache_rows < 2^31; max_cache_len at most 2^31 -
  * 2^14 - 1.  Q, Kc, Vc and O: 16 bytes, as are the row stride times the element size; the workspace: 256.  The workspace's size is enough for fewer requests, shorter ones
  * and fewer rows; calls that may overlap need one each. */
