@@ -64,9 +64,10 @@ class _Requests:
 
     def _accepted(self, step, rows):
         """Slots and rows of what a step accepted."""
-        if step.path_nodes.numel() > self.slots.numel():
-            raise ValueError(f"a step may accept {step.path_nodes.numel()} tokens, the cache was made for {self.slots.numel()} in a call")
-        return self._extend(torch.where(self.live, step.accept_len, -1), extra=1, path_nodes=step.path_nodes, rows=rows)
+        n = step.path_nodes.numel()
+        if n > self.slots.numel():
+            raise ValueError(f"a step may accept {n} tokens, the cache was made for {self.slots.numel()} in a call")
+        return self._extend(torch.where(self.live, step.accept_len, -1), extra=1, n=n, path_nodes=step.path_nodes, rows=rows)
 
     def release(self, finished):
         """Gives up the tokens of the requests with finished[b] != 0 ([B] on the GPU)."""

@@ -94,3 +94,12 @@ def test_positions_without_a_rotation_are_refused(calls):
     assert calls[-1][1]["pos"].data_ptr() == c.pos.data_ptr() and calls[-1][1]["pos"].numel() == 5
     c.store(0, K, K, inv_freq=freq, pos=pos)
     assert calls[-1][1]["pos"] is pos
+
+
+def test_an_append_is_of_the_steps_size(calls):
+    """... and not of the room for a chunk: a step accepts path_nodes.numel() tokens at most, whatever the cache was made for."""
+    c = _cache()
+    c.append(STEP, TREE, TREE)
+    (_, extend), (_, store) = calls[-2:]
+    assert extend["slots"].numel() == extend["src_row"].numel() == store["slots"].numel() == store["src_row"].numel() == STEP.path_nodes.numel() < c.slots.numel()
+    assert extend["slots"].data_ptr() == store["slots"].data_ptr() and extend["src_row"].data_ptr() == store["src_row"].data_ptr()
