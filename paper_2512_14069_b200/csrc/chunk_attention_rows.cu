@@ -422,14 +422,18 @@ struct RowsLaunch {
 //
 // Where a warp would go through many chunks, one load behind the other, the tensor cores' form with its copies in flight is the faster
 // one: beyond 8 chunks a warp, 24 where the blocks fill the machine (which then has enough loads in flight).  One token, us, this form / that
-// one, 32 / 8 heads of 128: B = 1, 1024 tokens 6.3 / 12.5, 4096 (2 chunks a warp) 11.3 / 16.0, 16384 (8) 25.8 / 24.4, 65536 (32) 76 / 54; B = 2, 4096
-// (4) 15.4 / 18.0, 16384 (16) 41 / 34; B = 8, 4096 (8) 27.8 / 32.8; filled: B = 32, 1024 (8) 27 / 36, 4096 (32) 88 / 93; B = 128, 1024 (8) 98 / 102, 4096
-// (32) 344 / 327; 16 / 1 heads: B = 1, 16384 (8) 16.6 / 27.3; B = 8, 16384 (16) 32 / 25; B = 64, 4096 (16, filled) 32 / 35.
+// one (chunks a warp), 32 / 8 heads of 128: B = 1, 1024 tokens 6.3 / 11.6, 4096 (2) 10.8 / 15.1, 8192 (4) 16.3 / 18.0, 16384 (8) 25.7 / 24.0, 32768 (16)
+// 42.8 / 34.5, 65536 (32) 75 / 54; B = 2, 4096 (4) 14.9 / 17.1, 8192 (8) 24.1 / 22.9, 16384 (16) 40.9 / 33.5; filled: B = 8, 4096 (8) 28.2 / 32.3, 8192
+// (16) 48.8 / 51.9; B = 32, 1024 (8) 27.0 / 34.5, 4096 (32) 88.8 / 92.9, 8192 (64) 170.4 / 169.6; B = 128, 1024 (8) 98.5 / 96.3, 2048 (16) 183 / 174, 4096
+// (32) 348 / 328; 16 / 1 heads: B = 1, 16384 (8) 16.5 / 18.9, 32768 (16) 25.7 / 23.6; B = 8, 8192 (8) 18.5 / 18.3, 16384 (16) 32.0 / 24.4; B = 64, 4096
+// (16, filled) 31.6 / 33.4, 8192 (32) 55.2 / 53.1.  So the forms meet between 4 and 16 chunks, or between 8 and 64, and near the rule's bounds either may be
+// up to 7 % ahead.
 // fp32 against the form of whole tiles: up to 8 rows this one, but for a few units over very many keys, which that one spreads over the machine: 32 / 8
-// heads of 128 (4 rows): B = 1, 1024 tokens 8.3 / 24.3, 65536 174 / 427; B = 32, 4096 183 / 831; 8 / 1 heads of 64: B = 1, 16384 (16 chunks a warp,
-// 16 blocks) 30 / 58, 65536 113 / 84; B = 4, 65536 (64 blocks) 115 / 128.  16 rows, one block an SM: this one up to 8 chunks a warp or where the blocks fill
-// the machine: 16 / 1 heads of 128: B = 1, 8192 tokens (8) 38 / 45, 16384 (16) 67 / 63; B = 4, 8192 (8) 41 / 43, 16384 (16) 72 / 63; B = 16, 2048 (8)
-// 39 / 34, 16384 (64) 253 / 149; B = 32, 16384 (64, filled) 255 / 278.
+// heads of 128 (4 rows): B = 1, 1024 tokens 8.4 / 19.1, 65536 174 / 268; B = 32, 4096 180 / 517; 8 / 1 heads of 64 (8 rows): B = 1, 16384 (16 chunks a warp,
+// 16 blocks) 30 / 54, 65536 112 / 72; B = 4, 16384 33 / 40.  (From a quarter of the SMs' number of blocks on the rule asks no more for the length, which
+// costs where 8 rows meet a very long cache: B = 4, 65536 117 / 88; B = 8 166 / 145.)  16 rows, one block an SM: this one up to 8 chunks a warp or where
+// the blocks fill the machine: 16 / 1 heads of 128: B = 1, 8192 tokens (8) 38 / 43, 16384 (16) 67 / 61, 65536 (64) 252 / 93; B = 4, 8192 (8) 40 / 42, 16384 (16)
+// 72 / 60; B = 16, 2048 (8) 38 / 33, 4096 (16) 70 / 52; B = 32, 2048 (8, filled) 40 / 51, 16384 (64, filled) 254 / 266.
 template <typename T, int D, int R>
 int launch_rows(radar_ctx* ctx, const ChunkParams& P, cudaStream_t stream, bool& taken) {
     void (*kernel)(ChunkParams, int);
